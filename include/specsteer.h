@@ -47,7 +47,8 @@ typedef enum {
   SPECSTEER_ERR_STATIC_LIMIT = 7 /* specsteer_verify_round_static: the shape does not fit the fixed scratch */
 } specsteer_status;
 
-typedef enum { SPECSTEER_F32 = 0, SPECSTEER_BF16 = 1 } specsteer_dtype;
+/* F16: the paged cache's operators only; the rounds take float32 or bf16 logits. */
+typedef enum { SPECSTEER_F32 = 0, SPECSTEER_BF16 = 1, SPECSTEER_F16 = 2 } specsteer_dtype;
 
 /* How alpha_t is formed for drafted token y at position t.
  *   RATIO    alpha = min(1, P_LLM(y) / (lambda * P_SLM-(y)))                (Eq. 7; Algorithm 1)
@@ -358,6 +359,133 @@ specsteer_status specsteer_ctx_time_streaming(specsteer_ctx *ctx, void *ev_begin
  * special-function rate instead of an assumed one.  sink: DEVICE, n_ctas * 1024 floats, overwritten.
  * Total evaluations: n_ctas * 1024 * 8 * iters.  Errors: INVALID_ARG, CUDA. */
 specsteer_status specsteer_probe_ex2(int32_t n_ctas, int32_t iters, float *sink, void *cuda_stream);
+
+/* ---- The paged key/value cache in front of the round ---------------------------------------------------------------
+ * A round verifies a chunk of new tokens per request: the last emitted token and the K drafts behind it (Algorithm 1
+ * phase 2).  The forward passes that give its logits (or the hidden states of specsteer_lmhead_round) attend that chunk
+ * over a cache of keys and values, of which the round then keeps accept_len + 1 tokens.  Three operators keep such a
+ * cache on the device, so that one round can follow another without the host learning any length:
+ *   specsteer_cache_plan       lengths and the round's accepted lengths -> page moves, block tables, slot map
+ *   specsteer_cache_append     the chunk's keys and values -> their slots
+ *   specsteer_chunk_attention  the chunk's queries over the cache
+ * Layout: a pool of n_pages pages of page_size tokens; block_table[b][i] is the page of request b's tokens
+ * [i*page_size, (i+1)*page_size); a slot is page*page_size + offset.  All three work on the CURRENT CUDA device, need no
+ * context, keep nothing from call to call, allocate nothing, only enqueue work on the given stream (they can be captured
+ * into a graph) and never synchronise.  Calls on several streams or threads may overlap as long as their outputs and
+ * workspaces are different memory.  Lengths, tables and slots are device data: what is wrong in them sets bits in
+ * req_status and gives the result stated, never an access outside the tensors described. */
+
+/* further bits of req_status[b], beside SPECSTEER_REQ_* of the round */
+enum {
+  SPECSTEER_REQ_BAD_PAGE = 32,  /* a needed page id lies outside [0, n_pages) */
+  SPECSTEER_REQ_NO_ROOM = 64,   /* plan: the chunk does not fit max_tokens; the request gets no tokens this time */
+  SPECSTEER_REQ_NO_PAGES = 128, /* plan: the pool has too few free pages; no tokens this time, pages as they were */
+  SPECSTEER_REQ_BAD_POOL = 256, /* plan: ring_pos does not describe a ring of n_pages entries; nothing is moved */
+  SPECSTEER_REQ_TIMEOUT = 512   /* attention: a bounded device-side wait gave up; outputs of the call are undefined */
+};
+
+/* Block tables and slot maps from request lengths.  Per request b, in this order:
+ *   kept   = seq_len + advance            tokens that stay in the cache (advance: the round's n_out; may be negative)
+ *   asked  = new_len                      tokens of the next chunk; -1 ends the request: kept = asked = 0, its pages go back
+ *   target = ceil((kept + asked) / page_size)
+ *   entries [target, pages_held) of its table go back to the pool, or entries [pages_held, target) are taken from it.
+ * The pool's free pages are a ring: free_ring[i mod n_pages] for ring_pos[0] <= i < ring_pos[1].  Pages given back are
+ * appended in request order (then table order) and can be taken in the same call; pages are taken from the front in
+ * request order.  A request is refused, and says so in req_status, when
+ *   BAD_LEN   new_len < -1, kept < 0, kept + asked > table_width*page_size or pages_held outside [0, table_width]: it
+ *             stays as it is (seq_len and pages_held are passed on, kv_len 0, no tokens);
+ *   NO_ROOM   asked > 0 and the sum of asked over the requests up to it (those not BAD_LEN) exceeds max_tokens: asked = 0;
+ *   NO_PAGES  the pages wanted by the requests up to it exceed those free: asked = 0, its pages stay as they were
+ *             (kept still advances);
+ *   BAD_POOL  every request, when ring_pos[1] - ring_pos[0] is outside [0, n_pages] or ring_pos[0] < 0: as BAD_LEN.
+ * Outputs: seq_len_out = kept; pages_held_out; ring_pos_out; cu_new[B+1], the running sum of asked (the chunk's tokens
+ * of request b are rows [cu_new[b], cu_new[b+1]) of the packed batch); kv_len = kept + asked; and for every row i
+ * below max_tokens slot_map[i], positions[i] (its position in the request) and token_req[i] (its request), -1 behind the
+ * last token.  A token whose page id is outside the pool gets slot -1 and BAD_PAGE.  seq_len_out, pages_held_out and
+ * ring_pos_out may be the inputs themselves (in place) or other arrays (then the call can be repeated); no other output
+ * may overlap an input.  Table entries from pages_held_out on are left as they are and read by nobody.
+ * B <= SPECSTEER_PLAN_MAX_B.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+#define SPECSTEER_PLAN_MAX_B 8192
+typedef struct {
+  int32_t B, page_size, n_pages, table_width, max_tokens;
+  int64_t ld_table;            /* elements between rows of block_table, >= table_width */
+  const int32_t *seq_len;      /* [B] */
+  const int32_t *advance;      /* [B] or NULL (0) */
+  const int32_t *new_len;      /* [B] */
+  const int32_t *pages_held;   /* [B] */
+  const int64_t *ring_pos;     /* [2] front and end of the ring */
+  int32_t *block_table;        /* [B][ld_table], in place */
+  int32_t *free_ring;          /* [n_pages], in place */
+  int32_t *seq_len_out;        /* [B] */
+  int32_t *pages_held_out;     /* [B] */
+  int64_t *ring_pos_out;       /* [2] */
+  int32_t *cu_new;             /* [B+1] */
+  int32_t *kv_len;             /* [B] */
+  int64_t *slot_map;           /* [max_tokens] */
+  int32_t *positions;          /* [max_tokens] or NULL */
+  int32_t *token_req;          /* [max_tokens] or NULL */
+  int32_t *req_status;         /* [B], written */
+} specsteer_cache_plan_desc;
+specsteer_status specsteer_cache_plan(const specsteer_cache_plan_desc *desc, void *cuda_stream);
+
+/* k and v of T tokens into their slots: cache[slot / page_size][slot mod page_size][h][:] = k[t][h][:].  A slot outside
+ * [0, n_pages*page_size) (-1: a padded row) names no place and its token is dropped.  Two tokens of one call that name
+ * the same slot leave a mixture of the two there (a plan never makes such slots unless tables share a page).  Strides in
+ * elements, the innermost axis dense; any strides and alignment are taken, 16-byte multiples are faster.  dtype: F32,
+ * BF16 or F16, the same on both sides.  Errors: INVALID_ARG, CUDA. */
+typedef struct {
+  int32_t T, Hkv, D, page_size, n_pages, dtype;
+  int64_t k_tok, k_head, v_tok, v_head;           /* strides of k and v */
+  int64_t kc_page, kc_slot, kc_head;              /* strides of k_cache */
+  int64_t vc_page, vc_slot, vc_head;              /* strides of v_cache */
+  const void *k, *v;                              /* [T][Hkv][D] */
+  const int64_t *slot_map;                        /* [T] */
+  void *k_cache, *v_cache;                        /* [n_pages][page_size][Hkv][D] */
+} specsteer_cache_append_desc;
+specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc, void *cuda_stream);
+
+/* Attention of a chunk of new tokens over the paged cache (which holds the chunk's own keys and values already).
+ * Row i of request b's n = cu_new[b+1] - cu_new[b] rows stands at position p = kv_len[b] - n + i and sees the keys
+ * j <= p, and with window > 0 only j > p - window.  For every query head h, with kv head h / (Hq/Hkv):
+ *   out[row][h] = sum_j softmax_j(scale * q[row][h] . k[j]) v[j],   lse[row][h] = log sum_j exp(scale * q[row][h] . k[j])
+ * One token per request is plain decoding.  A row that sees no key (p < 0) gets 0 and -inf.  Keys that a row does not see
+ * do not reach it, whatever they hold (NaN included).  Products are formed in float32 from the inputs' type, sums and
+ * maxima are float32, the weights of a tile are rounded to the inputs' type for the product with v.
+ *   - Requests with cu_new outside [0, T] or decreasing, or kv_len outside [0, table_width*page_size]: BAD_LEN, nothing
+ *     written.  Rows of no request are left as they are.
+ *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.
+ *   - req_status may be NULL; bits are OR-ed into it (clear it first; specsteer_cache_plan writes it).
+ *   - scale >= 0 and finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
+ *     caches and out.  Strides in elements, innermost axis dense.
+ *   - The tensor-core kernel takes D <= 128 in multiples of 8, page_size a divisor or a multiple of 128 and a multiple of
+ *     8, up to 128 query heads per kv head, and 16-byte aligned pointers and strides of q and the caches; everything else
+ *     runs on a slower generic kernel.
+ *   - workspace: 16-byte aligned device memory of at least specsteer_chunk_attention_workspace(desc) bytes, whose content
+ *     before and after the call means nothing; calls that may overlap (two streams, two graphs) need one each.
+ * Same inputs give the same bits.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE (too small), CUDA. */
+#define SPECSTEER_ATTENTION_MAX_D 256
+typedef struct {
+  int32_t B, T;                                   /* requests; rows of q and out */
+  int32_t Hq, Hkv, D, page_size, n_pages, table_width;
+  int32_t dtype, window;
+  float scale;
+  uint32_t flags;                                 /* 0, or SPECSTEER_ATTENTION_GENERIC */
+  int64_t ld_table;
+  int64_t q_tok, q_head, o_tok, o_head;           /* strides of q and out */
+  int64_t kc_page, kc_slot, kc_head;              /* strides of k_cache */
+  int64_t vc_page, vc_slot, vc_head;              /* strides of v_cache */
+  const void *q, *k_cache, *v_cache;              /* [T][Hq][D], [n_pages][page_size][Hkv][D] twice */
+  const int32_t *block_table, *cu_new, *kv_len;   /* [B][ld_table], [B+1], [B] */
+  void *out;                                      /* [T][Hq][D] */
+  float *lse;                                     /* [T][Hq] dense, or NULL */
+  int32_t *req_status;                            /* [B] or NULL */
+  void *workspace;
+  int64_t workspace_bytes;
+} specsteer_attention_desc;
+enum { SPECSTEER_ATTENTION_GENERIC = 1u };        /* run the generic kernel whatever the shape (comparison, tests) */
+specsteer_status specsteer_chunk_attention(const specsteer_attention_desc *desc, void *cuda_stream);
+/* Bytes of workspace the call needs (0 for a descriptor that specsteer_chunk_attention refuses). */
+size_t specsteer_chunk_attention_workspace(const specsteer_attention_desc *desc);
 
 /* Bytes of device workspace owned by the context. */
 size_t specsteer_ctx_workspace_bytes(const specsteer_ctx *ctx);

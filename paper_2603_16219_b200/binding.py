@@ -7,6 +7,7 @@ fallback: if the library has not been built, or no CUDA device is present, calls
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Dict, Optional
 
@@ -16,7 +17,7 @@ from . import build as _build
 
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_ORDER, ERR_TIMEOUT, ERR_STATIC_LIMIT = 1, 2, 3, 4, 5, 6, 7
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 ACCEPT_RATIO, ACCEPT_EXACT_Z = 0, 1
 RECOVER_STEER, RECOVER_RESIDUAL, RECOVER_ARGMAX = 0, 1, 2
 FLAG_BONUS = 1
@@ -24,6 +25,9 @@ FLAG_TWO_PHASE = 2
 FLAG_SEPARATE_LAUNCHES = 4
 FLAG_ONE_LAUNCH = 8
 REQ_BAD_TOKEN, REQ_BAD_LEN, REQ_NONFINITE, REQ_RESIDUAL_EMPTY, REQ_BAD_PARAM = 1, 2, 4, 8, 16
+REQ_BAD_PAGE, REQ_NO_ROOM, REQ_NO_PAGES, REQ_BAD_POOL, REQ_TIMEOUT = 32, 64, 128, 256, 512
+ATTENTION_GENERIC = 1
+PLAN_MAX_B, ATTENTION_MAX_D = 8192, 256
 
 EXPORTS = (
     "specsteer_ctx_create", "specsteer_ctx_destroy", "specsteer_verify_round", "specsteer_recover_sample",
@@ -36,6 +40,7 @@ EXPORTS = (
     "specsteer_lmhead_shard_local", "specsteer_lmhead_shard_combine", "specsteer_lmhead_shard_recover",
     "specsteer_shard_greedy_local", "specsteer_lmhead_shard_greedy_local", "specsteer_shard_greedy_finish",
     "specsteer_probe_ex2", "specsteer_ctx_set_wait_limit",
+    "specsteer_cache_plan", "specsteer_cache_append", "specsteer_chunk_attention", "specsteer_chunk_attention_workspace",
 )
 SHARD_PARTIAL_BYTES = 64
 MAX_SHARDS = 32
@@ -68,6 +73,46 @@ class LmheadDesc(C.Structure):
         ("x_slm_plus", C.c_void_p), ("w_slm_plus", C.c_void_p),
         ("x_slm_minus", C.c_void_p), ("w_slm_minus", C.c_void_p),
         ("d_llm", C.c_int32), ("d_slm", C.c_int32),
+    ]
+
+
+class CachePlanDesc(C.Structure):
+    """Mirror of ``specsteer_cache_plan_desc``."""
+    _fields_ = [
+        ("B", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("table_width", C.c_int32), ("max_tokens", C.c_int32),
+        ("ld_table", C.c_int64),
+        ("seq_len", C.c_void_p), ("advance", C.c_void_p), ("new_len", C.c_void_p), ("pages_held", C.c_void_p),
+        ("ring_pos", C.c_void_p), ("block_table", C.c_void_p), ("free_ring", C.c_void_p),
+        ("seq_len_out", C.c_void_p), ("pages_held_out", C.c_void_p), ("ring_pos_out", C.c_void_p),
+        ("cu_new", C.c_void_p), ("kv_len", C.c_void_p), ("slot_map", C.c_void_p), ("positions", C.c_void_p),
+        ("token_req", C.c_void_p), ("req_status", C.c_void_p),
+    ]
+
+
+class CacheAppendDesc(C.Structure):
+    """Mirror of ``specsteer_cache_append_desc``."""
+    _fields_ = [
+        ("T", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("dtype", C.c_int32),
+        ("k_tok", C.c_int64), ("k_head", C.c_int64), ("v_tok", C.c_int64), ("v_head", C.c_int64),
+        ("kc_page", C.c_int64), ("kc_slot", C.c_int64), ("kc_head", C.c_int64),
+        ("vc_page", C.c_int64), ("vc_slot", C.c_int64), ("vc_head", C.c_int64),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("slot_map", C.c_void_p), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
+    ]
+
+
+class AttentionDesc(C.Structure):
+    """Mirror of ``specsteer_attention_desc``."""
+    _fields_ = [
+        ("B", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32),
+        ("n_pages", C.c_int32), ("table_width", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32),
+        ("scale", C.c_float), ("flags", C.c_uint32), ("ld_table", C.c_int64),
+        ("q_tok", C.c_int64), ("q_head", C.c_int64), ("o_tok", C.c_int64), ("o_head", C.c_int64),
+        ("kc_page", C.c_int64), ("kc_slot", C.c_int64), ("kc_head", C.c_int64),
+        ("vc_page", C.c_int64), ("vc_slot", C.c_int64), ("vc_head", C.c_int64),
+        ("q", C.c_void_p), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
+        ("block_table", C.c_void_p), ("cu_new", C.c_void_p), ("kv_len", C.c_void_p),
+        ("out", C.c_void_p), ("lse", C.c_void_p), ("req_status", C.c_void_p),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
     ]
 
 
@@ -130,6 +175,13 @@ def load_library(path: Optional[str] = None):
     lib.specsteer_ctx_time_streaming.restype = C.c_int
     lib.specsteer_ctx_launch_count.argtypes = [C.c_void_p]
     lib.specsteer_ctx_launch_count.restype = C.c_uint64
+    for name, desc in (("specsteer_cache_plan", CachePlanDesc), ("specsteer_cache_append", CacheAppendDesc),
+                       ("specsteer_chunk_attention", AttentionDesc)):
+        fn = getattr(lib, name)
+        fn.argtypes = [C.POINTER(desc), C.c_void_p]
+        fn.restype = C.c_int
+    lib.specsteer_chunk_attention_workspace.argtypes = [C.POINTER(AttentionDesc)]
+    lib.specsteer_chunk_attention_workspace.restype = C.c_size_t
     lib.specsteer_status_string.argtypes = [C.c_int]
     lib.specsteer_status_string.restype = C.c_char_p
     lib.specsteer_version.restype = C.c_uint32
@@ -440,3 +492,153 @@ def verify_recover_round(ctx: Context, inputs, *, accept_mode=ACCEPT_RATIO, reco
     ctx.verify_round(desc, stream)
     ctx.recover_sample(desc, stream)
     return outputs
+
+
+# ---- the paged key/value cache in front of the round -----------------------------------------------------------------
+_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _launch(fn, name: str, desc, device):
+    """Call an entry point that works on the current device, on the tensors' device and its current stream."""
+    if device.type != "cuda":
+        raise RuntimeError("specsteer needs tensors on a CUDA device; there is no CPU fallback")
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        code = fn(desc, stream)
+    else:
+        with torch.cuda.device(device):
+            code = fn(desc, stream)
+    if code != OK:
+        raise SpecSteerError(code, name)
+
+
+def _flat(t: torch.Tensor, name: str, dtype, n: int, device) -> int:
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on %s" % (name, dtype, n, device))
+    return t.data_ptr()
+
+
+def _table(block_table: torch.Tensor, device):
+    if block_table.dim() != 2 or block_table.dtype != torch.int32 or block_table.device != device or block_table.shape[1] < 1 or \
+            (block_table.stride(1) != 1 and block_table.shape[1] > 1 and block_table.shape[0] > 0):
+        raise ValueError("block_table must be an int32 tensor [B, width] with dense rows on %s" % device)
+    B, width = block_table.shape
+    return block_table.data_ptr(), B, width, (block_table.stride(0) if B > 1 else width)
+
+
+def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor):
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.device != v_cache.device:
+        raise ValueError("k_cache and v_cache must share shape [n_pages, page_size, Hkv, D], dtype and device")
+    if k_cache.dtype not in _CACHE_DTYPES:
+        raise ValueError("the caches must be float32, bfloat16 or float16")
+    if k_cache.shape[3] > 1 and (k_cache.stride(3) != 1 or v_cache.stride(3) != 1):
+        raise ValueError("the caches need a contiguous last axis")
+
+
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
+    if t.dim() != 3 or t.dtype != like.dtype or t.device != like.device or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("%s must be a [tokens, heads, D] %s tensor with a contiguous last axis on %s" % (name, like.dtype, like.device))
+
+
+_PLAN_OUT = (("seq_len", torch.int32), ("pages_held", torch.int32), ("ring_pos", torch.int64), ("cu_new", torch.int32), ("kv_len", torch.int32),
+             ("slot_map", torch.int64), ("positions", torch.int32), ("token_req", torch.int32), ("status", torch.int32))
+
+
+def cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, pages_held: torch.Tensor, block_table: torch.Tensor, free_ring: torch.Tensor,
+               ring_pos: torch.Tensor, *, page_size: int, max_tokens: int, advance: Optional[torch.Tensor] = None,
+               out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Advance a paged cache on the device: keep ``seq_len + advance`` tokens of every request (``advance``: the round's
+    ``n_out``), make room for ``new_len`` more (-1 ends a request), move pages between the tables and the free ring.
+
+    seq_len, new_len, pages_held, advance [B] int32; block_table [B, width] and free_ring [n_pages] int32, updated in place;
+    ring_pos [2] int64.  Returns a dict with seq_len, pages_held, ring_pos (the next call's inputs), cu_new [B+1], kv_len [B],
+    slot_map / positions / token_req [max_tokens] and status [B].  ``out``: tensors to write those into; its seq_len,
+    pages_held and ring_pos may be the inputs themselves.  Formulas and refusals: specsteer_cache_plan."""
+    if stream is not None:   # what is allocated on the way belongs to that stream too
+        with torch.cuda.stream(stream):
+            return cache_plan(seq_len, new_len, pages_held, block_table, free_ring, ring_pos, page_size=page_size, max_tokens=max_tokens, advance=advance, out=out)
+    dev = block_table.device
+    table, B, width, ld = _table(block_table, dev)
+    max_tokens, n_pages = int(max_tokens), free_ring.numel()
+    sizes = (B, B, 2, B + 1, B, max_tokens, max_tokens, max_tokens, B)
+    if out is None:
+        out = {name: torch.empty(n, dtype=dt, device=dev) for (name, dt), n in zip(_PLAN_OUT, sizes)}
+    outs = [_flat(out[name], name, dt, n, dev) for (name, dt), n in zip(_PLAN_OUT, sizes)]
+    i32 = torch.int32
+    d = CachePlanDesc(B, int(page_size), n_pages, width, max_tokens, ld,
+                      _flat(seq_len, "seq_len", i32, B, dev), None if advance is None else _flat(advance, "advance", i32, B, dev),
+                      _flat(new_len, "new_len", i32, B, dev), _flat(pages_held, "pages_held", i32, B, dev),
+                      _flat(ring_pos, "ring_pos", torch.int64, 2, dev), table, _flat(free_ring, "free_ring", i32, n_pages, dev), *outs)
+    _launch(load_library().specsteer_cache_plan, "specsteer_cache_plan", d, dev)
+    return out
+
+
+def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slot_map: torch.Tensor, *, stream=None) -> None:
+    """Store the keys and values of T tokens, [T, Hkv, D], in their slots of the caches, [n_pages, page_size, Hkv, D] (any
+    strides with a contiguous last axis; a cache laid out by heads is passed as a transposed view).  slot_map [T] int64:
+    page * page_size + offset; a slot outside the cache (-1) drops its token."""
+    if stream is not None:   # what is allocated on the way belongs to that stream too
+        with torch.cuda.stream(stream):
+            return cache_append(k, v, k_cache, v_cache, slot_map)
+    _caches(k_cache, v_cache)
+    _heads(k, "k", k_cache)
+    _heads(v, "v", k_cache)
+    n_pages, page_size, H, D = k_cache.shape
+    if k.shape != v.shape or k.shape[1] != H or k.shape[2] != D:
+        raise ValueError("k and v must be [T, %d, %d]" % (H, D))
+    T, dev = k.shape[0], k_cache.device
+    a, b, e, f = k.stride(), v.stride(), k_cache.stride(), v_cache.stride()
+    d = CacheAppendDesc(T, H, D, page_size, n_pages, _CACHE_DTYPES[k_cache.dtype], a[0], a[1], b[0], b[1], e[0], e[1], e[2], f[0], f[1], f[2],
+                        k.data_ptr(), v.data_ptr(), _flat(slot_map, "slot_map", torch.int64, T, dev), k_cache.data_ptr(), v_cache.data_ptr())
+    _launch(load_library().specsteer_cache_append, "specsteer_cache_append", d, dev)
+
+
+def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
+                    kv_len: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    generic: bool = False, stream=None):
+    """Causal attention of a packed chunk of new tokens, q [T, Hq, D], over the paged caches [n_pages, page_size, Hkv, D]
+    that hold the chunk's own keys and values already.  Rows [cu_new[b], cu_new[b+1]) belong to request b, whose last row
+    stands at position kv_len[b] - 1.  One token per request is plain decoding.
+
+    scale: default 1/sqrt(D); window: 0, or the number of last keys a row sees; status [B] int32: bits are OR-ed into it.
+    Returns (out [T, Hq, D], lse [T, Hq] float32); rows of no request are left as they are in out and lse.  A workspace (uint8)
+    is allocated from torch's pool when none is given; a call captured into a graph, or overlapping others, keeps its
+    own.  Formulas, limits and refusals: specsteer_chunk_attention."""
+    if stream is not None:   # what is allocated on the way belongs to that stream too
+        with torch.cuda.stream(stream):
+            return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
+                                   workspace=workspace, generic=generic)
+    _caches(k_cache, v_cache)
+    _heads(q, "q", k_cache)
+    dev = q.device
+    n_pages, page_size, Hkv, D = k_cache.shape
+    T, Hq, Dq = q.shape
+    if Dq != D or k_cache.dtype == torch.float32:
+        raise ValueError("q and the caches must share D and be bfloat16 or float16")
+    table, B, width, ld = _table(block_table, dev)
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
+    else:
+        _heads(out, "out", k_cache)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    if lse is None:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+    a, o, e, f = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
+    d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, _CACHE_DTYPES[q.dtype], int(window),
+                      1.0 / math.sqrt(D) if scale is None else float(scale), ATTENTION_GENERIC if generic else 0, ld,
+                      a[0], a[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
+                      q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, "cu_new", torch.int32, B + 1, dev),
+                      _flat(kv_len, "kv_len", torch.int32, B, dev), out.data_ptr(), _flat(lse, "lse", torch.float32, T * Hq, dev),
+                      None if status is None else _flat(status, "status", torch.int32, B, dev), None, 0)
+    lib = load_library()
+    need = lib.specsteer_chunk_attention_workspace(d)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise ValueError("workspace must be a contiguous uint8 tensor on %s" % dev)
+        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _launch(lib.specsteer_chunk_attention, "specsteer_chunk_attention", d, dev)
+    return out, lse

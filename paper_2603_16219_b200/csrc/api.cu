@@ -976,8 +976,8 @@ const char* specsteer_status_string(specsteer_status s) {
   switch (s) {
     case SPECSTEER_OK: return "ok";
     case SPECSTEER_ERR_INVALID_ARG: return "invalid argument";
-    case SPECSTEER_ERR_UNSUPPORTED: return "shape exceeds the context's maxima";
-    case SPECSTEER_ERR_WORKSPACE: return "device allocation failed";
+    case SPECSTEER_ERR_UNSUPPORTED: return "shape exceeds the context's maxima or the operator's limits";
+    case SPECSTEER_ERR_WORKSPACE: return "device allocation failed or workspace too small";
     case SPECSTEER_ERR_CUDA: return "CUDA runtime error";
     case SPECSTEER_ERR_ORDER: return "recover_sample without a matching verify_round";
     case SPECSTEER_ERR_TIMEOUT: return "a bounded device-side wait gave up";

@@ -1,0 +1,130 @@
+"""Descriptors and host-side refusals of the paged cache's operators: nothing here needs a GPU."""
+import ctypes as C
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2603_16219_b200 import binding, build
+    build.build()
+    return binding
+
+
+@pytest.mark.parametrize("name,mirror,size", [("cache_plan", "CachePlanDesc", 6 * 4 + 8 + 16 * 8), ("cache_append", "CacheAppendDesc", 6 * 4 + 15 * 8),
+                                              ("attention", "AttentionDesc", 12 * 4 + 11 * 8 + 11 * 8)])
+def test_descriptor_layout_matches_header(binding, name, mirror, size):
+    hdr = open(os.path.join(ROOT, "include", "specsteer.h")).read()
+    end = hdr.index("} specsteer_%s_desc;" % name)
+    body = re.sub(r"/\*.*?\*/", "", hdr[hdr.rindex("typedef struct {", 0, end) + len("typedef struct {"):end], flags=re.S)
+    fields = []
+    for decl in body.split(";"):
+        for part in decl.strip().split(","):
+            if part.strip():
+                fields.append(re.findall(r"([A-Za-z_0-9]+)\s*$", part.strip())[0])
+    cls = getattr(binding, mirror)
+    assert fields == [n for n, _ in cls._fields_]
+    assert C.sizeof(cls) == size
+
+
+PTR = 4096   # a pointer that is not NULL; every call below is refused before anything is launched
+
+
+def _plan(binding, **k):
+    d = binding.CachePlanDesc(B=2, page_size=16, n_pages=8, table_width=4, max_tokens=10, ld_table=4)
+    for name, typ in d._fields_:
+        if typ is C.c_void_p:
+            setattr(d, name, PTR)
+    for name, v in k.items():
+        setattr(d, name, v)
+    return d
+
+
+def _append(binding, **k):
+    d = binding.CacheAppendDesc(T=2, Hkv=2, D=64, page_size=16, n_pages=8, dtype=binding.BF16, k_tok=128, k_head=64, v_tok=128, v_head=64, kc_page=2048, kc_slot=128,
+                                kc_head=64, vc_page=2048, vc_slot=128, vc_head=64, k=PTR, v=PTR, slot_map=PTR, k_cache=PTR, v_cache=PTR)
+    for name, v in k.items():
+        setattr(d, name, v)
+    return d
+
+
+def _attention(binding, **k):
+    d = binding.AttentionDesc(B=2, T=4, Hq=4, Hkv=2, D=64, page_size=16, n_pages=8, table_width=4, dtype=binding.BF16, window=0, scale=0.125, ld_table=4,
+                              q_tok=256, q_head=64, o_tok=256, o_head=64, kc_page=2048, kc_slot=128, kc_head=64, vc_page=2048, vc_slot=128, vc_head=64,
+                              q=PTR, k_cache=PTR, v_cache=PTR, block_table=PTR, cu_new=PTR, kv_len=PTR, out=PTR)
+    for name, v in k.items():
+        setattr(d, name, v)
+    return d
+
+
+@pytest.mark.parametrize("bad", [dict(B=-1), dict(page_size=0), dict(n_pages=0), dict(table_width=0), dict(max_tokens=-1), dict(ld_table=3), dict(seq_len=None),
+                                 dict(new_len=None), dict(pages_held=None), dict(ring_pos=None), dict(block_table=None), dict(free_ring=None), dict(seq_len_out=None),
+                                 dict(pages_held_out=None), dict(ring_pos_out=None), dict(cu_new=None), dict(kv_len=None), dict(slot_map=None), dict(req_status=None)])
+def test_plan_refuses(binding, bad):
+    assert binding.load_library().specsteer_cache_plan(_plan(binding, **bad), None) == binding.ERR_INVALID_ARG
+
+
+def test_plan_refuses_too_many_requests(binding):
+    assert binding.load_library().specsteer_cache_plan(_plan(binding, B=binding.PLAN_MAX_B + 1), None) == binding.ERR_UNSUPPORTED
+    assert binding.load_library().specsteer_cache_plan(None, None) == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bad", [dict(T=-1), dict(Hkv=0), dict(D=0), dict(page_size=0), dict(n_pages=0), dict(dtype=3), dict(dtype=-1), dict(k=None), dict(v=None),
+                                 dict(slot_map=None), dict(k_cache=None), dict(v_cache=None), dict(k_tok=-1), dict(vc_head=-8), dict(Hkv=1 << 16, D=1 << 16)])
+def test_append_refuses(binding, bad):
+    assert binding.load_library().specsteer_cache_append(_append(binding, **bad), None) == binding.ERR_INVALID_ARG
+    assert binding.load_library().specsteer_cache_append(None, None) == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bad", [dict(B=-1), dict(T=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=5), dict(D=0), dict(page_size=0), dict(n_pages=0), dict(table_width=0),
+                                 dict(ld_table=3), dict(dtype=0), dict(dtype=7), dict(window=-1), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+                                 dict(flags=2), dict(q_tok=-1), dict(o_head=-1), dict(kc_page=-1), dict(q=None), dict(k_cache=None), dict(v_cache=None),
+                                 dict(block_table=None), dict(cu_new=None), dict(kv_len=None), dict(out=None)])
+def test_attention_refuses(binding, bad):
+    lib = binding.load_library()
+    assert lib.specsteer_chunk_attention(_attention(binding, **bad), None) == binding.ERR_INVALID_ARG
+    assert lib.specsteer_chunk_attention_workspace(_attention(binding, **bad)) == 0
+
+
+def test_attention_refuses_wide_heads_and_takes_nothing(binding):
+    lib = binding.load_library()
+    assert lib.specsteer_chunk_attention(_attention(binding, D=binding.ATTENTION_MAX_D + 1), None) == binding.ERR_UNSUPPORTED
+    assert lib.specsteer_chunk_attention(None, None) == binding.ERR_INVALID_ARG
+    for d in (_attention(binding, T=0, q=None, out=None), _attention(binding, B=0, cu_new=None)):
+        assert lib.specsteer_chunk_attention(d, None) == binding.OK
+    assert lib.specsteer_cache_append(_append(binding, T=0, k=None), None) == binding.OK
+
+
+def test_binding_checks_tensors(binding):
+    import torch
+    i32 = torch.int32
+    seq, ring, pos = torch.zeros(2, dtype=i32), torch.zeros(8, dtype=i32), torch.zeros(2, dtype=torch.int64)
+    table = torch.zeros(2, 4, dtype=i32)
+    args = [seq, seq.clone(), seq.clone(), table, ring, pos]
+    for i, bad in ((0, torch.zeros(3, dtype=i32)), (1, torch.zeros(2)), (2, torch.zeros(4, dtype=i32)[::2]), (3, torch.zeros(2, 4)), (4, ring.long()), (5, torch.zeros(2, dtype=i32))):
+        broken = list(args)
+        broken[i] = bad
+        with pytest.raises(ValueError):
+            binding.cache_plan(*broken, page_size=16, max_tokens=4)
+    with pytest.raises(RuntimeError):                      # no CPU fallback
+        binding.cache_plan(*args, page_size=16, max_tokens=4)
+    bf = torch.bfloat16
+    kc, k = torch.zeros(8, 16, 2, 64, dtype=bf), torch.zeros(3, 2, 64, dtype=bf)
+    slot = torch.zeros(3, dtype=torch.int64)
+    for bad in ((k.half(), k, kc, kc, slot), (k, k[:2], kc, kc, slot), (k, k, kc, kc[:, :8], slot), (k, k, kc, kc, slot[:2]), (k, k, kc, kc, slot.int()),
+                (k[..., ::2], k[..., ::2], kc[..., ::2], kc[..., ::2], slot), (k.double(), k.double(), kc.double(), kc.double(), slot)):
+        with pytest.raises(ValueError):
+            binding.cache_append(*bad)
+    with pytest.raises(RuntimeError):
+        binding.cache_append(k, k, kc, kc, slot)
+    q, cu, kv = torch.zeros(3, 4, 64, dtype=bf), torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32)
+    for bad in ((q.half(), kc, kc, table, cu, kv), (q[..., :32], kc, kc, table, cu, kv), (q, kc, kc, table, cu[:2], kv), (q, kc, kc, table, cu, cu),
+                (q, kc, kc, table[0], cu, kv), (q.float(), kc.float(), kc.float(), table, cu, kv)):
+        with pytest.raises(ValueError):
+            binding.chunk_attention(*bad)
+    with pytest.raises(RuntimeError):
+        binding.chunk_attention(q, kc, kc, table, cu, kv)
