@@ -218,7 +218,7 @@ using namespace specsteer;
 
 extern "C" size_t specsteer_chunk_attention_workspace(const specsteer_attention_desc* d) {
   if (check_attention(d) != SPECSTEER_OK || d->B == 0 || d->T == 0) return 0;
-  return 0;
+  return attention_tc_takes(d) ? attention_tc_workspace(d) : 0;
 }
 
 extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_desc* d, void* cuda_stream) {
@@ -228,6 +228,13 @@ extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_
   const size_t need = specsteer_chunk_attention_workspace(d);
   if (need > 0 && (!d->workspace || d->workspace_bytes < (long long)need || ((uintptr_t)d->workspace & 15u))) return SPECSTEER_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)cuda_stream;
+  if (attention_tc_takes(d)) {
+    if (launch_attention_tc(d, s) != cudaSuccess) {
+      cudaGetLastError();
+      return SPECSTEER_ERR_CUDA;
+    }
+    return SPECSTEER_OK;
+  }
   const long long blocks = ((long long)d->T * (d->Hq / d->Hkv) + kGenRows - 1) / kGenRows + d->B;
   const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), d->Hkv);
   if (d->dtype == SPECSTEER_BF16) attention_generic_kernel<__nv_bfloat16><<<grid, kGenThreads, 0, s>>>(*d);

@@ -30,4 +30,9 @@ __device__ __forceinline__ void attn_span(const specsteer_attention_desc& p, con
   lo = p.window > 0 && hi > p.window ? hi - p.window : 0;
 }
 
+// The tensor-core kernel: whether it takes a (checked) descriptor, the workspace it needs, the launch.
+bool attention_tc_takes(const specsteer_attention_desc* d);
+size_t attention_tc_workspace(const specsteer_attention_desc* d);
+cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t s);
+
 }  // namespace specsteer

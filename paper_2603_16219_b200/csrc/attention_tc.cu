@@ -1,0 +1,946 @@
+// Attention of a chunk of new tokens over the paged cache on the tensor cores (tcgen05, TMA).
+//
+// Rows.  For one kv head a query tile is up to 128 rows, row r = token * G + head within the group (G = Hq/Hkv), so that
+// all query heads of a kv head share every key that is loaded.  A unit of work is one or two query tiles (two when the
+// request has more tokens than one tile holds) against all tiles of 128 keys that its rows see.
+//
+// Split.  The key tiles of all units, in order (request, kv head, unit), form one list, which is cut into equal ranges,
+// one per CTA (one CTA per SM).  Ragged lengths, one long request and a large batch then load the SMs alike, and the
+// cut needs nothing from the host: every CTA sums the lengths itself.  A unit that a cut goes through leaves partial
+// results (unnormalised sums, maximum and sum of weights per row) that attention_join_kernel puts together.
+//
+// Inside a CTA: warp 8 issues the TMA loads (a ring of stages of one 128-key tile of K or V; a page or its part of 128
+// keys is a box), warp 9 issues tcgen05.mma, warps 0..3 and 4..7 are two softmax groups (streams), one row a thread.
+// Stream s has scores S_s (128 columns of tensor memory, overwritten by the 16-bit weights P_s, which the second product
+// reads from tensor memory) and sums O_s (128 columns).  With two query tiles each stream owns one and both use every
+// key tile; with one query tile the streams take the key tiles in turn and are put together at the end.  Either way one
+// stream's exponentials run under the other stream's products.
+//
+// Maximum.  Weights are 2^(c s - c m) with a reference m per row that follows the running maximum only when that has
+// grown by more than 8 (in powers of two): O_s is then rescaled in tensor memory, which after the first tiles hardly
+// ever happens.  Weights stay below 2^8, sums are float32.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <atomic>
+
+#include "attention.cuh"
+
+namespace specsteer {
+namespace {
+
+constexpr int kKeys = 128;          // keys per tile
+constexpr int kTcThreads = 320;
+constexpr int kProducerWarp = 8, kMmaWarp = 9;
+constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
+constexpr float kGrow = 8.f;        // powers of two the maximum may exceed the reference by
+
+template <int DP> struct TcLayout {
+  static constexpr int kStageBytes = kKeys * DP * 2;
+  static constexpr int kStages = DP == 128 ? 5 : 12;
+  static constexpr int kQBytes = 128 * DP * 2;
+  static constexpr int kRing = 2 * kQBytes;                       // offset of the ring behind the two query tiles
+  static constexpr int kControl = kRing + kStages * kStageBytes;  // offset of TcShared
+};
+
+struct TcShared {
+  uint64_t full[12], empty[12];
+  uint64_t q_full[2], q_empty[2];
+  uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t both, group[2], drain;
+  uint32_t tmem_slot;
+  int abort_flag;
+  int nonfinite;           // an infinity or NaN was taken out of a tile of values: bit 0, and bit 1 in a tile with a bad page
+  int start_b, start_hk, start_u, start_off;
+  long long n_tiles;       // tiles of this CTA's range
+  long long scan[10];
+  uint32_t bad[16];        // per key tile (counted modulo 16): the boxes of it that lie outside the pool
+  float2 exch[2][128];     // reference and sum of each stream's rows
+};
+template <int DP> constexpr int tc_smem_bytes() { return TcLayout<DP>::kControl + (int)sizeof(TcShared); }
+static_assert(tc_smem_bytes<128>() <= 232448 && tc_smem_bytes<64>() <= 232448, "shared memory of one CTA");
+
+struct TcParams {
+  specsteer_attention_desc d;
+  int G, box_tok, box_rows, tile_tok;  // query box: tokens and rows; tokens of a query tile
+  int page_rows, boxes, page_shift;    // key box: keys, boxes per key tile, log2 of its keys
+  float c;                             // scale * log2(e)
+  int out_vec;                         // out rows are 16-byte aligned
+  float* part;                         // [2*gridDim][256][DP] unnormalised sums
+  float2* part_ml;                     // [2*gridDim][256] reference (powers of two) and sum
+  int* head;                           // [gridDim][8] see write_head
+};
+
+// ---- PTX wrappers -------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, int w, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+      "l"(tm), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(tm), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+__device__ __forceinline__ void tc_alloc(uint32_t* slot) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(kTcCols) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_dealloc(uint32_t addr) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(kTcCols) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// D (+)= A B^T with both operands in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// the same with A in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tm_ld32(uint32_t addr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
+        "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
+        "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(u[0]),
+      "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]),
+      "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]),
+      "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory descriptors of 128-byte swizzled operands, in units of 16 bytes.  K and Q (rows of 64 elements along the
+// summed axis): groups of 8 rows 1024 bytes apart.  V (the summed axis, keys, runs over the rows): 8-key groups 1024 bytes
+// apart, blocks of 64 columns one chunk of 128 rows apart.
+__device__ __forceinline__ uint64_t desc_rows(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ uint64_t desc_cols(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)((kKeys * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)2 << 61);
+}
+// Instruction descriptor: float32 accumulator, operands bf16 or f16, M = 128.
+__device__ __forceinline__ uint32_t instr_desc(bool bf16, int n, bool b_by_columns) {
+  const uint32_t f = bf16 ? 1u : 0u;
+  return (1u << 4) | (f << 7) | (f << 10) | ((b_by_columns ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+template <bool BF> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// the 16-bit halves of w that are infinite or NaN, as a mask of halves
+template <bool BF> __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t w) {
+  const uint32_t e = BF ? 0x7f80u : 0x7c00u;
+  return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
+}
+
+__device__ __forceinline__ bool aborted(const TcShared* sh) { return *reinterpret_cast<const volatile int*>(&sh->abort_flag) != 0; }
+__device__ __forceinline__ void give_up(TcShared* sh, const TcParams& p, int b) {
+  *reinterpret_cast<volatile int*>(&sh->abort_flag) = 1;
+  if (p.d.req_status && b < p.d.B) atomicOr(p.d.req_status + b, SPECSTEER_REQ_TIMEOUT);
+}
+
+// ---- units ----------------------------------------------------------------------------------------------------------
+struct Unit {
+  int tok0, tok1;          // tokens of the request
+  bool two;                // two query tiles
+  int hi_first, hi_last;   // keys the first / last row sees end here
+  int lo_first, lo_last;   // and begin here
+  int t0, nt;              // first key tile, key tiles (at least one, so that a unit that sees nothing is written too)
+};
+__device__ __forceinline__ Unit make_unit(const TcParams& p, const AttnRequest& rq, int u) {
+  Unit x;
+  x.tok0 = u * 2 * p.tile_tok;
+  x.tok1 = min(rq.n, x.tok0 + 2 * p.tile_tok);
+  x.two = x.tok1 - x.tok0 > p.tile_tok;
+  attn_span(p.d, rq, x.tok0, x.lo_first, x.hi_first);
+  attn_span(p.d, rq, x.tok1 - 1, x.lo_last, x.hi_last);
+  x.t0 = x.lo_first / kKeys;
+  x.nt = max(1, (max(x.hi_last, 0) + kKeys - 1) / kKeys - x.t0);
+  return x;
+}
+__device__ __forceinline__ int n_units(const TcParams& p, const AttnRequest& rq) { return (rq.n + 2 * p.tile_tok - 1) / (2 * p.tile_tok); }
+__device__ __forceinline__ long long head_tiles(const TcParams& p, const AttnRequest& rq) {
+  long long c = 0;
+  for (int u = 0, nu = n_units(p, rq); u < nu; ++u) c += make_unit(p, rq, u).nt;
+  return c;
+}
+
+// Walks this CTA's share: the pieces [off, off + take) of consecutive units.
+struct Walk {
+  int b, hk, u, off, take, index;
+  long long left;
+  AttnRequest rq;
+  Unit x;
+  __device__ __forceinline__ void begin(const TcParams& p, const TcShared* sh) {
+    b = sh->start_b; hk = sh->start_hk; u = sh->start_u; off = sh->start_off;
+    left = sh->n_tiles;
+    index = 0;
+    if (left > 0) load(p);
+  }
+  __device__ __forceinline__ void load(const TcParams& p) {
+    rq = attn_request(p.d, b);
+    x = make_unit(p, rq, u);
+    take = (int)min((long long)(x.nt - off), left);
+  }
+  __device__ __forceinline__ bool more() const { return left > 0; }
+  __device__ __forceinline__ bool starts() const { return off == 0; }
+  __device__ __forceinline__ bool ends() const { return off + take == x.nt; }
+  __device__ __forceinline__ void next(const TcParams& p) {
+    left -= take;
+    ++index;
+    if (left <= 0) return;
+    off = 0;
+    if (++u == n_units(p, rq)) {
+      u = 0;
+      if (++hk == p.d.Hkv) {
+        hk = 0;
+        do { ++b; rq = attn_request(p.d, b); } while (rq.n == 0 && b + 1 < p.d.B);   // left > 0: a request with rows follows
+      }
+    }
+    load(p);
+  }
+  // Ring items of a piece: the keys of the first `ahead` tiles, then per tile its values and the keys `ahead` tiles on.
+  __device__ __forceinline__ int ahead() const { return min(x.two ? 1 : 2, take); }
+  __device__ __forceinline__ int item_of_v(int t) const { return ahead() + min(t, take - ahead()) + t; }
+};
+
+// sums over the block of one value a thread; returns the exclusive sum, *total the sum
+__device__ __forceinline__ long long block_sum(long long v, TcShared* sh, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(kFullMask, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) sh->scan[warp] = x;
+  __syncthreads();
+  long long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kTcThreads / 32; ++w) {
+    if (w < warp) before += sh->scan[w];
+    all += sh->scan[w];
+  }
+  *total = all;
+  return before + x - v;
+}
+
+template <int DP, bool BF>
+__global__ void __launch_bounds__(kTcThreads, 1)
+attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                    const __grid_constant__ TcParams p) {
+  typedef TcLayout<DP> L;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  const uint32_t smem0 = smem_u32(smem_raw);
+  TcShared* sh = reinterpret_cast<TcShared*>(smem_raw + L::kControl);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  pdl_launch_dependents();   // attention_join_kernel may come up; it waits for the end of this kernel before it reads
+  if (tid == 0) {
+    for (int i = 0; i < L::kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 1);
+      mbar_init(&sh->s_full[i], 1); mbar_init(&sh->p_full[i], 4); mbar_init(&sh->pv_done[i], 1);
+      mbar_init(&sh->group[i], 4);
+    }
+    mbar_init(&sh->both, 8);
+    mbar_init(&sh->drain, 1);
+    sh->abort_flag = 0;
+    sh->nonfinite = 0;
+    sh->n_tiles = 0;
+    fence_barrier_init();
+  }
+  if (warp == kMmaWarp) tc_alloc(&sh->tmem_slot);
+
+  // ---- this CTA's range of the list of key tiles
+  {
+    const int per = (p.d.B + kTcThreads - 1) / kTcThreads, b_lo = min(p.d.B, tid * per), b_hi = min(p.d.B, b_lo + per);
+    long long mine = 0, total;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const AttnRequest rq = attn_request(p.d, b);
+      if (rq.bad && blockIdx.x == 0 && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_LEN);
+      if (rq.n > 0) mine += head_tiles(p, rq) * p.d.Hkv;
+    }
+    const long long before = block_sum(mine, sh, &total);   // (its barrier also publishes the set-up above)
+    const long long ctas = min(total, (long long)gridDim.x);   // every one of these has at least one tile
+    if (blockIdx.x < ctas) {
+      const long long s0 = total * blockIdx.x / ctas, s1 = total * (blockIdx.x + 1) / ctas;
+      if (s0 >= before && s0 < before + mine) {
+        long long rem = s0 - before;
+        for (int b = b_lo; b < b_hi; ++b) {
+          const AttnRequest rq = attn_request(p.d, b);
+          if (rq.n == 0) continue;
+          const long long per_head = head_tiles(p, rq);
+          if (rem >= per_head * p.d.Hkv) { rem -= per_head * p.d.Hkv; continue; }
+          const int hk = (int)(rem / per_head);
+          rem -= hk * per_head;
+          int u = 0;
+          for (;; ++u) {
+            const int nt = make_unit(p, rq, u).nt;
+            if (rem < nt) break;
+            rem -= nt;
+          }
+          sh->start_b = b; sh->start_hk = hk; sh->start_u = u; sh->start_off = (int)rem;
+          sh->n_tiles = s1 - s0;
+          break;
+        }
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sh->tmem_slot);
+
+  Walk w;
+  w.begin(p, sh);
+
+  if (warp == kProducerWarp) {
+    // ================= TMA =================
+    const int chunks = DP / 64;
+    const int box = lane / chunks, chunk = lane % chunks;
+    const bool loads = box < p.boxes;
+    const uint32_t lane_off = (uint32_t)chunk * (kKeys * 128) + (uint32_t)box * p.page_rows * 128;
+    int item = 0, qi = 0, tiles = 0;
+    bool ok = true;
+    // page of this lane's box of key tile t: the id, or n_pages (a coordinate outside, which reads zeros) for none
+    auto page_of = [&](int t) -> int {
+      const int key = t * kKeys + box * p.page_rows;
+      int page = p.d.n_pages;
+      if (loads && key < w.rq.kv) page = __ldg(p.d.block_table + (long long)w.b * p.d.ld_table + key / p.d.page_size);
+      return page;
+    };
+    auto stage_free = [&](int it) {
+      const bool got = !aborted(sh) && mbar_wait(&sh->empty[it % L::kStages], (uint32_t)((it / L::kStages) & 1) ^ 1u);
+      ok = __all_sync(kFullMask, got);
+    };
+    auto load_tile = [&](const CUtensorMap* tm, int t, int page) {
+      const int st = item % L::kStages;
+      stage_free(item);
+      if (!ok) return;
+      if (lane == 0) mbar_arrive_expect_tx(&sh->full[st], L::kStageBytes);
+      __syncwarp();
+      if (loads) {
+        const int pg = (page < 0 || page >= p.d.n_pages) ? p.d.n_pages : page;
+        tma_4d(smem0 + L::kRing + st * L::kStageBytes + lane_off, tm, chunk * 64, (t * kKeys) % p.d.page_size * (p.d.page_size >= kKeys), w.hk, pg, &sh->full[st]);
+      }
+      ++item;
+    };
+    auto load_k = [&](int t, int page) {
+      const bool outside = loads && t * kKeys + box * p.page_rows < w.rq.kv && (page < 0 || page >= p.d.n_pages);
+      const uint32_t votes = __ballot_sync(kFullMask, outside);
+      if (lane == 0) {
+        uint32_t bad = 0;
+        if (votes) {
+          for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (i * chunks)) & 1u) << i;
+          if (p.d.req_status) atomicOr(p.d.req_status + w.b, SPECSTEER_REQ_BAD_PAGE);
+        }
+        // the word is read by the softmax warps up to a ring's length of tiles later, well under 16
+        *reinterpret_cast<volatile uint32_t*>(&sh->bad[tiles & 15]) = bad;
+      }
+      ++tiles;
+      load_tile(&tm_k, t, page);
+    };
+    for (; w.more() && ok; w.next(p)) {
+      const int n_q = w.x.two ? 2 : 1;
+      for (int s = 0; s < n_q && ok; ++s, ++qi) {
+        const int slot = qi & 1;
+        const bool got = !aborted(sh) && mbar_wait(&sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
+        ok = __all_sync(kFullMask, got);
+        if (!ok) break;
+        const int tok = w.x.tok0 + s * p.tile_tok, cnt = min(p.tile_tok, w.x.tok1 - tok);
+        const int nb = (cnt + p.box_tok - 1) / p.box_tok;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
+          for (int i = 0; i < nb; ++i)
+            for (int ch = 0; ch < chunks; ++ch)
+              tma_3d(smem0 + slot * L::kQBytes + ch * (128 * 128) + i * p.box_rows * 128, &tm_q, ch * 64, w.hk * p.G, w.rq.row0 + tok + i * p.box_tok, &sh->q_full[slot]);
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      const int first = w.x.t0 + w.off, ahead = w.ahead();
+      int pg0 = page_of(first), pg1 = w.take > 1 ? page_of(first + 1) : 0, pg2 = w.take > 2 ? page_of(first + 2) : 0;
+      load_k(first, pg0);
+      if (ahead == 2 && ok) load_k(first + 1, pg1);
+      for (int t = 0; t < w.take && ok; ++t) {
+        const int pg3 = t + 3 < w.take ? page_of(first + t + 3) : 0;
+        load_tile(&tm_v, first + t, pg0);
+        if (t + ahead < w.take && ok) load_k(first + t + ahead, ahead == 2 ? pg2 : pg1);
+        pg0 = pg1; pg1 = pg2; pg2 = pg3;
+      }
+    }
+    if (!ok) {
+      if (lane == 0) {
+        give_up(sh, p, w.b);
+        // copies already issued may still be landing: wait for them (bounded) before the CTA exits
+        for (int i = item > L::kStages ? item - L::kStages : 0; i < item; ++i) mbar_wait(&sh->full[i % L::kStages], (uint32_t)((i / L::kStages) & 1));
+        for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) mbar_wait(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1));
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ================= tensor-core issuer =================
+    if (lane == 0) {
+      const uint32_t id_qk = instr_desc(BF, kKeys, false), id_pv = instr_desc(BF, DP, true);
+      int item = 0, qi = 0;
+      int n_p[2] = {0, 0};   // weights taken from each stream so far
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (!ok) return;
+        if (aborted(sh) || !mbar_wait(bar, parity)) { give_up(sh, p, w.b); ok = false; return; }
+        fence_after();
+      };
+      auto wait_item = [&](int it) { wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1)); };
+      auto stage_addr = [&](int it) { return smem0 + L::kRing + (it % L::kStages) * L::kStageBytes; };
+      auto scores = [&](int s, int slot, int it) {
+        const uint64_t a = desc_rows(smem0 + slot * L::kQBytes), b = desc_rows(stage_addr(it));
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+          const uint64_t step = (uint64_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2);
+          mma_ss(tmem + s * 128, a + step, b + step, id_qk, k != 0);
+        }
+        mma_commit(&sh->s_full[s]);
+      };
+      auto values = [&](int s, int it, bool accumulate) {
+        const uint64_t b = desc_cols(stage_addr(it));
+#pragma unroll
+        for (int k = 0; k < kKeys / 16; ++k)
+          mma_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, b + (uint64_t)(k * (2048 >> 4)), id_pv, accumulate || k != 0);
+        mma_commit(&sh->pv_done[s]);
+      };
+      for (; w.more() && ok; w.next(p)) {
+        const int take = w.take, ahead = w.ahead();
+        const int q0 = qi & 1, q1 = (qi + 1) & 1;
+        wait(&sh->q_full[q0], (uint32_t)((qi >> 1) & 1));
+        if (w.x.two) wait(&sh->q_full[q1], (uint32_t)(((qi + 1) >> 1) & 1));
+        // keys of the first tiles
+        wait_item(item);
+        if (!ok) break;
+        scores(0, q0, item);
+        if (w.x.two) scores(1, q1, item);
+        mma_commit(&sh->empty[item % L::kStages]);
+        ++item;
+        if (ahead == 2) {
+          wait_item(item);
+          if (!ok) break;
+          scores(1, q0, item);
+          mma_commit(&sh->empty[item % L::kStages]);
+          ++item;
+        }
+        for (int t = 0; t < take && ok; ++t) {
+          const int v = item++;
+          const bool next_k = t + ahead < take;
+          const int k = next_k ? item++ : 0;
+          if (w.x.two) {
+            wait(&sh->p_full[0], (uint32_t)(n_p[0]++ & 1));
+            wait_item(v);
+            if (!ok) break;
+            values(0, v, t > 0);
+            if (next_k) { wait_item(k); if (!ok) break; scores(0, q0, k); }
+            wait(&sh->p_full[1], (uint32_t)(n_p[1]++ & 1));
+            if (!ok) break;
+            values(1, v, t > 0);
+            mma_commit(&sh->empty[v % L::kStages]);
+            if (next_k) { scores(1, q1, k); mma_commit(&sh->empty[k % L::kStages]); }
+          } else {
+            const int s = t & 1;
+            wait(&sh->p_full[s], (uint32_t)(n_p[s]++ & 1));
+            wait_item(v);
+            if (!ok) break;
+            values(s, v, t > 1);
+            mma_commit(&sh->empty[v % L::kStages]);
+            if (next_k) {
+              wait_item(k);
+              if (!ok) break;
+              scores(s, q0, k);
+              mma_commit(&sh->empty[k % L::kStages]);
+            }
+          }
+        }
+        if (!ok) break;
+        mma_commit(&sh->q_empty[q0]);
+        if (w.x.two) mma_commit(&sh->q_empty[q1]);
+        qi += w.x.two ? 2 : 1;
+      }
+      if (!ok) {   // let everything issued finish before tensor memory is given back
+        mma_commit(&sh->drain);
+        mbar_wait(&sh->drain, 0);
+      }
+    }
+  } else {
+    // ================= softmax: one row a thread =================
+    const int s = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
+    const int r_tok = r / p.G, r_head = r - r_tok * p.G;
+    const float c = p.c;
+    int done[2] = {0, 0};        // tiles of each stream so far
+    int item0 = 0, tiles0 = 0, n_group = 0, n_both = 0;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (!ok) return;
+      const bool got = !aborted(sh) && mbar_wait(bar, parity);
+      ok = __all_sync(kFullMask, got);
+      if (!ok && lane == 0) give_up(sh, p, w.b);
+      fence_after();
+    };
+    // barriers among the softmax warps: of this group, of both groups (bounded like every wait)
+    auto meet = [&](bool all) {
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(all ? &sh->both : &sh->group[s]);
+      if (all) wait(&sh->both, (uint32_t)(n_both++ & 1));
+      else wait(&sh->group[s], (uint32_t)(n_group++ & 1));
+    };
+    if (tid == 0) {
+      int* h = p.head + blockIdx.x * 8;
+      h[0] = -1;   // slot of a unit that begins in this CTA and goes on in the next
+      h[1] = 0;    // 1: the unit that was going on ends in this CTA
+    }
+    for (; w.more() && ok; w.next(p)) {
+      const Unit& x = w.x;
+      const int tok = x.tok0 + (x.two ? s * p.tile_tok : 0) + r_tok;
+      const bool live = r_tok < p.tile_tok && tok < x.tok1;
+      const bool warp_live = __any_sync(kFullMask, live);
+      int lo = 0, hi = 0;
+      if (live) attn_span(p.d, w.rq, tok, lo, hi);
+      float m = kNegInf, l = 0.f;       // reference (raw score) and sum
+      int mine = 0;                     // tiles this stream has had in this piece
+      for (int t = x.two ? 0 : s; t < w.take && ok; t += x.two ? 1 : 2, ++mine) {
+        const int k0 = (x.t0 + w.off + t) * kKeys;
+        wait(&sh->s_full[s], (uint32_t)(done[s] + mine) & 1u);
+        if (!ok) break;
+        const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(tiles0 + t) & 15]);
+        const bool edge = k0 + kKeys > x.hi_first || k0 < x.lo_last || bad != 0;
+        if (warp_live) {
+          float v[128];
+          tm_ld32(t_s, v); tm_ld32(t_s + 32, v + 32); tm_ld32(t_s + 64, v + 64); tm_ld32(t_s + 96, v + 96);
+          tm_ld_wait();
+          if (edge) {
+            const int a = lo - k0, e = hi - k0;
+#pragma unroll
+            for (int j = 0; j < 128; ++j) v[j] = (j >= a && j < e) ? v[j] : kNegInf;
+            if (bad) {
+#pragma unroll
+              for (int j = 0; j < 128; ++j)
+                if ((bad >> (j >> p.page_shift)) & 1u) v[j] = kNegInf;
+            }
+          }
+          float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+#pragma unroll
+          for (int j = 0; j < 128; j += 8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          const bool raise = top > m && (m == kNegInf || (top - m) * c > kGrow);
+          if (__any_sync(kFullMask, raise)) {
+            const float alpha = !raise ? 1.f : m == kNegInf ? 0.f : ex2((m - top) * c);
+            if (mine > 0 && __any_sync(kFullMask, raise && m != kNegInf)) {
+              wait(&sh->pv_done[s], (uint32_t)(done[s] + mine - 1) & 1u);
+              if (!ok) break;
+#pragma unroll 1
+              for (int j0 = 0; j0 < DP; j0 += 32) {
+                float o[32];
+                tm_ld32(t_o + j0, o);
+                tm_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] *= alpha;
+                tm_st32(t_o + j0, reinterpret_cast<const uint32_t*>(o));
+              }
+            }
+            l *= alpha;
+            if (raise) m = top;
+          }
+          const float ref = m == kNegInf ? 0.f : m * c;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w16[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float e0 = ex2(fmaf(v[h * 64 + 2 * j], c, -ref)), e1 = ex2(fmaf(v[h * 64 + 2 * j + 1], c, -ref));
+              sum[(2 * j) & 3] += e0;
+              sum[(2 * j + 1) & 3] += e1;
+              // the weights go to the second product in the inputs' type, rounded to nearest; the sum above keeps 32 bits
+              w16[j] = pack2<BF>(e0, e1);
+            }
+            tm_st32(t_s + h * 32, w16);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tm_st_wait();
+        }
+        if (edge) {
+          // Values of keys that some row of the unit does not see: those that nobody sees (behind the last key, on a
+          // page outside the pool) become zero; an infinity or NaN among the others is taken out here, where it would
+          // reach rows with weight 0, and added in the epilogue to the rows that see it.
+          const int it = item0 + w.item_of_v(t);
+          wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
+          if (!ok) break;
+          unsigned char* vt = smem_raw + L::kRing + (it % L::kStages) * L::kStageBytes;
+          const int from = bad ? kKeys : min(kKeys, max(0, x.lo_last - k0)), to = bad ? kKeys : min(kKeys, max(from, x.hi_first - k0));
+          const int n_keys = from + (kKeys - to);          // keys [0, from) and [to, 128)
+          const int me = tid & 127;
+#pragma unroll 1
+          for (int pass = 0; pass < 2 && ok; ++pass) {
+            bool found = false;
+#pragma unroll 1
+            for (int e = me; e < n_keys * (DP / 8); e += 128) {
+              const int jj = e / (DP / 8), vec = e % (DP / 8), j = jj < from ? jj : jj - from + to;
+              uint4* at = reinterpret_cast<uint4*>(vt + (vec >> 3) * (kKeys * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
+              const bool nobody = k0 + j >= w.rq.kv || ((bad >> (j >> p.page_shift)) & 1u);
+              if (nobody) {
+                if (pass) *at = make_uint4(0u, 0u, 0u, 0u);
+              } else {
+                uint4 q = *at;
+                const uint32_t n0 = nonfinite_halves<BF>(q.x), n1 = nonfinite_halves<BF>(q.y), n2 = nonfinite_halves<BF>(q.z), n3 = nonfinite_halves<BF>(q.w);
+                if (n0 | n1 | n2 | n3) {
+                  found = true;
+                  if (pass) *at = make_uint4(q.x & ~n0, q.y & ~n1, q.z & ~n2, q.w & ~n3);
+                }
+              }
+            }
+            if (pass == 0) {
+              if (found) atomicOr(&sh->nonfinite, bad ? 3 : 1);
+              meet(x.two);   // everybody who has to has seen them before they go
+            }
+          }
+          if (!ok) break;
+          fence_async_proxy();
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->p_full[s]);
+      }
+      if (!ok) break;
+      // ---- end of the piece
+      const int n0 = x.two ? w.take : (w.take + 1) / 2, n1 = x.two ? w.take : w.take / 2;
+      const bool whole = w.starts() && w.ends();
+      const int slot = 2 * blockIdx.x + (w.index == 0 ? 0 : 1);
+      if (n0 > 0 && (s == 0 || !x.two)) wait(&sh->pv_done[0], (uint32_t)(done[0] + n0 - 1) & 1u);
+      if (n1 > 0 && (s == 1 || !x.two)) wait(&sh->pv_done[1], (uint32_t)(done[1] + n1 - 1) & 1u);
+      float f0 = 1.f, f1 = 1.f;
+      if (!x.two) {
+        sh->exch[s][r] = make_float2(m, l);
+        meet(true);
+        if (!ok) break;
+        const float2 a = sh->exch[0][r], b = sh->exch[1][r];
+        m = fmaxf(a.x, b.x);
+        f0 = a.x == kNegInf ? 0.f : ex2((a.x - m) * c);
+        f1 = b.x == kNegInf ? 0.f : ex2((b.x - m) * c);
+        l = a.y * f0 + b.y * f1;
+      }
+      if (!ok) break;
+      const int poisoned = *reinterpret_cast<volatile int*>(&sh->nonfinite);
+      const long long row = (long long)w.rq.row0 + tok;
+      const int head = w.hk * p.G + r_head;
+      const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+      const int part_row = (x.two ? s * 128 : 0) + r;
+      if (warp_live) {
+        const int j_lo = x.two ? 0 : s * (DP / 2), j_hi = x.two ? DP : (s + 1) * (DP / 2);
+#pragma unroll 1
+        for (int j0 = j_lo; j0 < j_hi; j0 += 32) {
+          float o[32];
+          if (x.two) {
+            tm_ld32(t_o + j0, o);
+            tm_ld_wait();
+          } else {
+            tm_ld32(tmem + lanes + 256 + j0, o);
+            tm_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] *= f0;
+            if (n1 > 0) {
+              float o1[32];
+              tm_ld32(tmem + lanes + 384 + j0, o1);
+              tm_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = fmaf(o1[j], f1, o[j]);
+            }
+          }
+          if (poisoned && live) {
+            const int k_lo = max(lo, (x.t0 + w.off) * kKeys), k_hi = min(hi, (x.t0 + w.off + w.take) * kKeys);
+            for (int key = k_lo; key < k_hi; ++key) {
+              // only those that were taken out: not seen by every row of the unit, or in a tile with a bad page
+              if (!(poisoned & 2) && key < x.hi_first && key >= x.lo_last) continue;
+              const int page = p.d.block_table[(long long)w.b * p.d.ld_table + key / p.d.page_size];
+              if (page < 0 || page >= p.d.n_pages) continue;
+              const unsigned short* v = reinterpret_cast<const unsigned short*>(p.d.v_cache) + page * p.d.vc_page + (key % p.d.page_size) * p.d.vc_slot + w.hk * p.d.vc_head + j0;
+              for (int j = 0; j < 32 && j0 + j < p.d.D; ++j) {
+                const unsigned short bits = v[j];
+                if (nonfinite_halves<BF>(bits) & 0xffffu) {
+                  const float y = BF ? __uint_as_float((uint32_t)bits << 16) : __half2float(__ushort_as_half(bits));
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if (i == j) o[i] += y;
+                }
+              }
+            }
+          }
+          if (live) {
+            if (whole) {
+              unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head + j0;
+              uint32_t y[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) y[j] = pack2<BF>(o[2 * j] * inv, o[2 * j + 1] * inv);
+              if (p.out_vec) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (j0 + 8 * j < p.d.D) reinterpret_cast<uint4*>(dst)[j] = make_uint4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                  if (j0 + j < p.d.D) dst[j] = (unsigned short)(y[j >> 1] >> ((j & 1) * 16));
+              }
+            } else {
+              float4* dst = reinterpret_cast<float4*>(p.part + ((long long)slot * 256 + part_row) * DP + j0);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+            }
+          }
+        }
+        if (live && (x.two || s == 0)) {
+          if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m * c, l);   // c > 0: -inf stays
+          else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m * c + log2f(l)) * kLn2;
+        }
+      }
+      if (tid == 0 && !whole) {
+        int* h = p.head + blockIdx.x * 8;
+        if (w.starts()) { h[0] = slot; h[2] = w.b; h[3] = w.hk; h[4] = w.u; }
+        else if (w.ends()) h[1] = 1;
+      }
+      if (!x.two) meet(true);   // both halves of the sums are read before either stream goes on
+      done[0] += n0;
+      done[1] += n1;
+      item0 += 2 * w.take;
+      tiles0 += w.take;
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    fence_after();
+    tc_dealloc(tmem);
+  }
+}
+
+// Puts the parts of a cut unit together: block x takes the unit that begins in CTA x and goes on in the CTAs behind it.
+// One warp a row; the parts are added in their order, so the bits do not depend on who came first.
+template <int DP, bool BF>
+__global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
+  pdl_wait();
+  const int cta = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int* h = p.head + cta * 8;
+  const int slot0 = h[0];
+  if (slot0 < 0) return;
+  const int b = h[2], hk = h[3], u = h[4];
+  const AttnRequest rq = attn_request(p.d, b);
+  const Unit x = make_unit(p, rq, u);
+  int parts = 1;
+  while (cta + parts < n_cta) {   // part i lies in slot 2*(cta + i), the first one in slot0
+    const bool end = p.head[(cta + parts) * 8 + 1] != 0;
+    ++parts;
+    if (end) break;
+  }
+  const int rows = (x.tok1 - x.tok0) * p.G;
+  for (int q = blockIdx.y * 8 + warp; q < rows; q += gridDim.y * 8) {
+    const int tile_rows = p.tile_tok * p.G;
+    const int part_row = q < tile_rows ? q : 128 + q - tile_rows;
+    auto slot_of = [&](int i) { return (long long)(i == 0 ? slot0 : 2 * (cta + i)) * 256 + part_row; };
+    float m = kNegInf;
+    for (int i = lane; i < parts; i += 32) m = fmaxf(m, p.part_ml[slot_of(i)].x);
+    m = warp_max(m);
+    float l = 0.f, o[DP / 32];
+#pragma unroll
+    for (int j = 0; j < DP / 32; ++j) o[j] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+      const long long at = slot_of(i);
+      const float2 ml = p.part_ml[at];
+      const float f = ml.x == kNegInf ? 0.f : ex2(ml.x - m);
+      l = fmaf(ml.y, f, l);
+      const float* src = p.part + at * DP + lane * (DP / 32);
+      if (DP == 128) {
+        const float4 y = *reinterpret_cast<const float4*>(src);
+        o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]); o[2 % (DP / 32)] = fmaf(y.z, f, o[2 % (DP / 32)]); o[3 % (DP / 32)] = fmaf(y.w, f, o[3 % (DP / 32)]);
+      } else {
+        const float2 y = *reinterpret_cast<const float2*>(src);
+        o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]);
+      }
+    }
+    const int tok = x.tok0 + q / p.G, head = hk * p.G + q % p.G;
+    const long long row = (long long)rq.row0 + tok;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head;
+#pragma unroll
+    for (int j = 0; j < DP / 32; j += 2) {
+      const int d = lane * (DP / 32) + j;
+      const uint32_t y = pack2<BF>(o[j] * inv, o[j + 1] * inv);
+      if (d < p.d.D) dst[d] = (unsigned short)y;
+      if (d + 1 < p.d.D) dst[d + 1] = (unsigned short)(y >> 16);
+    }
+    if (lane == 0 && p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m + log2f(l)) * kLn2;
+  }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn tiled_encoder() {
+  static EncodeTiledFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      return (EncodeTiledFn) nullptr;
+    return (EncodeTiledFn)f;
+  }();
+  return fn;
+}
+
+// A tensor of 16-bit elements, innermost axis dense, boxes of 64 elements (128 bytes, 128-byte swizzle), zeros outside.
+bool encode(CUtensorMap* tm, bool bf16, const void* base, int rank, const long long* dims, const long long* strides, const int* box) {
+  EncodeTiledFn fn = tiled_encoder();
+  if (!fn) return false;
+  cuuint64_t d[4], st[3];
+  cuuint32_t bx[4], one[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    bx[i] = (cuuint32_t)box[i];
+    if (i) st[i - 1] = (cuuint64_t)(dims[i] > 1 ? strides[i] * 2 : 16);   // the stride of an axis of one carries nothing
+  }
+  return fn(tm, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, bx, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
+
+// Query boxes of whole tokens: as few tokens as make a multiple of 8 rows (the swizzle's period), then about 32 rows.
+bool query_box(int G, int* box_tok, int* boxes) {
+  if (G > 128) return false;
+  int tok = 8 / gcd(G, 8);
+  if (tok * G > 128) return false;
+  while (tok * G * 2 <= 32) tok *= 2;
+  *box_tok = tok;
+  *boxes = 128 / (tok * G);
+  return true;
+}
+
+constexpr int kMaxCtas = 148;
+size_t part_bytes(int DP) { return (size_t)2 * kMaxCtas * 256 * DP * sizeof(float); }
+size_t ml_bytes() { return (size_t)2 * kMaxCtas * 256 * sizeof(float2); }
+size_t head_bytes() { return (size_t)kMaxCtas * 8 * sizeof(int); }
+
+template <int DP, bool BF>
+cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStream_t s) {
+  static std::atomic<bool> attr_set[64];   // per device; two host threads that both find it clear set the same value
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!attr_set[dev & 63].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(attention_tc_kernel<DP, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem_bytes<DP>());
+    if (e != cudaSuccess) return e;
+    attr_set[dev & 63].store(true, std::memory_order_release);
+  }
+  attention_tc_kernel<DP, BF><<<grid, kTcThreads, tc_smem_bytes<DP>(), s>>>(tm[0], tm[1], tm[2], p);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 4);
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attention_join_kernel<DP, BF>, p, grid);
+}
+
+}  // namespace
+
+bool attention_tc_takes(const specsteer_attention_desc* d) {
+  int tok, boxes;
+  auto a16 = [](const void* q) { return ((uintptr_t)q & 15u) == 0; };
+  // strides of axes longer than one: positive multiples of 16 bytes below the tensor map's limit
+  auto ok = [](long long stride, long long extent) { return extent <= 1 || (stride > 0 && stride % 8 == 0 && stride < (1ll << 38)); };
+  const int pr = d->page_size < kKeys ? d->page_size : kKeys;
+  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->D >= 64 && d->D <= 128 && d->D % 8 == 0 && pr % 8 == 0 && kKeys % pr == 0 && d->page_size % pr == 0 &&
+         query_box(d->Hq / d->Hkv, &tok, &boxes) && a16(d->q) && a16(d->k_cache) && a16(d->v_cache) && ok(d->q_tok, d->T) && ok(d->q_head, d->Hq) &&
+         ok(d->kc_page, d->n_pages) && ok(d->kc_slot, d->page_size) && ok(d->kc_head, d->Hkv) && ok(d->vc_page, d->n_pages) &&
+         ok(d->vc_slot, d->page_size) && ok(d->vc_head, d->Hkv);
+}
+
+size_t attention_tc_workspace(const specsteer_attention_desc* d) { return part_bytes(d->D <= 64 ? 64 : 128) + ml_bytes() + head_bytes(); }
+
+cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t s) {
+  const int sm = current_sm_count();
+  if (sm <= 0) return cudaErrorInvalidDevice;
+  const bool bf16 = d->dtype == SPECSTEER_BF16;
+  const int DP = d->D <= 64 ? 64 : 128;
+  TcParams p;
+  p.d = *d;
+  p.G = d->Hq / d->Hkv;
+  int boxes = 0;
+  query_box(p.G, &p.box_tok, &boxes);
+  p.box_rows = p.box_tok * p.G;
+  p.tile_tok = boxes * p.box_tok;
+  p.page_rows = d->page_size < kKeys ? d->page_size : kKeys;
+  p.boxes = kKeys / p.page_rows;
+  p.page_shift = 0;
+  while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
+  p.c = d->scale * kLog2e;
+  if (p.c < 1e-30f) p.c = 1e-30f;   // a scale of zero: weights all 1 without 0 * infinity for masked scores
+  p.out_vec = ((uintptr_t)d->out & 15u) == 0 && d->o_tok % 8 == 0 && d->o_head % 8 == 0;
+  p.part = (float*)d->workspace;
+  p.part_ml = (float2*)((char*)d->workspace + part_bytes(DP));
+  p.head = (int*)((char*)d->workspace + part_bytes(DP) + ml_bytes());
+  CUtensorMap tm[3];
+  {
+    const long long dims[3] = {d->D, d->Hq, d->T}, st[3] = {0, d->q_head, d->q_tok};
+    const int box[3] = {64, p.G, p.box_tok};
+    if (!encode(&tm[0], bf16, d->q, 3, dims, st, box)) return cudaErrorInvalidValue;
+  }
+  const long long dims[4] = {d->D, d->page_size, d->Hkv, d->n_pages};
+  const int box[4] = {64, p.page_rows, 1, 1};
+  const long long ks[4] = {0, d->kc_slot, d->kc_head, d->kc_page}, vs[4] = {0, d->vc_slot, d->vc_head, d->vc_page};
+  if (!encode(&tm[1], bf16, d->k_cache, 4, dims, ks, box) || !encode(&tm[2], bf16, d->v_cache, 4, dims, vs, box)) return cudaErrorInvalidValue;
+  const int grid = sm < kMaxCtas ? sm : kMaxCtas;
+  if (DP == 128) return bf16 ? launch<128, true>(tm, p, grid, s) : launch<128, false>(tm, p, grid, s);
+  return bf16 ? launch<64, true>(tm, p, grid, s) : launch<64, false>(tm, p, grid, s);
+}
+
+}  // namespace specsteer
