@@ -53,8 +53,8 @@ struct TcShared {
   int abort_flag;
   int nonfinite;           // an infinity or NaN was taken out of a tile of values: bit 0, and bit 1 in a tile with a bad page
   int start_b, start_hk, start_u, start_off;
-  long long n_tiles;       // tiles of this CTA's range
-  long long scan[10];
+  long long end;           // where this CTA's range ends, from the beginning of its first unit (0: it has none)
+  long long scan[kTcThreads / 32];
   uint32_t bad[16];        // per key tile (counted modulo 16): the boxes of it that lie outside the pool
   float2 exch[2][128];     // reference and sum of each stream's rows
 };
@@ -135,7 +135,32 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
       "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tm_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(u[0]),
+      "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]),
+      "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
+      : "memory");
+}
+// Waits for the loads issued so far.  v, the registers of the load, are operands so that nothing that uses them moves ahead.
+__device__ __forceinline__ void tm_ld_wait(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                 "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tm_ld_wait(float* v, float* w) {
+  tm_ld_wait(v);
+  asm volatile("" : "+f"(w[0]), "+f"(w[1]), "+f"(w[2]), "+f"(w[3]), "+f"(w[4]), "+f"(w[5]), "+f"(w[6]), "+f"(w[7]),
+                 "+f"(w[8]), "+f"(w[9]), "+f"(w[10]), "+f"(w[11]), "+f"(w[12]), "+f"(w[13]), "+f"(w[14]), "+f"(w[15]),
+                 "+f"(w[16]), "+f"(w[17]), "+f"(w[18]), "+f"(w[19]), "+f"(w[20]), "+f"(w[21]), "+f"(w[22]), "+f"(w[23]),
+                 "+f"(w[24]), "+f"(w[25]), "+f"(w[26]), "+f"(w[27]), "+f"(w[28]), "+f"(w[29]), "+f"(w[30]), "+f"(w[31])
+               :
+               : "memory");
+}
 __device__ __forceinline__ void tm_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared-memory descriptors of 128-byte swizzled operands, in units of 16 bytes.  K and Q (rows of 64 elements along the
@@ -154,6 +179,24 @@ __device__ __forceinline__ uint32_t instr_desc(bool bf16, int n, bool b_by_colum
   return (1u << 4) | (f << 7) | (f << 10) | ((b_by_columns ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
+// two float32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
 template <bool BF> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
   if (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -167,12 +210,25 @@ template <bool BF> __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t
 }
 
 __device__ __forceinline__ bool aborted(const TcShared* sh) { return *reinterpret_cast<const volatile int*>(&sh->abort_flag) != 0; }
+// Bounded wait for a phase of a barrier; gives up too when another warp has.
+__device__ __forceinline__ bool tc_wait(TcShared* sh, uint64_t* bar, uint32_t parity) {
+  if (mbar_test(bar, parity, kSuspendNs)) return true;
+  const long long t0 = clock64();
+  for (;;) {
+    if (mbar_test(bar, parity, kSuspendNs)) return true;
+    if (aborted(sh) || clock64() - t0 > kWaitCycles) return false;
+  }
+}
 __device__ __forceinline__ void give_up(TcShared* sh, const TcParams& p, int b) {
   *reinterpret_cast<volatile int*>(&sh->abort_flag) = 1;
   if (p.d.req_status && b < p.d.B) atomicOr(p.d.req_status + b, SPECSTEER_REQ_TIMEOUT);
 }
 
 // ---- units ----------------------------------------------------------------------------------------------------------
+// The cut weighs a unit by its key tiles, twice as much with two query tiles, and a constant for its beginning and end
+// (queries, first scores, result).
+constexpr int kUnitCost = 8;
+
 struct Unit {
   int tok0, tok1;          // tokens of the request
   bool two;                // two query tiles
@@ -191,43 +247,50 @@ __device__ __forceinline__ Unit make_unit(const TcParams& p, const AttnRequest& 
   x.nt = max(1, (max(x.hi_last, 0) + kKeys - 1) / kKeys - x.t0);
   return x;
 }
+__device__ __forceinline__ long long unit_cost(const Unit& x) { return (long long)x.nt * (x.two ? 2 : 1) + kUnitCost; }
+// The key tile at which a cut `pos` into the unit falls.
+__device__ __forceinline__ int cut_tile(const Unit& x, long long pos) {
+  return pos <= kUnitCost ? 0 : (int)min((long long)x.nt, (pos - kUnitCost) / (x.two ? 2 : 1));
+}
 __device__ __forceinline__ int n_units(const TcParams& p, const AttnRequest& rq) { return (rq.n + 2 * p.tile_tok - 1) / (2 * p.tile_tok); }
-__device__ __forceinline__ long long head_tiles(const TcParams& p, const AttnRequest& rq) {
+__device__ __forceinline__ long long head_cost(const TcParams& p, const AttnRequest& rq) {
   long long c = 0;
-  for (int u = 0, nu = n_units(p, rq); u < nu; ++u) c += make_unit(p, rq, u).nt;
+  for (int u = 0, nu = n_units(p, rq); u < nu; ++u) c += unit_cost(make_unit(p, rq, u));
   return c;
 }
 
 // Walks this CTA's share: the pieces [off, off + take) of consecutive units.
 struct Walk {
   int b, hk, u, off, take, index;
-  long long left;
+  long long end;     // where the range ends, from the beginning of the unit
   AttnRequest rq;
   Unit x;
   __device__ __forceinline__ void begin(const TcParams& p, const TcShared* sh) {
     b = sh->start_b; hk = sh->start_hk; u = sh->start_u; off = sh->start_off;
-    left = sh->n_tiles;
+    end = sh->end;
     index = 0;
-    if (left > 0) load(p);
+    take = 0;
+    if (end > 0) load(p);
   }
   __device__ __forceinline__ void load(const TcParams& p) {
     rq = attn_request(p.d, b);
     x = make_unit(p, rq, u);
-    take = (int)min((long long)(x.nt - off), left);
+    take = (end >= unit_cost(x) ? x.nt : cut_tile(x, end)) - off;
   }
-  __device__ __forceinline__ bool more() const { return left > 0; }
+  __device__ __forceinline__ bool more() const { return take > 0; }
   __device__ __forceinline__ bool starts() const { return off == 0; }
   __device__ __forceinline__ bool ends() const { return off + take == x.nt; }
   __device__ __forceinline__ void next(const TcParams& p) {
-    left -= take;
+    end -= unit_cost(x);
+    take = 0;
     ++index;
-    if (left <= 0) return;
+    if (end <= 0) return;
     off = 0;
     if (++u == n_units(p, rq)) {
       u = 0;
       if (++hk == p.d.Hkv) {
         hk = 0;
-        do { ++b; rq = attn_request(p.d, b); } while (rq.n == 0 && b + 1 < p.d.B);   // left > 0: a request with rows follows
+        do { ++b; rq = attn_request(p.d, b); } while (rq.n == 0 && b + 1 < p.d.B);   // end > 0: a request with rows follows
       }
     }
     load(p);
@@ -280,7 +343,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     mbar_init(&sh->drain, 1);
     sh->abort_flag = 0;
     sh->nonfinite = 0;
-    sh->n_tiles = 0;
+    sh->end = 0;
     fence_barrier_init();
   }
   if (warp == kMmaWarp) tc_alloc(&sh->tmem_slot);
@@ -292,31 +355,27 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     for (int b = b_lo; b < b_hi; ++b) {
       const AttnRequest rq = attn_request(p.d, b);
       if (rq.bad && blockIdx.x == 0 && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_LEN);
-      if (rq.n > 0) mine += head_tiles(p, rq) * p.d.Hkv;
+      if (rq.n > 0) mine += head_cost(p, rq) * p.d.Hkv;
     }
     const long long before = block_sum(mine, sh, &total);   // (its barrier also publishes the set-up above)
-    const long long ctas = min(total, (long long)gridDim.x);   // every one of these has at least one tile
-    if (blockIdx.x < ctas) {
-      const long long s0 = total * blockIdx.x / ctas, s1 = total * (blockIdx.x + 1) / ctas;
-      if (s0 >= before && s0 < before + mine) {
-        long long rem = s0 - before;
-        for (int b = b_lo; b < b_hi; ++b) {
-          const AttnRequest rq = attn_request(p.d, b);
-          if (rq.n == 0) continue;
-          const long long per_head = head_tiles(p, rq);
-          if (rem >= per_head * p.d.Hkv) { rem -= per_head * p.d.Hkv; continue; }
-          const int hk = (int)(rem / per_head);
-          rem -= hk * per_head;
-          int u = 0;
-          for (;; ++u) {
-            const int nt = make_unit(p, rq, u).nt;
-            if (rem < nt) break;
-            rem -= nt;
-          }
-          sh->start_b = b; sh->start_hk = hk; sh->start_u = u; sh->start_off = (int)rem;
-          sh->n_tiles = s1 - s0;
+    const long long s0 = total * blockIdx.x / gridDim.x, s1 = total * (blockIdx.x + 1) / gridDim.x;
+    if (s1 > s0 && s0 >= before && s0 < before + mine) {
+      long long rem = s0 - before;
+      for (int b = b_lo; b < b_hi; ++b) {
+        const AttnRequest rq = attn_request(p.d, b);
+        if (rq.n == 0) continue;
+        const long long per_head = head_cost(p, rq);
+        if (rem >= per_head * p.d.Hkv) { rem -= per_head * p.d.Hkv; continue; }
+        const int hk = (int)(rem / per_head);
+        rem -= hk * per_head;
+        for (int u = 0;; ++u) {
+          const Unit x = make_unit(p, rq, u);
+          if (rem >= unit_cost(x)) { rem -= unit_cost(x); continue; }
+          sh->start_b = b; sh->start_hk = hk; sh->start_u = u; sh->start_off = cut_tile(x, rem);
+          sh->end = rem + s1 - s0;
           break;
         }
+        break;
       }
     }
   }
@@ -344,7 +403,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       return page;
     };
     auto stage_free = [&](int it) {
-      const bool got = !aborted(sh) && mbar_wait(&sh->empty[it % L::kStages], (uint32_t)((it / L::kStages) & 1) ^ 1u);
+      const bool got = tc_wait(sh, &sh->empty[it % L::kStages], (uint32_t)((it / L::kStages) & 1) ^ 1u);
       ok = __all_sync(kFullMask, got);
     };
     auto load_tile = [&](const CUtensorMap* tm, int t, int page) {
@@ -378,7 +437,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const int n_q = w.x.two ? 2 : 1;
       for (int s = 0; s < n_q && ok; ++s, ++qi) {
         const int slot = qi & 1;
-        const bool got = !aborted(sh) && mbar_wait(&sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
+        const bool got = tc_wait(sh, &sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
         ok = __all_sync(kFullMask, got);
         if (!ok) break;
         const int tok = w.x.tok0 + s * p.tile_tok, cnt = min(p.tile_tok, w.x.tok1 - tok);
@@ -420,7 +479,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (!ok) return;
-        if (aborted(sh) || !mbar_wait(bar, parity)) { give_up(sh, p, w.b); ok = false; return; }
+        if (!tc_wait(sh, bar, parity)) { give_up(sh, p, w.b); ok = false; return; }
         fence_after();
       };
       auto wait_item = [&](int it) { wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1)); };
@@ -512,7 +571,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (!ok) return;
-      const bool got = !aborted(sh) && mbar_wait(bar, parity);
+      const bool got = tc_wait(sh, bar, parity);
       ok = __all_sync(kFullMask, got);
       if (!ok && lane == 0) give_up(sh, p, w.b);
       fence_after();
@@ -528,7 +587,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     if (tid == 0) {
       int* h = p.head + blockIdx.x * 8;
       h[0] = -1;   // slot of a unit that begins in this CTA and goes on in the next
-      h[1] = 0;    // 1: the unit that was going on ends in this CTA
+      h[1] = 0;    // its part of a unit that began in a CTA before: 0 none, 1 the end, 2 some in between
     }
     for (; w.more() && ok; w.next(p)) {
       const Unit& x = w.x;
@@ -546,24 +605,40 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(tiles0 + t) & 15]);
         const bool edge = k0 + kKeys > x.hi_first || k0 < x.lo_last || bad != 0;
         if (warp_live) {
-          float v[128];
-          tm_ld32(t_s, v); tm_ld32(t_s + 32, v + 32); tm_ld32(t_s + 64, v + 64); tm_ld32(t_s + 96, v + 96);
-          tm_ld_wait();
-          if (edge) {
-            const int a = lo - k0, e = hi - k0;
-#pragma unroll
-            for (int j = 0; j < 128; ++j) v[j] = (j >= a && j < e) ? v[j] : kNegInf;
+          // The scores are read from tensor memory twice, 32 columns at a time, rather than kept in 128 registers, and the
+          // loops stay loops: unrolled, the masked and plain variants overran the instruction cache.
+          const int a = lo - k0, e = hi - k0;
+          // the columns of [j0, j0 + 32) that the row sees, as bits
+          auto seen = [&](int j0) -> uint32_t {
+            const int from = max(a - j0, 0), to = min(e - j0, 32);
+            uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
             if (bad) {
-#pragma unroll
-              for (int j = 0; j < 128; ++j)
-                if ((bad >> (j >> p.page_shift)) & 1u) v[j] = kNegInf;
+              for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
+                if ((bad >> ((j0 + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
             }
-          }
+            return keep;
+          };
+          auto mask = [&](float* v, uint32_t keep) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = (keep & (1u << j)) ? v[j] : kNegInf;
+          };
+          float va[32], vb[32];
           float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+          auto take_max = [&](const float* v) {
 #pragma unroll
-          for (int j = 0; j < 128; j += 8) {
+            for (int j = 0; j < 32; j += 8) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
+              for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
+            }
+          };
+#pragma unroll 1
+          for (int j0 = 0; j0 < kKeys; j0 += 64) {
+            tm_ld32(t_s + j0, va);
+            tm_ld32(t_s + j0 + 32, vb);
+            tm_ld_wait(va, vb);
+            if (edge) { mask(va, seen(j0)); mask(vb, seen(j0 + 32)); }
+            take_max(va);
+            take_max(vb);
           }
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           const bool raise = top > m && (m == kNegInf || (top - m) * c > kGrow);
@@ -576,7 +651,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               for (int j0 = 0; j0 < DP; j0 += 32) {
                 float o[32];
                 tm_ld32(t_o + j0, o);
-                tm_ld_wait();
+                tm_ld_wait(o);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) o[j] *= alpha;
                 tm_st32(t_o + j0, reinterpret_cast<const uint32_t*>(o));
@@ -586,21 +661,32 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (raise) m = top;
           }
           const float ref = m == kNegInf ? 0.f : m * c;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          // Weights of 32 columns; they take 16 columns of the scores' place, all of them read by then.  They go to the
+          // second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
+          auto weigh = [&](const float* v, int j0) {
+            uint32_t w16[16];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w16[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float e0 = ex2(fmaf(v[h * 64 + 2 * j], c, -ref)), e1 = ex2(fmaf(v[h * 64 + 2 * j + 1], c, -ref));
-              sum[(2 * j) & 3] += e0;
-              sum[(2 * j + 1) & 3] += e1;
-              // the weights go to the second product in the inputs' type, rounded to nearest; the sum above keeps 32 bits
-              w16[j] = pack2<BF>(e0, e1);
+            for (int j = 0; j < 16; ++j) {
+              const float2 x2 = fma2(make_float2(v[2 * j], v[2 * j + 1]), c2, ref2);
+              const float2 y = make_float2(ex2(x2.x), ex2(x2.y));
+              sum[j & 1] = add2(sum[j & 1], y);
+              w16[j] = pack2<BF>(y.x, y.y);
             }
-            tm_st32(t_s + h * 32, w16);
+            tm_st16(t_s + j0 / 2, w16);
+          };
+#pragma unroll 1
+          for (int j0 = 0; j0 < kKeys; j0 += 64) {
+            tm_ld32(t_s + j0, va);
+            tm_ld32(t_s + j0 + 32, vb);
+            tm_ld_wait(va, vb);
+            if (edge) { mask(va, seen(j0)); mask(vb, seen(j0 + 32)); }
+            weigh(va, j0);
+            weigh(vb, j0 + 32);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          sum[0] = add2(sum[0], sum[1]);
+          l += sum[0].x + sum[0].y;
           tm_st_wait();
         }
         if (edge) {
@@ -676,16 +762,16 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           float o[32];
           if (x.two) {
             tm_ld32(t_o + j0, o);
-            tm_ld_wait();
+            tm_ld_wait(o);
           } else {
             tm_ld32(tmem + lanes + 256 + j0, o);
-            tm_ld_wait();
+            tm_ld_wait(o);
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] *= f0;
             if (n1 > 0) {
               float o1[32];
               tm_ld32(tmem + lanes + 384 + j0, o1);
-              tm_ld_wait();
+              tm_ld_wait(o1);
 #pragma unroll
               for (int j = 0; j < 32; ++j) o[j] = fmaf(o1[j], f1, o[j]);
             }
@@ -739,7 +825,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (tid == 0 && !whole) {
         int* h = p.head + blockIdx.x * 8;
         if (w.starts()) { h[0] = slot; h[2] = w.b; h[3] = w.hk; h[4] = w.u; }
-        else if (w.ends()) h[1] = 1;
+        else h[1] = w.ends() ? 1 : 2;
       }
       if (!x.two) meet(true);   // both halves of the sums are read before either stream goes on
       done[0] += n0;
@@ -768,25 +854,29 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   const int b = h[2], hk = h[3], u = h[4];
   const AttnRequest rq = attn_request(p.d, b);
   const Unit x = make_unit(p, rq, u);
-  int parts = 1;
-  while (cta + parts < n_cta) {   // part i lies in slot 2*(cta + i), the first one in slot0
-    const bool end = p.head[(cta + parts) * 8 + 1] != 0;
-    ++parts;
-    if (end) break;
+  // the parts: the first one in slot0, then slot 2*(cta + i) of every CTA behind that has one, to the unit's end
+  int span = 1;
+  while (cta + span < n_cta) {
+    const int kind = p.head[(cta + span) * 8 + 1];
+    ++span;
+    if (kind == 1) break;
   }
   const int rows = (x.tok1 - x.tok0) * p.G;
   for (int q = blockIdx.y * 8 + warp; q < rows; q += gridDim.y * 8) {
     const int tile_rows = p.tile_tok * p.G;
     const int part_row = q < tile_rows ? q : 128 + q - tile_rows;
     auto slot_of = [&](int i) { return (long long)(i == 0 ? slot0 : 2 * (cta + i)) * 256 + part_row; };
+    auto has = [&](int i) { return i == 0 || p.head[(cta + i) * 8 + 1] != 0; };
     float m = kNegInf;
-    for (int i = lane; i < parts; i += 32) m = fmaxf(m, p.part_ml[slot_of(i)].x);
+    for (int i = lane; i < span; i += 32)
+      if (has(i)) m = fmaxf(m, p.part_ml[slot_of(i)].x);
     m = warp_max(m);
     float l = 0.f, o[DP / 32];
 #pragma unroll
     for (int j = 0; j < DP / 32; ++j) o[j] = 0.f;
 #pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
+    for (int i = 0; i < span; ++i) {
+      if (!has(i)) continue;
       const long long at = slot_of(i);
       const float2 ml = p.part_ml[at];
       const float f = ml.x == kNegInf ? 0.f : ex2(ml.x - m);
