@@ -9,9 +9,10 @@
 // cut needs nothing from the host: every CTA sums the lengths itself.  A unit that a cut goes through leaves partial
 // results (unnormalised sums, maximum and sum of weights per row) that attention_join_kernel puts together.
 //
-// Inside a CTA: warp 8 issues the TMA loads (a ring of stages of one 128-key tile of K or V; a page or its part of 128
-// keys is a box), warp 9 issues tcgen05.mma, warps 0..3 and 4..7 are two softmax groups (streams), one row a thread.
-// Stream s has scores S_s (128 columns of tensor memory, overwritten by the 16-bit weights P_s, which the second product
+// Inside a CTA: warp 16 issues the TMA loads (a ring of stages of one 128-key tile of K or V; a page or its part of 128
+// keys is a box), warp 17 issues tcgen05.mma, and two softmax groups (streams) of 8 warps turn scores into weights.  A row
+// belongs to two threads of two warps, 64 keys of a tile each, which exchange their maxima through shared memory: one
+// thread a row left too few independent instructions to fill the pipes.  Stream s has scores S_s (128 columns of tensor memory, overwritten by the 16-bit weights P_s, which the second product
 // reads from tensor memory) and sums O_s (128 columns).  With two query tiles each stream owns one and both use every
 // key tile; with one query tile the streams take the key tiles in turn and are put together at the end.  Either way one
 // stream's exponentials run under the other stream's products.
@@ -31,10 +32,14 @@ namespace specsteer {
 namespace {
 
 constexpr int kKeys = 128;          // keys per tile
-constexpr int kTcThreads = 320;
-constexpr int kProducerWarp = 8, kMmaWarp = 9;
+constexpr int kSplit = 1;           // threads that share a row of scores
+constexpr int kSoftmaxWarps = 8 * kSplit;
+constexpr int kProducerWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+constexpr int kTcThreads = 32 * (kSoftmaxWarps + 2);
 constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
+constexpr int kPolyPairs = 0;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
 constexpr float kGrow = 8.f;        // powers of two the maximum may exceed the reference by
+constexpr int kPieces = 4;          // pieces of work the producer may be ahead
 
 template <int DP> struct TcLayout {
   static constexpr int kStageBytes = kKeys * DP * 2;
@@ -44,19 +49,38 @@ template <int DP> struct TcLayout {
   static constexpr int kControl = kRing + kStages * kStageBytes;  // offset of TcShared
 };
 
+// A piece of work: key tiles [first, first + take) of one unit (see Unit).
+struct Piece {
+  int b, hk, u;
+  int row0, n, kv;             // of the request
+  int tok0, tok1;              // the unit's tokens
+  int two;                     // two query tiles
+  int hi_first, lo_last;       // where the keys of the first row end, where those of the last row begin
+  int first, take;             // take = 0: no more pieces
+  int starts, ends;            // the piece holds the unit's first / last key tile
+  int index;                   // of the pieces of this CTA
+  // Ring items: the keys of the first `ahead` tiles, then per tile its values and the keys `ahead` tiles on.
+  __device__ __forceinline__ int ahead() const { return min(two ? 1 : 2, take); }
+  __device__ __forceinline__ int item_of_v(int t) const { return ahead() + min(t, take - ahead()) + t; }
+};
+
 struct TcShared {
   uint64_t full[12], empty[12];
   uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t s_full[2], p_full[2][2], o_full;   // p_full[s][h]: weights of the first / last 64 keys of a tile
+  uint64_t piece_full[kPieces], piece_empty[kPieces];
   uint64_t both, group[2], drain;
   uint32_t tmem_slot;
   int abort_flag;
   int nonfinite;           // an infinity or NaN was taken out of a tile of values: bit 0, and bit 1 in a tile with a bad page
   int start_b, start_hk, start_u, start_off;
   long long end;           // where this CTA's range ends, from the beginning of its first unit (0: it has none)
-  long long scan[kTcThreads / 32];
+  Piece piece[kPieces];
   uint32_t bad[16];        // per key tile (counted modulo 16): the boxes of it that lie outside the pool
-  float2 exch[2][128];     // reference and sum of each stream's rows
+  union {
+    long long scan[kTcThreads / 32];
+    float exch[2][2][128]; // [stream][half][row]: a tile's maxima; at the end of a piece sums, references
+  };
 };
 template <int DP> constexpr int tc_smem_bytes() { return TcLayout<DP>::kControl + (int)sizeof(TcShared); }
 static_assert(tc_smem_bytes<128>() <= 232448 && tc_smem_bytes<64>() <= 232448, "shared memory of one CTA");
@@ -65,6 +89,7 @@ struct TcParams {
   specsteer_attention_desc d;
   int G, box_tok, box_rows, tile_tok;  // query box: tokens and rows; tokens of a query tile
   int page_rows, boxes, page_shift;    // key box: keys, boxes per key tile, log2 of its keys
+  int page_tiles;                      // key tiles per page (1 when a tile has several pages)
   float c;                             // scale * log2(e)
   int out_vec;                         // out rows are 16-byte aligned
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
@@ -95,22 +120,31 @@ __device__ __forceinline__ void tc_dealloc(uint32_t addr) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// D (+)= A B^T with both operands in shared memory
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// One thread of the (converged) warp issues.  The election is inside the statement: behind a branch of that thread the
+// compiler moves every operand to uniform registers anew, and the issue takes longer than the product.
+// D (+)= A B^T with both operands in shared memory; descriptors by their low words, the high words are alike.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 x, y;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHigh)
       : "memory");
 }
 // the same with A in tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 y;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHigh)
       : "memory");
 }
+// the barrier receives one arrival once every tcgen05.mma issued so far by the electing thread has completed
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+      : "memory");
 }
 __device__ __forceinline__ void tm_ld32(uint32_t addr, float* r) {
   uint32_t* u = reinterpret_cast<uint32_t*>(r);
@@ -125,14 +159,13 @@ __device__ __forceinline__ void tm_ld32(uint32_t addr, float* r) {
       : "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
+__device__ __forceinline__ void tm_ld16(uint32_t addr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(u[0]),
-      "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]),
-      "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]),
-      "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(addr)
       : "memory");
 }
 __device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* u) {
@@ -152,27 +185,30 @@ __device__ __forceinline__ void tm_ld_wait(float* v) {
                :
                : "memory");
 }
-__device__ __forceinline__ void tm_ld_wait(float* v, float* w) {
-  tm_ld_wait(v);
-  asm volatile("" : "+f"(w[0]), "+f"(w[1]), "+f"(w[2]), "+f"(w[3]), "+f"(w[4]), "+f"(w[5]), "+f"(w[6]), "+f"(w[7]),
-                 "+f"(w[8]), "+f"(w[9]), "+f"(w[10]), "+f"(w[11]), "+f"(w[12]), "+f"(w[13]), "+f"(w[14]), "+f"(w[15]),
-                 "+f"(w[16]), "+f"(w[17]), "+f"(w[18]), "+f"(w[19]), "+f"(w[20]), "+f"(w[21]), "+f"(w[22]), "+f"(w[23]),
-                 "+f"(w[24]), "+f"(w[25]), "+f"(w[26]), "+f"(w[27]), "+f"(w[28]), "+f"(w[29]), "+f"(w[30]), "+f"(w[31])
+// the same for further registers of the loads that tm_ld_wait waited for
+__device__ __forceinline__ void tm_ld_tie(float* v) {
+  asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+               "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+               "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+               "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tm_ld_wait16(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
                :
                : "memory");
 }
 __device__ __forceinline__ void tm_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Shared-memory descriptors of 128-byte swizzled operands, in units of 16 bytes.  K and Q (rows of 64 elements along the
-// summed axis): groups of 8 rows 1024 bytes apart.  V (the summed axis, keys, runs over the rows): 8-key groups 1024 bytes
-// apart, blocks of 64 columns one chunk of 128 rows apart.
-__device__ __forceinline__ uint64_t desc_rows(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-__device__ __forceinline__ uint64_t desc_cols(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)((kKeys * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)2 << 61);
-}
+// Shared-memory descriptors of 128-byte swizzled operands, in units of 16 bytes: low words (address, leading offset); the
+// high word is the stride offset (groups of 8 rows 1024 bytes apart), the version 1 and the swizzle mode 2.  K and Q (rows
+// of 64 elements along the summed axis) have no leading offset (1); of V (the summed axis, keys, runs over the rows) it is
+// the distance of blocks of 64 columns, one chunk of 128 rows.
+__device__ __forceinline__ uint32_t desc_rows(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_cols(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | ((uint32_t)((kKeys * 128) >> 4) << 16); }
 // Instruction descriptor: float32 accumulator, operands bf16 or f16, M = 128.
 __device__ __forceinline__ uint32_t instr_desc(bool bf16, int n, bool b_by_columns) {
   const uint32_t f = bf16 ? 1u : 0u;
@@ -197,6 +233,35 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {   // a NaN stays
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// 2^x of two numbers on the FMA and integer pipes: x = i + f with |f| <= 1/2, 2^f by the polynomial of degree 5 of least
+// largest relative error (7.5e-8, 2.2e-7 with the roundings; coefficients by a Remez exchange), times 2^i.  Zero below
+// 2^-126 (i = -127 makes the factor's bits zero), NaN for NaN; x up to 127.
+__device__ __forceinline__ float2 ex2_poly(float2 x) {
+  const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);
+  x = make_float2(max_nan(x.x, -127.f), max_nan(x.y, -127.f));
+  const float2 t = add2(x, magic);                                          // i in the low bits
+  const float2 f = fma2(add2(t, unmagic), make_float2(-1.f, -1.f), x);
+  float2 y = fma2(f, make_float2(1.3276472454890609e-3f, 1.3276472454890609e-3f), make_float2(9.675540961325169e-3f, 9.675540961325169e-3f));
+  y = fma2(y, f, make_float2(5.550713092088699e-2f, 5.550713092088699e-2f));
+  y = fma2(y, f, make_float2(2.4022120237350464e-1f, 2.4022120237350464e-1f));
+  y = fma2(y, f, make_float2(6.931469440460205e-1f, 6.931469440460205e-1f));
+  y = fma2(y, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
+  return mul2(y, make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000)));
+}
+
 template <bool BF> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
   if (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -210,18 +275,31 @@ template <bool BF> __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t
 }
 
 __device__ __forceinline__ bool aborted(const TcShared* sh) { return *reinterpret_cast<const volatile int*>(&sh->abort_flag) != 0; }
-// Bounded wait for a phase of a barrier; gives up too when another warp has.
-__device__ __forceinline__ bool tc_wait(TcShared* sh, uint64_t* bar, uint32_t parity) {
-  if (mbar_test(bar, parity, kSuspendNs)) return true;
-  const long long t0 = clock64();
-  for (;;) {
-    if (mbar_test(bar, parity, kSuspendNs)) return true;
-    if (aborted(sh) || clock64() - t0 > kWaitCycles) return false;
-  }
+// One poll of a barrier's phase in the form without a time hint: the hardware parks the thread until the phase completes
+// or a time of its own has passed.  (With a hint the compiler makes a loop of naps of it, and a waiting warp wakes late.)
+__device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
-__device__ __forceinline__ void give_up(TcShared* sh, const TcParams& p, int b) {
+// Bounded wait of a whole warp (or, WARP false, of a single thread) for a phase of a barrier.  2^24 polls are a second or
+// much more, which no healthy run comes near.
+constexpr int kPolls = 1 << 24;
+template <bool WARP> __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+  for (int n = kPolls; n > 0; --n) {
+    const bool got = poll(bar, parity);
+    if (WARP ? __all_sync(kFullMask, got) : got) return true;
+  }
+  return false;
+}
+__device__ __noinline__ void give_up(TcShared* sh, int* status) {
   *reinterpret_cast<volatile int*>(&sh->abort_flag) = 1;
-  if (p.d.req_status && b < p.d.B) atomicOr(p.d.req_status + b, SPECSTEER_REQ_TIMEOUT);
+  if (status) atomicOr(status, SPECSTEER_REQ_TIMEOUT);
 }
 
 // ---- units ----------------------------------------------------------------------------------------------------------
@@ -250,11 +328,12 @@ __device__ __forceinline__ Unit make_unit(const TcParams& p, const AttnRequest& 
 __device__ __forceinline__ long long unit_cost(const Unit& x) { return (long long)x.nt * (x.two ? 2 : 1) + kUnitCost; }
 // The key tile at which a cut `pos` into the unit falls.
 __device__ __forceinline__ int cut_tile(const Unit& x, long long pos) {
-  return pos <= kUnitCost ? 0 : (int)min((long long)x.nt, (pos - kUnitCost) / (x.two ? 2 : 1));
+  return pos <= kUnitCost ? 0 : (int)min((long long)x.nt, (pos - kUnitCost) >> (x.two ? 1 : 0));
 }
 __device__ __forceinline__ int n_units(const TcParams& p, const AttnRequest& rq) { return (rq.n + 2 * p.tile_tok - 1) / (2 * p.tile_tok); }
 __device__ __forceinline__ long long head_cost(const TcParams& p, const AttnRequest& rq) {
   long long c = 0;
+#pragma unroll 1
   for (int u = 0, nu = n_units(p, rq); u < nu; ++u) c += unit_cost(make_unit(p, rq, u));
   return c;
 }
@@ -265,39 +344,41 @@ struct Walk {
   long long end;     // where the range ends, from the beginning of the unit
   AttnRequest rq;
   Unit x;
-  __device__ __forceinline__ void begin(const TcParams& p, const TcShared* sh) {
+  __device__ __forceinline__ void begin(const TcShared* sh) {
     b = sh->start_b; hk = sh->start_hk; u = sh->start_u; off = sh->start_off;
     end = sh->end;
     index = 0;
     take = 0;
-    if (end > 0) load(p);
   }
   __device__ __forceinline__ void load(const TcParams& p) {
+    take = 0;
+    if (end <= 0) return;
     rq = attn_request(p.d, b);
     x = make_unit(p, rq, u);
     take = (end >= unit_cost(x) ? x.nt : cut_tile(x, end)) - off;
   }
-  __device__ __forceinline__ bool more() const { return take > 0; }
-  __device__ __forceinline__ bool starts() const { return off == 0; }
-  __device__ __forceinline__ bool ends() const { return off + take == x.nt; }
   __device__ __forceinline__ void next(const TcParams& p) {
     end -= unit_cost(x);
-    take = 0;
     ++index;
-    if (end <= 0) return;
     off = 0;
+    if (end <= 0) return;
     if (++u == n_units(p, rq)) {
       u = 0;
       if (++hk == p.d.Hkv) {
         hk = 0;
-        do { ++b; rq = attn_request(p.d, b); } while (rq.n == 0 && b + 1 < p.d.B);   // end > 0: a request with rows follows
+        do { ++b; } while (b + 1 < p.d.B && attn_request(p.d, b).n == 0);   // end > 0: a request with rows follows
       }
     }
-    load(p);
   }
-  // Ring items of a piece: the keys of the first `ahead` tiles, then per tile its values and the keys `ahead` tiles on.
-  __device__ __forceinline__ int ahead() const { return min(x.two ? 1 : 2, take); }
-  __device__ __forceinline__ int item_of_v(int t) const { return ahead() + min(t, take - ahead()) + t; }
+  __device__ __forceinline__ void publish(Piece* q) const {
+    q->b = b; q->hk = hk; q->u = u;
+    q->row0 = rq.row0; q->n = rq.n; q->kv = rq.kv;
+    q->tok0 = x.tok0; q->tok1 = x.tok1; q->two = x.two;
+    q->hi_first = x.hi_first; q->lo_last = x.lo_last;
+    q->first = x.t0 + off; q->take = take;
+    q->starts = off == 0; q->ends = off + take == x.nt;
+    q->index = index;
+  }
 };
 
 // sums over the block of one value a thread; returns the exclusive sum, *total the sum
@@ -336,10 +417,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     for (int i = 0; i < L::kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 1);
-      mbar_init(&sh->s_full[i], 1); mbar_init(&sh->p_full[i], 4); mbar_init(&sh->pv_done[i], 1);
-      mbar_init(&sh->group[i], 4);
+      mbar_init(&sh->s_full[i], 1); mbar_init(&sh->p_full[i][0], 4); mbar_init(&sh->p_full[i][1], 4);
+      mbar_init(&sh->group[i], kSoftmaxWarps / 2);
     }
-    mbar_init(&sh->both, 8);
+    for (int i = 0; i < kPieces; ++i) { mbar_init(&sh->piece_full[i], 1); mbar_init(&sh->piece_empty[i], kSoftmaxWarps + 1); }
+    mbar_init(&sh->both, kSoftmaxWarps);
+    mbar_init(&sh->o_full, 1);
     mbar_init(&sh->drain, 1);
     sh->abort_flag = 0;
     sh->nonfinite = 0;
@@ -352,6 +435,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   {
     const int per = (p.d.B + kTcThreads - 1) / kTcThreads, b_lo = min(p.d.B, tid * per), b_hi = min(p.d.B, b_lo + per);
     long long mine = 0, total;
+#pragma unroll 1
     for (int b = b_lo; b < b_hi; ++b) {
       const AttnRequest rq = attn_request(p.d, b);
       if (rq.bad && blockIdx.x == 0 && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_LEN);
@@ -361,6 +445,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const long long s0 = total * blockIdx.x / gridDim.x, s1 = total * (blockIdx.x + 1) / gridDim.x;
     if (s1 > s0 && s0 >= before && s0 < before + mine) {
       long long rem = s0 - before;
+#pragma unroll 1
       for (int b = b_lo; b < b_hi; ++b) {
         const AttnRequest rq = attn_request(p.d, b);
         if (rq.n == 0) continue;
@@ -368,6 +453,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (rem >= per_head * p.d.Hkv) { rem -= per_head * p.d.Hkv; continue; }
         const int hk = (int)(rem / per_head);
         rem -= hk * per_head;
+#pragma unroll 1
         for (int u = 0;; ++u) {
           const Unit x = make_unit(p, rq, u);
           if (rem >= unit_cost(x)) { rem -= unit_cost(x); continue; }
@@ -384,39 +470,36 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sh->tmem_slot);
 
-  Walk w;
-  w.begin(p, sh);
-
   if (warp == kProducerWarp) {
-    // ================= TMA =================
+    // ================= work list and TMA =================
     const int chunks = DP / 64;
     const int box = lane / chunks, chunk = lane % chunks;
     const bool loads = box < p.boxes;
-    const uint32_t lane_off = (uint32_t)chunk * (kKeys * 128) + (uint32_t)box * p.page_rows * 128;
-    int item = 0, qi = 0, tiles = 0;
+    const uint32_t lane_off = smem0 + L::kRing + (uint32_t)chunk * (kKeys * 128) + (uint32_t)box * p.page_rows * 128;
+    int item = 0, st = 0, qi = 0, tiles = 0;   // st: stage of the item
+    uint32_t st_phase = 1;
     bool ok = true;
+    Walk w;
+    w.begin(sh);
+    const int* table = nullptr;
     // page of this lane's box of key tile t: the id, or n_pages (a coordinate outside, which reads zeros) for none
     auto page_of = [&](int t) -> int {
       const int key = t * kKeys + box * p.page_rows;
       int page = p.d.n_pages;
-      if (loads && key < w.rq.kv) page = __ldg(p.d.block_table + (long long)w.b * p.d.ld_table + key / p.d.page_size);
+      if (loads && key < w.rq.kv) page = __ldg(table + (p.boxes > 1 ? t * p.boxes + box : t / p.page_tiles));
       return page;
     };
-    auto stage_free = [&](int it) {
-      const bool got = tc_wait(sh, &sh->empty[it % L::kStages], (uint32_t)((it / L::kStages) & 1) ^ 1u);
-      ok = __all_sync(kFullMask, got);
-    };
     auto load_tile = [&](const CUtensorMap* tm, int t, int page) {
-      const int st = item % L::kStages;
-      stage_free(item);
+      if (!ok) return;
+      ok = tc_wait<true>(&sh->empty[st], st_phase);
       if (!ok) return;
       if (lane == 0) mbar_arrive_expect_tx(&sh->full[st], L::kStageBytes);
       __syncwarp();
-      if (loads) {
-        const int pg = (page < 0 || page >= p.d.n_pages) ? p.d.n_pages : page;
-        tma_4d(smem0 + L::kRing + st * L::kStageBytes + lane_off, tm, chunk * 64, (t * kKeys) % p.d.page_size * (p.d.page_size >= kKeys), w.hk, pg, &sh->full[st]);
-      }
+      if (loads)
+        tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, p.page_tiles > 1 ? t % p.page_tiles * kKeys : 0, w.hk,
+               (page < 0 || page >= p.d.n_pages) ? p.d.n_pages : page, &sh->full[st]);
       ++item;
+      if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
     };
     auto load_k = [&](int t, int page) {
       const bool outside = loads && t * kKeys + box * p.page_rows < w.rq.kv && (page < 0 || page >= p.d.n_pages);
@@ -433,228 +516,302 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       ++tiles;
       load_tile(&tm_k, t, page);
     };
-    for (; w.more() && ok; w.next(p)) {
+    int pc = 0;
+#pragma unroll 1
+    for (;; ++pc) {
+      w.load(p);
+      ok = tc_wait<true>(&sh->piece_empty[pc % kPieces], (uint32_t)((pc / kPieces) & 1) ^ 1u);
+      if (!ok) break;
+      if (lane == 0) {
+        if (w.take > 0) w.publish(&sh->piece[pc % kPieces]);
+        else sh->piece[pc % kPieces].take = 0;
+        mbar_arrive(&sh->piece_full[pc % kPieces]);
+      }
+      __syncwarp();
+      if (w.take <= 0) break;
+      table = p.d.block_table + (long long)w.b * p.d.ld_table;
       const int n_q = w.x.two ? 2 : 1;
+#pragma unroll 1
       for (int s = 0; s < n_q && ok; ++s, ++qi) {
         const int slot = qi & 1;
-        const bool got = tc_wait(sh, &sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
-        ok = __all_sync(kFullMask, got);
+        ok = tc_wait<true>(&sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
         if (!ok) break;
         const int tok = w.x.tok0 + s * p.tile_tok, cnt = min(p.tile_tok, w.x.tok1 - tok);
         const int nb = (cnt + p.box_tok - 1) / p.box_tok;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
-          for (int i = 0; i < nb; ++i)
-            for (int ch = 0; ch < chunks; ++ch)
-              tma_3d(smem0 + slot * L::kQBytes + ch * (128 * 128) + i * p.box_rows * 128, &tm_q, ch * 64, w.hk * p.G, w.rq.row0 + tok + i * p.box_tok, &sh->q_full[slot]);
-        }
+        if (lane == 0) mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
         __syncwarp();
+        if (box < nb)
+          tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + box * p.box_rows * 128, &tm_q, chunk * 64, w.hk * p.G, w.rq.row0 + tok + box * p.box_tok, &sh->q_full[slot]);
+      }
+      const int first = w.x.t0 + w.off, take = w.take, ahead = min(w.x.two ? 1 : 2, take);
+      int pg0 = page_of(first), pg1 = take > 1 ? page_of(first + 1) : 0, pg2 = take > 2 ? page_of(first + 2) : 0;
+#pragma unroll 1
+      for (int t = -ahead; t < take && ok; ++t) {
+        // values of tile t, then keys of tile t + ahead
+        const int pg3 = t >= 0 && t + 3 < take ? page_of(first + t + 3) : 0;
+        if (t >= 0) load_tile(&tm_v, first + t, pg0);
+        if (t + ahead < take && ok) load_k(first + t + ahead, t + ahead == 0 ? pg0 : (t + ahead == 1 && t < 0) || ahead == 1 ? pg1 : pg2);
+        if (t >= 0) { pg0 = pg1; pg1 = pg2; pg2 = pg3; }
       }
       if (!ok) break;
-      const int first = w.x.t0 + w.off, ahead = w.ahead();
-      int pg0 = page_of(first), pg1 = w.take > 1 ? page_of(first + 1) : 0, pg2 = w.take > 2 ? page_of(first + 2) : 0;
-      load_k(first, pg0);
-      if (ahead == 2 && ok) load_k(first + 1, pg1);
-      for (int t = 0; t < w.take && ok; ++t) {
-        const int pg3 = t + 3 < w.take ? page_of(first + t + 3) : 0;
-        load_tile(&tm_v, first + t, pg0);
-        if (t + ahead < w.take && ok) load_k(first + t + ahead, ahead == 2 ? pg2 : pg1);
-        pg0 = pg1; pg1 = pg2; pg2 = pg3;
-      }
+      w.next(p);
     }
-    if (!ok) {
-      if (lane == 0) {
-        give_up(sh, p, w.b);
-        // copies already issued may still be landing: wait for them (bounded) before the CTA exits
-        for (int i = item > L::kStages ? item - L::kStages : 0; i < item; ++i) mbar_wait(&sh->full[i % L::kStages], (uint32_t)((i / L::kStages) & 1));
-        for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) mbar_wait(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1));
-      }
+    if (!ok && lane == 0) {
+      give_up(sh, p.d.req_status ? p.d.req_status + w.b : nullptr);
+      // copies already issued may still be landing: wait for them (bounded) before the CTA exits
+      for (int i = item > L::kStages ? item - L::kStages : 0; i < item; ++i) tc_wait<false>(&sh->full[i % L::kStages], (uint32_t)((i / L::kStages) & 1));
+      for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_wait<false>(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1));
     }
   } else if (warp == kMmaWarp) {
     // ================= tensor-core issuer =================
-    if (lane == 0) {
-      const uint32_t id_qk = instr_desc(BF, kKeys, false), id_pv = instr_desc(BF, DP, true);
-      int item = 0, qi = 0;
-      int n_p[2] = {0, 0};   // weights taken from each stream so far
-      bool ok = true;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
+    // The whole warp runs the loop, so that addresses and descriptors stay in uniform registers.
+    // All columns were allocated, so tensor memory begins at column 0.
+    constexpr uint32_t t_base = 0;
+    const uint32_t id_qk = instr_desc(BF, kKeys, false), id_pv = instr_desc(BF, DP, true);
+    int st = 0, qi = 0, pc = 0, b = 0;   // st: stage of the next ring item
+    uint32_t st_phase = 0, p_phase = 0;  // p_phase: bit s, of the weights of stream s
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = tc_wait<true>(bar, parity);
+      fence_after();
+    };
+    // the next ring item has landed; its stage
+    auto item = [&]() -> int {
+      wait(&sh->full[st], st_phase);
+      const int got = st;
+      if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
+      return got;
+    };
+    // Scores of stream s.  The commit also says that the stream's product with the values before it is complete.
+    auto scores = [&](int s, int slot, int stage, bool last_use) {
+      if (!ok) return;
+      const uint32_t a = desc_rows(smem0 + slot * L::kQBytes), b = desc_rows(smem0 + L::kRing + stage * L::kStageBytes);
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        const uint32_t step = (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2);
+        mma_ss(t_base + s * 128, a + step, b + step, id_qk, k != 0);
+      }
+      mma_commit(&sh->s_full[s]);
+      if (last_use) mma_commit(&sh->empty[stage]);
+    };
+    auto values = [&](int s, int stage, bool accumulate, bool last_use) {
+      const uint32_t b = desc_cols(smem0 + L::kRing + stage * L::kStageBytes);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        wait(&sh->p_full[s][h], (p_phase >> s) & 1u);
         if (!ok) return;
-        if (!tc_wait(sh, bar, parity)) { give_up(sh, p, w.b); ok = false; return; }
-        fence_after();
-      };
-      auto wait_item = [&](int it) { wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1)); };
-      auto stage_addr = [&](int it) { return smem0 + L::kRing + (it % L::kStages) * L::kStageBytes; };
-      auto scores = [&](int s, int slot, int it) {
-        const uint64_t a = desc_rows(smem0 + slot * L::kQBytes), b = desc_rows(stage_addr(it));
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k) {
-          const uint64_t step = (uint64_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2);
-          mma_ss(tmem + s * 128, a + step, b + step, id_qk, k != 0);
-        }
-        mma_commit(&sh->s_full[s]);
-      };
-      auto values = [&](int s, int it, bool accumulate) {
-        const uint64_t b = desc_cols(stage_addr(it));
-#pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k)
-          mma_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, b + (uint64_t)(k * (2048 >> 4)), id_pv, accumulate || k != 0);
-        mma_commit(&sh->pv_done[s]);
-      };
-      for (; w.more() && ok; w.next(p)) {
-        const int take = w.take, ahead = w.ahead();
-        const int q0 = qi & 1, q1 = (qi + 1) & 1;
-        wait(&sh->q_full[q0], (uint32_t)((qi >> 1) & 1));
-        if (w.x.two) wait(&sh->q_full[q1], (uint32_t)(((qi + 1) >> 1) & 1));
-        // keys of the first tiles
-        wait_item(item);
-        if (!ok) break;
-        scores(0, q0, item);
-        if (w.x.two) scores(1, q1, item);
-        mma_commit(&sh->empty[item % L::kStages]);
-        ++item;
-        if (ahead == 2) {
-          wait_item(item);
-          if (!ok) break;
-          scores(1, q0, item);
-          mma_commit(&sh->empty[item % L::kStages]);
-          ++item;
-        }
-        for (int t = 0; t < take && ok; ++t) {
-          const int v = item++;
-          const bool next_k = t + ahead < take;
-          const int k = next_k ? item++ : 0;
-          if (w.x.two) {
-            wait(&sh->p_full[0], (uint32_t)(n_p[0]++ & 1));
-            wait_item(v);
-            if (!ok) break;
-            values(0, v, t > 0);
-            if (next_k) { wait_item(k); if (!ok) break; scores(0, q0, k); }
-            wait(&sh->p_full[1], (uint32_t)(n_p[1]++ & 1));
-            if (!ok) break;
-            values(1, v, t > 0);
-            mma_commit(&sh->empty[v % L::kStages]);
-            if (next_k) { scores(1, q1, k); mma_commit(&sh->empty[k % L::kStages]); }
-          } else {
-            const int s = t & 1;
-            wait(&sh->p_full[s], (uint32_t)(n_p[s]++ & 1));
-            wait_item(v);
-            if (!ok) break;
-            values(s, v, t > 1);
-            mma_commit(&sh->empty[v % L::kStages]);
-            if (next_k) {
-              wait_item(k);
-              if (!ok) break;
-              scores(s, q0, k);
-              mma_commit(&sh->empty[k % L::kStages]);
-            }
+        for (int k = h * 4; k < h * 4 + 4; ++k)
+          mma_ts(t_base + 256 + s * 128, t_base + s * 128 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, k != 0 || accumulate);
+      }
+      if (last_use) mma_commit(&sh->empty[stage]);
+      p_phase ^= 1u << s;
+    };
+#pragma unroll 1
+    for (;; ++pc) {
+      wait(&sh->piece_full[pc % kPieces], (uint32_t)((pc / kPieces) & 1));
+      if (!ok) break;
+      const Piece* q = &sh->piece[pc % kPieces];
+      // (through a reduction, whose result the compiler knows to be the same in the whole warp)
+      const int take = __reduce_max_sync(kFullMask, q->take), two = __reduce_max_sync(kFullMask, q->two), ahead = min(two ? 1 : 2, take);
+      b = q->b;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
+      if (take <= 0) break;
+      const int q0 = qi & 1, q1 = two ? q0 ^ 1 : q0;
+      wait(&sh->q_full[q0], (uint32_t)((qi >> 1) & 1));
+      if (two) wait(&sh->q_full[q1], (uint32_t)(((qi + 1) >> 1) & 1));
+      // t < 0: keys of the first tiles only
+#pragma unroll 1
+      for (int t = -ahead; t < take && ok; ++t) {
+        const bool next_k = t + ahead < take;
+        const int v = t >= 0 ? item() : 0;
+        if (two) {
+          if (t >= 0) values(0, v, t > 0, false);
+          const int k = next_k ? item() : 0;
+          if (next_k) scores(0, q0, k, false);
+          if (t >= 0) values(1, v, t > 0, true);
+          if (next_k) scores(1, q1, k, true);
+        } else {
+          if (t >= 0) values(t & 1, v, t > 1, true);
+          if (next_k) {
+            const int k = item();
+            scores((t + ahead) & 1, q0, k, true);
           }
         }
-        if (!ok) break;
-        mma_commit(&sh->q_empty[q0]);
-        if (w.x.two) mma_commit(&sh->q_empty[q1]);
-        qi += w.x.two ? 2 : 1;
       }
-      if (!ok) {   // let everything issued finish before tensor memory is given back
-        mma_commit(&sh->drain);
-        mbar_wait(&sh->drain, 0);
-      }
+      if (!ok) break;
+      mma_commit(&sh->o_full);
+      mma_commit(&sh->q_empty[q0]);
+      if (two) mma_commit(&sh->q_empty[q1]);
+      qi += two ? 2 : 1;
+    }
+    if (!ok) {   // let everything issued finish before tensor memory is given back
+      if (lane == 0) give_up(sh, p.d.req_status ? p.d.req_status + b : nullptr);
+      __syncwarp();
+      mma_commit(&sh->drain);
+      tc_wait<true>(&sh->drain, 0);
     }
   } else {
-    // ================= softmax: one row a thread =================
-    const int s = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    // ================= softmax: kSplit threads a row =================
+    const int s = warp / (4 * kSplit), half = (warp >> 2) % kSplit, quarter = warp & 3, r = quarter * 32 + lane;
+    constexpr int kCols = kKeys / kSplit;      // scores of a row that a thread has
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
     const int r_tok = r / p.G, r_head = r - r_tok * p.G;
+    const int pair_id = 1 + s * 4 + quarter;   // hardware barrier of the two warps that share 32 rows
     const float c = p.c;
-    int done[2] = {0, 0};        // tiles of each stream so far
-    int item0 = 0, tiles0 = 0, n_group = 0, n_both = 0;
+    uint32_t s_phase = 0;
+    uint32_t group_phase = 0, both_phase = 0;
+    int item0 = 0, tiles0 = 0, pc = 0, b = 0;
     bool ok = true;
+    // Gives up: the partner warp may stand at the pair's barrier now or come there once more; it is let through and then
+    // sees the abort flag.
+    auto fail = [&]() {
+      ok = false;
+      if (lane == 0) give_up(sh, p.d.req_status ? p.d.req_status + b : nullptr);
+      __threadfence_block();
+      __syncwarp();
+      if (kSplit > 1) asm volatile("barrier.cta.arrive %0, 64;" ::"r"(pair_id) : "memory");
+    };
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (!ok) return;
-      const bool got = tc_wait(sh, bar, parity);
-      ok = __all_sync(kFullMask, got);
-      if (!ok && lane == 0) give_up(sh, p, w.b);
+      if (ok && !tc_wait<true>(bar, parity)) fail();
       fence_after();
     };
-    // barriers among the softmax warps: of this group, of both groups (bounded like every wait)
+    auto pair = [&]() {
+      if (kSplit == 1 || !ok) return;
+      asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_id) : "memory");
+      ok = __all_sync(kFullMask, !aborted(sh));
+    };
+    // barriers among the softmax warps: of this stream, of both (bounded like every wait)
     auto meet = [&](bool all) {
+      if (!ok) return;
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(all ? &sh->both : &sh->group[s]);
-      if (all) wait(&sh->both, (uint32_t)(n_both++ & 1));
-      else wait(&sh->group[s], (uint32_t)(n_group++ & 1));
+      wait(all ? &sh->both : &sh->group[s], all ? both_phase : group_phase);
+      if (all) both_phase ^= 1u;
+      else group_phase ^= 1u;
     };
     if (tid == 0) {
       int* h = p.head + blockIdx.x * 8;
       h[0] = -1;   // slot of a unit that begins in this CTA and goes on in the next
       h[1] = 0;    // its part of a unit that began in a CTA before: 0 none, 1 the end, 2 some in between
     }
-    for (; w.more() && ok; w.next(p)) {
-      const Unit& x = w.x;
-      const int tok = x.tok0 + (x.two ? s * p.tile_tok : 0) + r_tok;
+#pragma unroll 1
+    for (; ok; ++pc) {
+      wait(&sh->piece_full[pc % kPieces], (uint32_t)((pc / kPieces) & 1));
+      if (!ok) break;
+      const Piece& x = sh->piece[pc % kPieces];
+      const int take = x.take, two = x.two, first = x.first;
+      if (take <= 0) break;
+      b = x.b;
+      const int tok = x.tok0 + (two ? s * p.tile_tok : 0) + r_tok;
       const bool live = r_tok < p.tile_tok && tok < x.tok1;
       const bool warp_live = __any_sync(kFullMask, live);
       int lo = 0, hi = 0;
-      if (live) attn_span(p.d, w.rq, tok, lo, hi);
-      float m = kNegInf, l = 0.f;       // reference (raw score) and sum
-      int mine = 0;                     // tiles this stream has had in this piece
-      for (int t = x.two ? 0 : s; t < w.take && ok; t += x.two ? 1 : 2, ++mine) {
-        const int k0 = (x.t0 + w.off + t) * kKeys;
-        wait(&sh->s_full[s], (uint32_t)(done[s] + mine) & 1u);
+      if (live) {
+        hi = x.kv - x.n + tok + 1;
+        lo = p.d.window > 0 && hi > p.d.window ? hi - p.d.window : 0;
+      }
+      const int hi_first = x.hi_first, lo_last = x.lo_last;
+      float m = kNegInf, l = 0.f;       // reference (raw score, the same in a row's threads), sum over this thread's keys
+      const int step = two ? 1 : 2, t_from = two ? 0 : s;
+#pragma unroll 1
+      for (int t = t_from; t < take; t += step) {
+        const int k0 = (first + t) * kKeys;
+        wait(&sh->s_full[s], s_phase);
+        s_phase ^= 1u;
         if (!ok) break;
         const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(tiles0 + t) & 15]);
-        const bool edge = k0 + kKeys > x.hi_first || k0 < x.lo_last || bad != 0;
-        if (warp_live) {
-          // The scores are read from tensor memory twice, 32 columns at a time, rather than kept in 128 registers, and the
-          // loops stay loops: unrolled, the masked and plain variants overran the instruction cache.
-          const int a = lo - k0, e = hi - k0;
-          // the columns of [j0, j0 + 32) that the row sees, as bits
-          auto seen = [&](int j0) -> uint32_t {
-            const int from = max(a - j0, 0), to = min(e - j0, 32);
-            uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
-            if (bad) {
-              for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
-                if ((bad >> ((j0 + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
-            }
-            return keep;
-          };
-          auto mask = [&](float* v, uint32_t keep) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = (keep & (1u << j)) ? v[j] : kNegInf;
-          };
-          float va[32], vb[32];
-          float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
-          auto take_max = [&](const float* v) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
-            }
-          };
+        const bool edge = k0 + kKeys > hi_first || k0 < lo_last || bad != 0;
+        if (edge) {
+          // Values of keys that some row of the unit does not see: those that nobody sees (behind the last key, on a
+          // page outside the pool) become zero; an infinity or NaN among the others is taken out here, where it would
+          // reach rows with weight 0, and added in the epilogue to the rows that see it.
+          const int it = item0 + x.item_of_v(t);
+          wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
+          if (!ok) break;
+          unsigned char* vt = smem_raw + L::kRing + (it % L::kStages) * L::kStageBytes;
+          const int from = bad ? kKeys : min(kKeys, max(0, lo_last - k0)), to = bad ? kKeys : min(kKeys, max(from, hi_first - k0));
+          const int n_vec = (from + (kKeys - to)) * (DP / 8);          // of keys [0, from) and [to, 128)
+          const int kv = x.kv;
 #pragma unroll 1
-          for (int j0 = 0; j0 < kKeys; j0 += 64) {
-            tm_ld32(t_s + j0, va);
-            tm_ld32(t_s + j0 + 32, vb);
-            tm_ld_wait(va, vb);
-            if (edge) { mask(va, seen(j0)); mask(vb, seen(j0 + 32)); }
-            take_max(va);
-            take_max(vb);
+          for (int pass = 0; pass < 2; ++pass) {
+            bool found = false;
+#pragma unroll 1
+            for (int e = tid % (128 * kSplit); e < n_vec; e += 128 * kSplit) {
+              const int jj = e / (DP / 8), vec = e % (DP / 8), j = jj < from ? jj : jj - from + to;
+              uint4* at = reinterpret_cast<uint4*>(vt + (vec >> 3) * (kKeys * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
+              const bool nobody = k0 + j >= kv || ((bad >> (j >> p.page_shift)) & 1u);
+              uint4 y = *at;
+              uint32_t n0 = 0xffffffffu, n1 = n0, n2 = n0, n3 = n0;
+              if (!nobody) {
+                n0 = nonfinite_halves<BF>(y.x); n1 = nonfinite_halves<BF>(y.y); n2 = nonfinite_halves<BF>(y.z); n3 = nonfinite_halves<BF>(y.w);
+                found = found || (n0 | n1 | n2 | n3);
+              }
+              if (pass && (n0 | n1 | n2 | n3)) *at = make_uint4(y.x & ~n0, y.y & ~n1, y.z & ~n2, y.w & ~n3);
+            }
+            if (pass == 0) {
+              if (found) atomicOr(&sh->nonfinite, bad ? 3 : 1);
+              meet(two);   // everybody who has to has seen them before they go
+            }
           }
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          if (!ok) break;
+          fence_async_proxy();
+        }
+        if (warp_live) {
+          float v[kCols];
+#pragma unroll
+          for (int i = 0; i < kCols; i += 32) tm_ld32(t_s + half * kCols + i, v + i);
+          tm_ld_wait(v);
+#pragma unroll
+          for (int i = 32; i < kCols; i += 32) tm_ld_tie(v + i);
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < kCols; i += 32) {
+              // the columns of 32 that the row sees, as bits
+              const int j0 = half * kCols + i, from = max(lo - k0 - j0, 0), to = min(hi - k0 - j0, 32);
+              uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
+              if (bad) {
+#pragma unroll 1
+                for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
+                  if ((bad >> ((j0 + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
+              }
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[i + j] = (keep & (1u << j)) ? v[i + j] : kNegInf;
+            }
+          }
+          float mx[8] = {kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf};
+#pragma unroll
+          for (int j = 0; j < kCols; j += 16) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
+          }
+          float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
+          if (kSplit > 1) {
+            // The maxima of a row's two threads.  A slot is written again one tile later, after scores that were formed
+            // after both threads' weights of this tile, hence after the reads here.  The barrier also says that both have
+            // their scores in registers, whose place the weights take.
+            sh->exch[s][half][r] = top;
+            pair();
+            if (!ok) break;
+            top = fmaxf(top, sh->exch[s][half ^ 1][r]);
+          }
           const bool raise = top > m && (m == kNegInf || (top - m) * c > kGrow);
           if (__any_sync(kFullMask, raise)) {
             const float alpha = !raise ? 1.f : m == kNegInf ? 0.f : ex2((m - top) * c);
-            if (mine > 0 && __any_sync(kFullMask, raise && m != kNegInf)) {
-              wait(&sh->pv_done[s], (uint32_t)(done[s] + mine - 1) & 1u);
-              if (!ok) break;
+            if (t > t_from && __any_sync(kFullMask, raise && m != kNegInf)) {
+              // the sums are at rest: the product before was complete when these scores were
+              const int j_lo = half * (DP / kSplit);
 #pragma unroll 1
-              for (int j0 = 0; j0 < DP; j0 += 32) {
-                float o[32];
-                tm_ld32(t_o + j0, o);
-                tm_ld_wait(o);
+              for (int j0 = j_lo; j0 < j_lo + DP / kSplit; j0 += 16) {
+                float o[16];
+                tm_ld16(t_o + j0, o);
+                tm_ld_wait16(o);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] *= alpha;
-                tm_st32(t_o + j0, reinterpret_cast<const uint32_t*>(o));
+                for (int j = 0; j < 16; ++j) o[j] *= alpha;
+                tm_st16(t_o + j0, reinterpret_cast<const uint32_t*>(o));
               }
             }
             l *= alpha;
@@ -662,134 +819,108 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
           const float ref = m == kNegInf ? 0.f : m * c;
           const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          // Weights of 32 columns; they take 16 columns of the scores' place, all of them read by then.  They go to the
-          // second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
-          auto weigh = [&](const float* v, int j0) {
+          float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          // The weights go to the second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
+#pragma unroll
+          for (int i = 0; i < kCols; i += 32) {
             uint32_t w16[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-              const float2 x2 = fma2(make_float2(v[2 * j], v[2 * j + 1]), c2, ref2);
-              const float2 y = make_float2(ex2(x2.x), ex2(x2.y));
-              sum[j & 1] = add2(sum[j & 1], y);
+              const float2 x2 = fma2(make_float2(v[i + 2 * j], v[i + 2 * j + 1]), c2, ref2);
+              const bool poly = ((i / 2 + j) * kPolyPairs) % 32 < kPolyPairs;
+              const float2 y = poly ? ex2_poly(x2) : make_float2(ex2(x2.x), ex2(x2.y));
+              sum[j & 3] = add2(sum[j & 3], y);
               w16[j] = pack2<BF>(y.x, y.y);
             }
-            tm_st16(t_s + j0 / 2, w16);
-          };
-#pragma unroll 1
-          for (int j0 = 0; j0 < kKeys; j0 += 64) {
-            tm_ld32(t_s + j0, va);
-            tm_ld32(t_s + j0 + 32, vb);
-            tm_ld_wait(va, vb);
-            if (edge) { mask(va, seen(j0)); mask(vb, seen(j0 + 32)); }
-            weigh(va, j0);
-            weigh(vb, j0 + 32);
+            tm_st16(t_s + (half * kCols + i) / 2, w16);
+            if (i % 64 == 32) {
+              tm_st_wait();
+              fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh->p_full[s][kSplit == 1 ? i / 64 : half]);
+            }
           }
-          sum[0] = add2(sum[0], sum[1]);
+          sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
           l += sum[0].x + sum[0].y;
-          tm_st_wait();
-        }
-        if (edge) {
-          // Values of keys that some row of the unit does not see: those that nobody sees (behind the last key, on a
-          // page outside the pool) become zero; an infinity or NaN among the others is taken out here, where it would
-          // reach rows with weight 0, and added in the epilogue to the rows that see it.
-          const int it = item0 + w.item_of_v(t);
-          wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
-          if (!ok) break;
-          unsigned char* vt = smem_raw + L::kRing + (it % L::kStages) * L::kStageBytes;
-          const int from = bad ? kKeys : min(kKeys, max(0, x.lo_last - k0)), to = bad ? kKeys : min(kKeys, max(from, x.hi_first - k0));
-          const int n_keys = from + (kKeys - to);          // keys [0, from) and [to, 128)
-          const int me = tid & 127;
-#pragma unroll 1
-          for (int pass = 0; pass < 2 && ok; ++pass) {
-            bool found = false;
-#pragma unroll 1
-            for (int e = me; e < n_keys * (DP / 8); e += 128) {
-              const int jj = e / (DP / 8), vec = e % (DP / 8), j = jj < from ? jj : jj - from + to;
-              uint4* at = reinterpret_cast<uint4*>(vt + (vec >> 3) * (kKeys * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
-              const bool nobody = k0 + j >= w.rq.kv || ((bad >> (j >> p.page_shift)) & 1u);
-              if (nobody) {
-                if (pass) *at = make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                uint4 q = *at;
-                const uint32_t n0 = nonfinite_halves<BF>(q.x), n1 = nonfinite_halves<BF>(q.y), n2 = nonfinite_halves<BF>(q.z), n3 = nonfinite_halves<BF>(q.w);
-                if (n0 | n1 | n2 | n3) {
-                  found = true;
-                  if (pass) *at = make_uint4(q.x & ~n0, q.y & ~n1, q.z & ~n2, q.w & ~n3);
-                }
-              }
-            }
-            if (pass == 0) {
-              if (found) atomicOr(&sh->nonfinite, bad ? 3 : 1);
-              meet(x.two);   // everybody who has to has seen them before they go
-            }
+        } else {
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&sh->p_full[s][half]);
+            if (kSplit == 1) mbar_arrive(&sh->p_full[s][1]);
           }
-          if (!ok) break;
-          fence_async_proxy();
         }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh->p_full[s]);
       }
       if (!ok) break;
       // ---- end of the piece
-      const int n0 = x.two ? w.take : (w.take + 1) / 2, n1 = x.two ? w.take : w.take / 2;
-      const bool whole = w.starts() && w.ends();
-      const int slot = 2 * blockIdx.x + (w.index == 0 ? 0 : 1);
-      if (n0 > 0 && (s == 0 || !x.two)) wait(&sh->pv_done[0], (uint32_t)(done[0] + n0 - 1) & 1u);
-      if (n1 > 0 && (s == 1 || !x.two)) wait(&sh->pv_done[1], (uint32_t)(done[1] + n1 - 1) & 1u);
+      const int n1 = two ? take : take / 2;   // tiles of the second stream
+      const bool whole = x.starts && x.ends;
+      const int slot = 2 * blockIdx.x + (x.index == 0 ? 0 : 1);
+      wait(&sh->o_full, (uint32_t)pc & 1u);
+      // the row's sum over both threads
+      if (kSplit > 1) {
+        sh->exch[s][half][r] = l;
+        pair();
+        if (!ok) break;
+        l += sh->exch[s][half ^ 1][r];
+        pair();
+        if (!ok) break;
+      }
+      if (m == kNegInf && l == l) l = 0.f;   // no key, or only scores of -inf: nothing was weighed
       float f0 = 1.f, f1 = 1.f;
-      if (!x.two) {
-        sh->exch[s][r] = make_float2(m, l);
+      if (!two) {
+        if (kSplit == 1 || half == 0) sh->exch[s][0][r] = m;
+        if (kSplit == 1 || half == 1) sh->exch[s][1][r] = l;
         meet(true);
         if (!ok) break;
-        const float2 a = sh->exch[0][r], b = sh->exch[1][r];
-        m = fmaxf(a.x, b.x);
-        f0 = a.x == kNegInf ? 0.f : ex2((a.x - m) * c);
-        f1 = b.x == kNegInf ? 0.f : ex2((b.x - m) * c);
-        l = a.y * f0 + b.y * f1;
+        const float m0 = sh->exch[0][0][r], m1 = sh->exch[1][0][r];
+        m = fmaxf(m0, m1);
+        f0 = m0 == kNegInf ? 0.f : ex2((m0 - m) * c);
+        f1 = m1 == kNegInf ? 0.f : ex2((m1 - m) * c);
+        l = sh->exch[0][1][r] * f0 + sh->exch[1][1][r] * f1;
       }
-      if (!ok) break;
       const int poisoned = *reinterpret_cast<volatile int*>(&sh->nonfinite);
-      const long long row = (long long)w.rq.row0 + tok;
-      const int head = w.hk * p.G + r_head;
+      const long long row = (long long)x.row0 + tok;
+      const int head = x.hk * p.G + r_head;
       const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-      const int part_row = (x.two ? s * 128 : 0) + r;
+      const int part_row = (two ? s * 128 : 0) + r;
       if (warp_live) {
-        const int j_lo = x.two ? 0 : s * (DP / 2), j_hi = x.two ? DP : (s + 1) * (DP / 2);
+        // with one query tile the four groups of warps share the columns, with two the stream's two groups do
+        const int share = DP / (two ? kSplit : 2 * kSplit), j_lo = (two ? half : s * kSplit + half) * share;
 #pragma unroll 1
-        for (int j0 = j_lo; j0 < j_hi; j0 += 32) {
-          float o[32];
-          if (x.two) {
-            tm_ld32(t_o + j0, o);
-            tm_ld_wait(o);
+        for (int j0 = j_lo; j0 < j_lo + share; j0 += 16) {
+          float o[16];
+          if (two) {
+            tm_ld16(t_o + j0, o);
+            tm_ld_wait16(o);
           } else {
-            tm_ld32(tmem + lanes + 256 + j0, o);
-            tm_ld_wait(o);
+            tm_ld16(tmem + lanes + 256 + j0, o);
+            tm_ld_wait16(o);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] *= f0;
+            for (int j = 0; j < 16; ++j) o[j] *= f0;
             if (n1 > 0) {
-              float o1[32];
-              tm_ld32(tmem + lanes + 384 + j0, o1);
-              tm_ld_wait(o1);
+              float o1[16];
+              tm_ld16(tmem + lanes + 384 + j0, o1);
+              tm_ld_wait16(o1);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = fmaf(o1[j], f1, o[j]);
+              for (int j = 0; j < 16; ++j) o[j] = fmaf(o1[j], f1, o[j]);
             }
           }
           if (poisoned && live) {
-            const int k_lo = max(lo, (x.t0 + w.off) * kKeys), k_hi = min(hi, (x.t0 + w.off + w.take) * kKeys);
+            const int k_lo = max(lo, first * kKeys), k_hi = min(hi, (first + take) * kKeys);
+#pragma unroll 1
             for (int key = k_lo; key < k_hi; ++key) {
               // only those that were taken out: not seen by every row of the unit, or in a tile with a bad page
-              if (!(poisoned & 2) && key < x.hi_first && key >= x.lo_last) continue;
-              const int page = p.d.block_table[(long long)w.b * p.d.ld_table + key / p.d.page_size];
+              if (!(poisoned & 2) && key < hi_first && key >= lo_last) continue;
+              const int page = p.d.block_table[(long long)x.b * p.d.ld_table + key / p.d.page_size];
               if (page < 0 || page >= p.d.n_pages) continue;
-              const unsigned short* v = reinterpret_cast<const unsigned short*>(p.d.v_cache) + page * p.d.vc_page + (key % p.d.page_size) * p.d.vc_slot + w.hk * p.d.vc_head + j0;
-              for (int j = 0; j < 32 && j0 + j < p.d.D; ++j) {
+              const unsigned short* v = reinterpret_cast<const unsigned short*>(p.d.v_cache) + page * p.d.vc_page + (key % p.d.page_size) * p.d.vc_slot + x.hk * p.d.vc_head + j0;
+#pragma unroll 1
+              for (int j = 0; j < 16 && j0 + j < p.d.D; ++j) {
                 const unsigned short bits = v[j];
                 if (nonfinite_halves<BF>(bits) & 0xffffu) {
                   const float y = BF ? __uint_as_float((uint32_t)bits << 16) : __half2float(__ushort_as_half(bits));
 #pragma unroll
-                  for (int i = 0; i < 32; ++i)
+                  for (int i = 0; i < 16; ++i)
                     if (i == j) o[i] += y;
                 }
               }
@@ -798,40 +929,40 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (live) {
             if (whole) {
               unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head + j0;
-              uint32_t y[16];
+              uint32_t y[8];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) y[j] = pack2<BF>(o[2 * j] * inv, o[2 * j + 1] * inv);
+              for (int j = 0; j < 8; ++j) y[j] = pack2<BF>(o[2 * j] * inv, o[2 * j + 1] * inv);
               if (p.out_vec) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 2; ++j)
                   if (j0 + 8 * j < p.d.D) reinterpret_cast<uint4*>(dst)[j] = make_uint4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
               } else {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
+                for (int j = 0; j < 16; ++j)
                   if (j0 + j < p.d.D) dst[j] = (unsigned short)(y[j >> 1] >> ((j & 1) * 16));
               }
             } else {
               float4* dst = reinterpret_cast<float4*>(p.part + ((long long)slot * 256 + part_row) * DP + j0);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+              for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
             }
           }
         }
-        if (live && (x.two || s == 0)) {
+        if (live && half == 0 && (two || s == 0)) {
           if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m * c, l);   // c > 0: -inf stays
           else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m * c + log2f(l)) * kLn2;
         }
       }
       if (tid == 0 && !whole) {
         int* h = p.head + blockIdx.x * 8;
-        if (w.starts()) { h[0] = slot; h[2] = w.b; h[3] = w.hk; h[4] = w.u; }
-        else h[1] = w.ends() ? 1 : 2;
+        if (x.starts) { h[0] = slot; h[2] = x.b; h[3] = x.hk; h[4] = x.u; }
+        else h[1] = x.ends ? 1 : 2;
       }
-      if (!x.two) meet(true);   // both halves of the sums are read before either stream goes on
-      done[0] += n0;
-      done[1] += n1;
-      item0 += 2 * w.take;
-      tiles0 += w.take;
+      if (!two) meet(true);   // both halves of the sums are read before either stream goes on
+      item0 += 2 * take;
+      tiles0 += take;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
     }
   }
   fence_before();
@@ -1010,6 +1141,7 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   p.tile_tok = boxes * p.box_tok;
   p.page_rows = d->page_size < kKeys ? d->page_size : kKeys;
   p.boxes = kKeys / p.page_rows;
+  p.page_tiles = d->page_size / p.page_rows;
   p.page_shift = 0;
   while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
   p.c = d->scale * kLog2e;
