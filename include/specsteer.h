@@ -460,7 +460,7 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *   - The tensor-core kernel takes D <= 128 in multiples of 8, page_size a divisor or a multiple of 128 and a multiple of
  *     8, up to 128 query heads per kv head, and 16-byte aligned pointers and strides of q and the caches; everything else
  *     runs on a slower generic kernel.
- *   - workspace: 16-byte aligned device memory of at least specsteer_chunk_attention_workspace(desc) bytes, whose content
+ *   - workspace: 32-byte aligned device memory of at least specsteer_chunk_attention_workspace(desc) bytes, whose content
  *     before and after the call means nothing; calls that may overlap (two streams, two graphs) need one each.
  * Same inputs give the same bits.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE (too small), CUDA. */
 #define SPECSTEER_ATTENTION_MAX_D 256

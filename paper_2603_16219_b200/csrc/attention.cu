@@ -226,7 +226,7 @@ extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_
   if (st != SPECSTEER_OK) return st;
   if (d->B == 0 || d->T == 0) return SPECSTEER_OK;
   const size_t need = specsteer_chunk_attention_workspace(d);
-  if (need > 0 && (!d->workspace || d->workspace_bytes < (long long)need || ((uintptr_t)d->workspace & 15u))) return SPECSTEER_ERR_WORKSPACE;
+  if (need > 0 && (!d->workspace || d->workspace_bytes < (long long)need || ((uintptr_t)d->workspace & 31u))) return SPECSTEER_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   if (attention_tc_takes(d)) {
     if (launch_attention_tc(d, s) != cudaSuccess) {

@@ -9,17 +9,18 @@
 // cut needs nothing from the host: every CTA sums the lengths itself.  A unit that a cut goes through leaves partial
 // results (unnormalised sums, maximum and sum of weights per row) that attention_join_kernel puts together.
 //
-// Inside a CTA: warp 16 issues the TMA loads (a ring of stages of one 128-key tile of K or V; a page or its part of 128
-// keys is a box), warp 17 issues tcgen05.mma, and two softmax groups (streams) of 8 warps turn scores into weights.  A row
-// belongs to two threads of two warps, 64 keys of a tile each, which exchange their maxima through shared memory: one
-// thread a row left too few independent instructions to fill the pipes.  Stream s has scores S_s (128 columns of tensor memory, overwritten by the 16-bit weights P_s, which the second product
-// reads from tensor memory) and sums O_s (128 columns).  With two query tiles each stream owns one and both use every
-// key tile; with one query tile the streams take the key tiles in turn and are put together at the end.  Either way one
-// stream's exponentials run under the other stream's products.
+// Inside a CTA: warp 8 walks the list and issues the TMA loads (a ring of stages of one 128-key tile of K or V; a page or
+// its part of 128 keys is a box), warp 9 issues tcgen05.mma, warps 0..3 and 4..7 are two softmax groups (streams), one row
+// a thread.  Stream s has scores S_s (two blocks of 64 keys, 64 columns of tensor memory each, overwritten by the 16-bit
+// weights P_s, which the second product reads from tensor memory) and sums O_s (128 columns).  The product that gives a
+// block's next scores is issued behind the one that takes its weights, so while a group weighs one block the tensor cores
+// work on the other.  With two query tiles each stream owns one and both use every key tile; with one query tile the
+// streams take the key tiles in turn and are put together at the end.
 //
-// Maximum.  Weights are 2^(c s - c m) with a reference m per row that follows the running maximum only when that has
-// grown by more than 8 (in powers of two): O_s is then rescaled in tensor memory, which after the first tiles hardly
-// ever happens.  Weights stay below 2^8, sums are float32.
+// Maximum.  Weights are 2^(c s - c m) with a reference m per row.  A block is weighed against the reference there is; only
+// if that makes its weights sum to more than 2^15 (or there is none yet) the block's maximum is formed, the reference raised,
+// O_s rescaled in tensor memory and the block weighed again.  Weights are then at most 2^15, which float16 holds, and after
+// the first tile hardly any block needs its maximum, a sixth of the work.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -32,13 +33,12 @@ namespace specsteer {
 namespace {
 
 constexpr int kKeys = 128;          // keys per tile
-constexpr int kSplit = 1;           // threads that share a row of scores
-constexpr int kSoftmaxWarps = 8 * kSplit;
+constexpr int kSoftmaxWarps = 8;
 constexpr int kProducerWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 constexpr int kTcThreads = 32 * (kSoftmaxWarps + 2);
 constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
 constexpr int kPolyPairs = 0;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
-constexpr float kGrow = 8.f;        // powers of two the maximum may exceed the reference by
+constexpr float kMostSum = 32768.f; // of the weights of a row and block before the reference is raised
 constexpr int kPieces = 4;          // pieces of work the producer may be ahead
 
 template <int DP> struct TcLayout {
@@ -67,19 +67,20 @@ struct Piece {
 struct TcShared {
   uint64_t full[12], empty[12];
   uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[2], p_full[2][2], o_full;   // p_full[s][h]: weights of the first / last 64 keys of a tile
+  uint64_t s_full[2][2], p_full[2][2];   // [s][h]: scores, weights of stream s, first / last 64 keys of a tile
+  uint64_t o_full, half_done[2];         // a piece's sums; those of the stream but for the last 64 keys
   uint64_t piece_full[kPieces], piece_empty[kPieces];
   uint64_t both, group[2], drain;
   uint32_t tmem_slot;
   int abort_flag;
-  int nonfinite;           // an infinity or NaN was taken out of a tile of values: bit 0, and bit 1 in a tile with a bad page
+  int nonfinite;           // an infinity or NaN was taken out of a tile of values
   int start_b, start_hk, start_u, start_off;
   long long end;           // where this CTA's range ends, from the beginning of its first unit (0: it has none)
   Piece piece[kPieces];
   uint32_t bad[16];        // per key tile (counted modulo 16): the boxes of it that lie outside the pool
   union {
     long long scan[kTcThreads / 32];
-    float exch[2][2][128]; // [stream][half][row]: a tile's maxima; at the end of a piece sums, references
+    float2 exch[2][128];   // reference and sum of each stream's rows
   };
 };
 template <int DP> constexpr int tc_smem_bytes() { return TcLayout<DP>::kControl + (int)sizeof(TcShared); }
@@ -91,7 +92,7 @@ struct TcParams {
   int page_rows, boxes, page_shift;    // key box: keys, boxes per key tile, log2 of its keys
   int page_tiles;                      // key tiles per page (1 when a tile has several pages)
   float c;                             // scale * log2(e)
-  int out_vec;                         // out rows are 16-byte aligned
+  int out_vec;                         // out rows are 32-byte aligned and a multiple of 32 bytes long
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
   float2* part_ml;                     // [2*gridDim][256] reference (powers of two) and sum
   int* head;                           // [gridDim][8] see write_head
@@ -199,6 +200,12 @@ __device__ __forceinline__ void tm_ld_wait16(float* v) {
                : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
                  "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
                :
+               : "memory");
+}
+// 32 bytes to a 32-byte aligned address: a whole sector a thread, a row a thread
+__device__ __forceinline__ void st_256(void* at, const uint32_t* u) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]),
+               "r"(u[5]), "r"(u[6]), "r"(u[7])
                : "memory");
 }
 __device__ __forceinline__ void tm_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -417,7 +424,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     for (int i = 0; i < L::kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 1);
-      mbar_init(&sh->s_full[i], 1); mbar_init(&sh->p_full[i][0], 4); mbar_init(&sh->p_full[i][1], 4);
+      for (int h = 0; h < 2; ++h) { mbar_init(&sh->s_full[i][h], 1); mbar_init(&sh->p_full[i][h], 4); }
+      mbar_init(&sh->half_done[i], 1);
       mbar_init(&sh->group[i], kSoftmaxWarps / 2);
     }
     for (int i = 0; i < kPieces; ++i) { mbar_init(&sh->piece_full[i], 1); mbar_init(&sh->piece_empty[i], kSoftmaxWarps + 1); }
@@ -530,24 +538,25 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       __syncwarp();
       if (w.take <= 0) break;
       table = p.d.block_table + (long long)w.b * p.d.ld_table;
-      const int n_q = w.x.two ? 2 : 1;
-#pragma unroll 1
-      for (int s = 0; s < n_q && ok; ++s, ++qi) {
-        const int slot = qi & 1;
-        ok = tc_wait<true>(&sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
-        if (!ok) break;
-        const int tok = w.x.tok0 + s * p.tile_tok, cnt = min(p.tile_tok, w.x.tok1 - tok);
-        const int nb = (cnt + p.box_tok - 1) / p.box_tok;
-        if (lane == 0) mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
-        __syncwarp();
-        if (box < nb)
-          tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + box * p.box_rows * 128, &tm_q, chunk * 64, w.hk * p.G, w.rq.row0 + tok + box * p.box_tok, &sh->q_full[slot]);
-      }
       const int first = w.x.t0 + w.off, take = w.take, ahead = min(w.x.two ? 1 : 2, take);
       int pg0 = page_of(first), pg1 = take > 1 ? page_of(first + 1) : 0, pg2 = take > 2 ? page_of(first + 2) : 0;
 #pragma unroll 1
       for (int t = -ahead; t < take && ok; ++t) {
-        // values of tile t, then keys of tile t + ahead
+        // values of tile t, then keys of tile t + ahead; the queries behind the first keys, whose stages are free sooner
+#pragma unroll 1
+        for (int s = 0; t == 0 && s < (w.x.two ? 2 : 1) && ok; ++s, ++qi) {
+          const int slot = qi & 1;
+          ok = tc_wait<true>(&sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
+          if (!ok) break;
+          const int tok = w.x.tok0 + s * p.tile_tok, cnt = min(p.tile_tok, w.x.tok1 - tok);
+          const int nb = (cnt + p.box_tok - 1) / p.box_tok;
+          if (lane == 0) mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
+          __syncwarp();
+          if (box < nb)
+            tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + box * p.box_rows * 128, &tm_q, chunk * 64, w.hk * p.G,
+                   w.rq.row0 + tok + box * p.box_tok, &sh->q_full[slot]);
+        }
+        if (!ok) break;
         const int pg3 = t >= 0 && t + 3 < take ? page_of(first + t + 3) : 0;
         if (t >= 0) load_tile(&tm_v, first + t, pg0);
         if (t + ahead < take && ok) load_k(first + t + ahead, t + ahead == 0 ? pg0 : (t + ahead == 1 && t < 0) || ahead == 1 ? pg1 : pg2);
@@ -567,9 +576,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // The whole warp runs the loop, so that addresses and descriptors stay in uniform registers.
     // All columns were allocated, so tensor memory begins at column 0.
     constexpr uint32_t t_base = 0;
-    const uint32_t id_qk = instr_desc(BF, kKeys, false), id_pv = instr_desc(BF, DP, true);
+    const uint32_t id_qk = instr_desc(BF, 64, false), id_pv = instr_desc(BF, DP, true);
     int st = 0, qi = 0, pc = 0, b = 0;   // st: stage of the next ring item
-    uint32_t st_phase = 0, p_phase = 0;  // p_phase: bit s, of the weights of stream s
+    uint32_t st_phase = 0, p_phase = 0;  // p_phase: bit 2 s + h, of the weights of block h of stream s
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (ok) ok = tc_wait<true>(bar, parity);
@@ -582,30 +591,25 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
       return got;
     };
-    // Scores of stream s.  The commit also says that the stream's product with the values before it is complete.
-    auto scores = [&](int s, int slot, int stage, bool last_use) {
+    // Scores of block h of stream s.  The commit also says that the product with the block's values before it is complete.
+    auto scores = [&](int s, int h, int slot, int stage) {
       if (!ok) return;
-      const uint32_t a = desc_rows(smem0 + slot * L::kQBytes), b = desc_rows(smem0 + L::kRing + stage * L::kStageBytes);
+      const uint32_t a = desc_rows(smem0 + slot * L::kQBytes), b = desc_rows(smem0 + L::kRing + stage * L::kStageBytes) + h * (64 * 128 >> 4);
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k) {
         const uint32_t step = (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2);
-        mma_ss(t_base + s * 128, a + step, b + step, id_qk, k != 0);
+        mma_ss(t_base + s * 128 + h * 64, a + step, b + step, id_qk, k != 0);
       }
-      mma_commit(&sh->s_full[s]);
-      if (last_use) mma_commit(&sh->empty[stage]);
+      mma_commit(&sh->s_full[s][h]);
     };
-    auto values = [&](int s, int stage, bool accumulate, bool last_use) {
-      const uint32_t b = desc_cols(smem0 + L::kRing + stage * L::kStageBytes);
+    auto values = [&](int s, int h, int stage, bool accumulate) {
+      const uint32_t b = desc_cols(smem0 + L::kRing + stage * L::kStageBytes) + h * (64 * 128 >> 4);
+      wait(&sh->p_full[s][h], (p_phase >> (2 * s + h)) & 1u);
+      p_phase ^= 1u << (2 * s + h);
+      if (!ok) return;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        wait(&sh->p_full[s][h], (p_phase >> s) & 1u);
-        if (!ok) return;
-#pragma unroll
-        for (int k = h * 4; k < h * 4 + 4; ++k)
-          mma_ts(t_base + 256 + s * 128, t_base + s * 128 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, k != 0 || accumulate);
-      }
-      if (last_use) mma_commit(&sh->empty[stage]);
-      p_phase ^= 1u << s;
+      for (int k = 0; k < 4; ++k)
+        mma_ts(t_base + 256 + s * 128, t_base + s * 128 + h * 64 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, k != 0 || accumulate);
     };
 #pragma unroll 1
     for (;; ++pc) {
@@ -626,19 +630,24 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       for (int t = -ahead; t < take && ok; ++t) {
         const bool next_k = t + ahead < take;
         const int v = t >= 0 ? item() : 0;
-        if (two) {
-          if (t >= 0) values(0, v, t > 0, false);
-          const int k = next_k ? item() : 0;
-          if (next_k) scores(0, q0, k, false);
-          if (t >= 0) values(1, v, t > 0, true);
-          if (next_k) scores(1, q1, k, true);
-        } else {
-          if (t >= 0) values(t & 1, v, t > 1, true);
-          if (next_k) {
-            const int k = item();
-            scores((t + ahead) & 1, q0, k, true);
+        int k = 0;
+        // the streams of tile t, which are those of tile t + ahead if there is one
+        const int s0 = two ? 0 : (t >= 0 ? t : t + ahead) & 1, s1 = two ? 1 : s0;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+          for (int s = s0; s <= s1; ++s) {
+            if (t >= 0) values(s, h, v, t >= ahead || h > 0);
+            if (next_k) {
+              if (h == 0 && s == s0) k = item();
+              scores(s, h, s ? q1 : q0, k);
+            } else if (h == 0 && ok) {
+              mma_commit(&sh->half_done[s]);
+            }
           }
         }
+        if (t >= 0 && ok) mma_commit(&sh->empty[v]);
+        if (next_k && ok) mma_commit(&sh->empty[k]);
       }
       if (!ok) break;
       mma_commit(&sh->o_full);
@@ -653,35 +662,22 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       tc_wait<true>(&sh->drain, 0);
     }
   } else {
-    // ================= softmax: kSplit threads a row =================
-    const int s = warp / (4 * kSplit), half = (warp >> 2) % kSplit, quarter = warp & 3, r = quarter * 32 + lane;
-    constexpr int kCols = kKeys / kSplit;      // scores of a row that a thread has
+    // ================= softmax: one row a thread =================
+    const int s = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
     const int r_tok = r / p.G, r_head = r - r_tok * p.G;
-    const int pair_id = 1 + s * 4 + quarter;   // hardware barrier of the two warps that share 32 rows
     const float c = p.c;
-    uint32_t s_phase = 0;
+    uint32_t s_phase = 0, half_phase = 0;   // s_phase: of both blocks at the beginning of a tile
     uint32_t group_phase = 0, both_phase = 0;
     int item0 = 0, tiles0 = 0, pc = 0, b = 0;
     bool ok = true;
-    // Gives up: the partner warp may stand at the pair's barrier now or come there once more; it is let through and then
-    // sees the abort flag.
-    auto fail = [&]() {
-      ok = false;
-      if (lane == 0) give_up(sh, p.d.req_status ? p.d.req_status + b : nullptr);
-      __threadfence_block();
-      __syncwarp();
-      if (kSplit > 1) asm volatile("barrier.cta.arrive %0, 64;" ::"r"(pair_id) : "memory");
-    };
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok && !tc_wait<true>(bar, parity)) fail();
+      if (ok && !tc_wait<true>(bar, parity)) {
+        ok = false;
+        if (lane == 0) give_up(sh, p.d.req_status ? p.d.req_status + b : nullptr);
+      }
       fence_after();
-    };
-    auto pair = [&]() {
-      if (kSplit == 1 || !ok) return;
-      asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_id) : "memory");
-      ok = __all_sync(kFullMask, !aborted(sh));
     };
     // barriers among the softmax warps: of this stream, of both (bounded like every wait)
     auto meet = [&](bool all) {
@@ -715,168 +711,169 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         lo = p.d.window > 0 && hi > p.d.window ? hi - p.d.window : 0;
       }
       const int hi_first = x.hi_first, lo_last = x.lo_last;
-      float m = kNegInf, l = 0.f;       // reference (raw score, the same in a row's threads), sum over this thread's keys
+      float m = live ? kNegInf : 0.f, l = 0.f;       // reference (raw score; none yet: -inf), sum
       const int step = two ? 1 : 2, t_from = two ? 0 : s;
 #pragma unroll 1
       for (int t = t_from; t < take; t += step) {
         const int k0 = (first + t) * kKeys;
-        wait(&sh->s_full[s], s_phase);
-        s_phase ^= 1u;
+        wait(&sh->s_full[s][0], s_phase);   // the tile's keys have landed, and what was loaded before them
         if (!ok) break;
         const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(tiles0 + t) & 15]);
         const bool edge = k0 + kKeys > hi_first || k0 < lo_last || bad != 0;
         if (edge) {
-          // Values of keys that some row of the unit does not see: those that nobody sees (behind the last key, on a
-          // page outside the pool) become zero; an infinity or NaN among the others is taken out here, where it would
-          // reach rows with weight 0, and added in the epilogue to the rows that see it.
+          // Values of keys that some row of the unit does not see.  What lies behind the last key in its page becomes zero
+          // (whole pages behind it, and pages outside the pool, were loaded as zeros); an infinity or NaN among the others is
+          // taken out here, where it would reach rows with weight 0, and added in the epilogue to the rows that see it.
           const int it = item0 + x.item_of_v(t);
           wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
           if (!ok) break;
           unsigned char* vt = smem_raw + L::kRing + (it % L::kStages) * L::kStageBytes;
-          const int from = bad ? kKeys : min(kKeys, max(0, lo_last - k0)), to = bad ? kKeys : min(kKeys, max(from, hi_first - k0));
-          const int n_vec = (from + (kKeys - to)) * (DP / 8);          // of keys [0, from) and [to, 128)
-          const int kv = x.kv;
+          const int kv_here = min(kKeys, x.kv - k0);
+          const int from = min(kv_here, max(0, lo_last - k0)), to = min(kv_here, max(from, hi_first - k0));
+          const int zero_to = min(kKeys, (kv_here + p.page_rows - 1) & -p.page_rows);
+          auto vector = [&](int j, int vec) {
+            return reinterpret_cast<uint4*>(vt + (vec >> 3) * (kKeys * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
+          };
+          // two query tiles: the groups share the work
+          const int me = two ? tid : tid & 127, team = two ? 256 : 128;
+          constexpr int kVec = DP / 8;
 #pragma unroll 1
-          for (int pass = 0; pass < 2; ++pass) {
-            bool found = false;
-#pragma unroll 1
-            for (int e = tid % (128 * kSplit); e < n_vec; e += 128 * kSplit) {
-              const int jj = e / (DP / 8), vec = e % (DP / 8), j = jj < from ? jj : jj - from + to;
-              uint4* at = reinterpret_cast<uint4*>(vt + (vec >> 3) * (kKeys * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
-              const bool nobody = k0 + j >= kv || ((bad >> (j >> p.page_shift)) & 1u);
-              uint4 y = *at;
-              uint32_t n0 = 0xffffffffu, n1 = n0, n2 = n0, n3 = n0;
-              if (!nobody) {
-                n0 = nonfinite_halves<BF>(y.x); n1 = nonfinite_halves<BF>(y.y); n2 = nonfinite_halves<BF>(y.z); n3 = nonfinite_halves<BF>(y.w);
-                found = found || (n0 | n1 | n2 | n3);
-              }
-              if (pass && (n0 | n1 | n2 | n3)) *at = make_uint4(y.x & ~n0, y.y & ~n1, y.z & ~n2, y.w & ~n3);
-            }
-            if (pass == 0) {
-              if (found) atomicOr(&sh->nonfinite, bad ? 3 : 1);
-              meet(two);   // everybody who has to has seen them before they go
-            }
+          for (int e = kv_here * kVec + me; e < zero_to * kVec; e += team) *vector(e / kVec, e % kVec) = make_uint4(0u, 0u, 0u, 0u);
+          const int n_vec = (from + (kv_here - to)) * kVec;          // of keys [0, from) and [to, kv)
+          bool found = false;
+#pragma unroll 2
+          for (int e = me; e < n_vec; e += team) {
+            const int j = e / kVec;
+            const uint4 y = *vector(j < from ? j : j - from + to, e % kVec);
+            found = found || (nonfinite_halves<BF>(y.x) | nonfinite_halves<BF>(y.y) | nonfinite_halves<BF>(y.z) | nonfinite_halves<BF>(y.w));
           }
-          if (!ok) break;
+          if (found) *reinterpret_cast<volatile int*>(&sh->nonfinite) = 1;
           fence_async_proxy();
-        }
-        if (warp_live) {
-          float v[kCols];
-#pragma unroll
-          for (int i = 0; i < kCols; i += 32) tm_ld32(t_s + half * kCols + i, v + i);
-          tm_ld_wait(v);
-#pragma unroll
-          for (int i = 32; i < kCols; i += 32) tm_ld_tie(v + i);
-          if (edge) {
-#pragma unroll
-            for (int i = 0; i < kCols; i += 32) {
-              // the columns of 32 that the row sees, as bits
-              const int j0 = half * kCols + i, from = max(lo - k0 - j0, 0), to = min(hi - k0 - j0, 32);
-              uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
-              if (bad) {
+          meet(two);   // everybody has looked before anything is taken out
+          if (!ok) break;
+          if (*reinterpret_cast<volatile int*>(&sh->nonfinite)) {   // (or in an earlier tile: then there is nothing to find)
 #pragma unroll 1
-                for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
-                  if ((bad >> ((j0 + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
-              }
-#pragma unroll
-              for (int j = 0; j < 32; ++j) v[i + j] = (keep & (1u << j)) ? v[i + j] : kNegInf;
+            for (int e = tid & 127; e < n_vec; e += 128) {
+              const int j = e / kVec;
+              uint4* at = vector(j < from ? j : j - from + to, e % kVec);
+              const uint4 y = *at;
+              const uint32_t n0 = nonfinite_halves<BF>(y.x), n1 = nonfinite_halves<BF>(y.y), n2 = nonfinite_halves<BF>(y.z), n3 = nonfinite_halves<BF>(y.w);
+              if (n0 | n1 | n2 | n3) *at = make_uint4(y.x & ~n0, y.y & ~n1, y.z & ~n2, y.w & ~n3);
             }
+            fence_async_proxy();
           }
-          float mx[8] = {kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf};
+        }
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          if (h) wait(&sh->s_full[s][1], s_phase);
+          if (!ok) break;
+          if (warp_live) {
+            float v[64];
+            tm_ld32(t_s + h * 64, v);
+            tm_ld32(t_s + h * 64 + 32, v + 32);
+            tm_ld_wait(v);
+            tm_ld_tie(v + 32);
+            if (edge) {
 #pragma unroll
-          for (int j = 0; j < kCols; j += 16) {
+              for (int i = 0; i < 64; i += 32) {
+                // the columns of 32 that the row sees, as bits
+                const int j0 = h * 64 + i, from = max(lo - k0 - j0, 0), to = min(hi - k0 - j0, 32);
+                uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
+                if (bad) {
+#pragma unroll 1
+                  for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
+                    if ((bad >> ((j0 + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
+                }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
-          }
-          float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
-          if (kSplit > 1) {
-            // The maxima of a row's two threads.  A slot is written again one tile later, after scores that were formed
-            // after both threads' weights of this tile, hence after the reads here.  The barrier also says that both have
-            // their scores in registers, whose place the weights take.
-            sh->exch[s][half][r] = top;
-            pair();
+                for (int j = 0; j < 32; ++j) v[i + j] = (keep & (1u << j)) ? v[i + j] : kNegInf;
+              }
+            }
+            bool raise = __any_sync(kFullMask, m == kNegInf);
+#pragma unroll 1
+            for (;;) {
+              if (raise) {
+                float mx[8] = {m, m, m, m, m, m, m, m};
+#pragma unroll
+                for (int j = 0; j < 64; j += 16) {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) mx[i] = max3(mx[i], v[j + 2 * i], v[j + 2 * i + 1]);
+                }
+                const float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
+                const float alpha = top > m && m != kNegInf ? ex2((m - top) * c) : 1.f;   // (without a reference the sums are zero)
+                if (t + h > t_from && __any_sync(kFullMask, alpha != 1.f)) {
+                  // The sums are at rest once the product with the last weights is complete: the scores of the other
+                  // block that were formed behind it say so, or at the end of the piece a commit of its own.
+                  if (h == 0) wait(&sh->s_full[s][1], s_phase);
+                  else if (t + step < take) wait(&sh->s_full[s][0], s_phase ^ 1u);
+                  else wait(&sh->half_done[s], half_phase);
+                  if (!ok) break;
+#pragma unroll 1
+                  for (int j0 = 0; j0 < DP; j0 += 16) {
+                    float o[16];
+                    tm_ld16(t_o + j0, o);
+                    tm_ld_wait16(o);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] *= alpha;
+                    tm_st16(t_o + j0, reinterpret_cast<const uint32_t*>(o));
+                  }
+                }
+                l *= alpha;
+                m = top;
+              }
+              const float ref = m == kNegInf ? 0.f : m * c;
+              const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
+              float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+              // The weights go to the second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
+#pragma unroll
+              for (int i = 0; i < 64; i += 32) {
+                uint32_t w16[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  const float2 x2 = fma2(make_float2(v[i + 2 * j], v[i + 2 * j + 1]), c2, ref2);
+                  const bool poly = ((i / 2 + j) * kPolyPairs) % 32 < kPolyPairs;
+                  const float2 y = poly ? ex2_poly(x2) : make_float2(ex2(x2.x), ex2(x2.y));
+                  sum[j & 3] = add2(sum[j & 3], y);
+                  w16[j] = pack2<BF>(y.x, y.y);
+                }
+                tm_st16(t_s + h * 64 + i / 2, w16);
+              }
+              sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+              const float total = sum[0].x + sum[0].y;
+              if (raise || __all_sync(kFullMask, !live || total <= kMostSum)) {
+                l += total;
+                break;
+              }
+              raise = true;
+            }
             if (!ok) break;
-            top = fmaxf(top, sh->exch[s][half ^ 1][r]);
+            tm_st_wait();
+            fence_before();
           }
-          const bool raise = top > m && (m == kNegInf || (top - m) * c > kGrow);
-          if (__any_sync(kFullMask, raise)) {
-            const float alpha = !raise ? 1.f : m == kNegInf ? 0.f : ex2((m - top) * c);
-            if (t > t_from && __any_sync(kFullMask, raise && m != kNegInf)) {
-              // the sums are at rest: the product before was complete when these scores were
-              const int j_lo = half * (DP / kSplit);
-#pragma unroll 1
-              for (int j0 = j_lo; j0 < j_lo + DP / kSplit; j0 += 16) {
-                float o[16];
-                tm_ld16(t_o + j0, o);
-                tm_ld_wait16(o);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] *= alpha;
-                tm_st16(t_o + j0, reinterpret_cast<const uint32_t*>(o));
-              }
-            }
-            l *= alpha;
-            if (raise) m = top;
-          }
-          const float ref = m == kNegInf ? 0.f : m * c;
-          const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
-          float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          // The weights go to the second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
-#pragma unroll
-          for (int i = 0; i < kCols; i += 32) {
-            uint32_t w16[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float2 x2 = fma2(make_float2(v[i + 2 * j], v[i + 2 * j + 1]), c2, ref2);
-              const bool poly = ((i / 2 + j) * kPolyPairs) % 32 < kPolyPairs;
-              const float2 y = poly ? ex2_poly(x2) : make_float2(ex2(x2.x), ex2(x2.y));
-              sum[j & 3] = add2(sum[j & 3], y);
-              w16[j] = pack2<BF>(y.x, y.y);
-            }
-            tm_st16(t_s + (half * kCols + i) / 2, w16);
-            if (i % 64 == 32) {
-              tm_st_wait();
-              fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&sh->p_full[s][kSplit == 1 ? i / 64 : half]);
-            }
-          }
-          sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-          l += sum[0].x + sum[0].y;
-        } else {
           __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(&sh->p_full[s][half]);
-            if (kSplit == 1) mbar_arrive(&sh->p_full[s][1]);
-          }
+          if (lane == 0) mbar_arrive(&sh->p_full[s][h]);
         }
+        if (!ok) break;
+        s_phase ^= 1u;
       }
       if (!ok) break;
+      if (t_from < take) half_phase ^= 1u;
       // ---- end of the piece
       const int n1 = two ? take : take / 2;   // tiles of the second stream
       const bool whole = x.starts && x.ends;
       const int slot = 2 * blockIdx.x + (x.index == 0 ? 0 : 1);
       wait(&sh->o_full, (uint32_t)pc & 1u);
-      // the row's sum over both threads
-      if (kSplit > 1) {
-        sh->exch[s][half][r] = l;
-        pair();
-        if (!ok) break;
-        l += sh->exch[s][half ^ 1][r];
-        pair();
-        if (!ok) break;
-      }
+      if (!ok) break;
       if (m == kNegInf && l == l) l = 0.f;   // no key, or only scores of -inf: nothing was weighed
       float f0 = 1.f, f1 = 1.f;
       if (!two) {
-        if (kSplit == 1 || half == 0) sh->exch[s][0][r] = m;
-        if (kSplit == 1 || half == 1) sh->exch[s][1][r] = l;
+        sh->exch[s][r] = make_float2(m, l);
         meet(true);
         if (!ok) break;
-        const float m0 = sh->exch[0][0][r], m1 = sh->exch[1][0][r];
-        m = fmaxf(m0, m1);
-        f0 = m0 == kNegInf ? 0.f : ex2((m0 - m) * c);
-        f1 = m1 == kNegInf ? 0.f : ex2((m1 - m) * c);
-        l = sh->exch[0][1][r] * f0 + sh->exch[1][1][r] * f1;
+        const float2 e0 = sh->exch[0][r], e1 = sh->exch[1][r];
+        m = fmaxf(e0.x, e1.x);
+        f0 = e0.x == kNegInf ? 0.f : ex2((e0.x - m) * c);
+        f1 = e1.x == kNegInf ? 0.f : ex2((e1.x - m) * c);
+        l = e0.y * f0 + e1.y * f1;
       }
       const int poisoned = *reinterpret_cast<volatile int*>(&sh->nonfinite);
       const long long row = (long long)x.row0 + tok;
@@ -884,71 +881,68 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
       const int part_row = (two ? s * 128 : 0) + r;
       if (warp_live) {
-        // with one query tile the four groups of warps share the columns, with two the stream's two groups do
-        const int share = DP / (two ? kSplit : 2 * kSplit), j_lo = (two ? half : s * kSplit + half) * share;
+        // with one query tile the two groups share the columns
+        const int share = two ? DP : DP / 2, j_lo = two ? 0 : s * share;
+        const uint32_t t_0 = two ? t_o : tmem + lanes + 256;
+        unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head;
+        float* part = p.part + ((long long)slot * 256 + part_row) * DP;
 #pragma unroll 1
-        for (int j0 = j_lo; j0 < j_lo + share; j0 += 16) {
-          float o[16];
-          if (two) {
-            tm_ld16(t_o + j0, o);
-            tm_ld_wait16(o);
+        for (int j0 = j_lo; j0 < j_lo + share; j0 += 32) {
+          float o[32];
+          tm_ld32(t_0 + j0, o);
+          if (!two && n1 > 0) {
+            float o1[32];
+            tm_ld32(tmem + lanes + 384 + j0, o1);
+            tm_ld_wait(o);
+            tm_ld_tie(o1);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = fmaf(o1[j], f1, o[j] * f0);
           } else {
-            tm_ld16(tmem + lanes + 256 + j0, o);
-            tm_ld_wait16(o);
+            tm_ld_wait(o);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] *= f0;
-            if (n1 > 0) {
-              float o1[16];
-              tm_ld16(tmem + lanes + 384 + j0, o1);
-              tm_ld_wait16(o1);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = fmaf(o1[j], f1, o[j]);
-            }
+            for (int j = 0; j < 32; ++j) o[j] *= f0;
           }
           if (poisoned && live) {
             const int k_lo = max(lo, first * kKeys), k_hi = min(hi, (first + take) * kKeys);
 #pragma unroll 1
             for (int key = k_lo; key < k_hi; ++key) {
-              // only those that were taken out: not seen by every row of the unit, or in a tile with a bad page
-              if (!(poisoned & 2) && key < hi_first && key >= lo_last) continue;
+              if (key < hi_first && key >= lo_last) continue;   // only those that were taken out
               const int page = p.d.block_table[(long long)x.b * p.d.ld_table + key / p.d.page_size];
               if (page < 0 || page >= p.d.n_pages) continue;
               const unsigned short* v = reinterpret_cast<const unsigned short*>(p.d.v_cache) + page * p.d.vc_page + (key % p.d.page_size) * p.d.vc_slot + x.hk * p.d.vc_head + j0;
 #pragma unroll 1
-              for (int j = 0; j < 16 && j0 + j < p.d.D; ++j) {
+              for (int j = 0; j < 32 && j0 + j < p.d.D; ++j) {
                 const unsigned short bits = v[j];
                 if (nonfinite_halves<BF>(bits) & 0xffffu) {
                   const float y = BF ? __uint_as_float((uint32_t)bits << 16) : __half2float(__ushort_as_half(bits));
 #pragma unroll
-                  for (int i = 0; i < 16; ++i)
+                  for (int i = 0; i < 32; ++i)
                     if (i == j) o[i] += y;
                 }
               }
             }
           }
           if (live) {
-            if (whole) {
-              unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head + j0;
-              uint32_t y[8];
+            if (!whole) {
 #pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = pack2<BF>(o[2 * j] * inv, o[2 * j + 1] * inv);
+              for (int j = 0; j < 32; j += 8) st_256(part + j0 + j, reinterpret_cast<const uint32_t*>(o + j));
+            } else {
+              uint32_t y[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) y[j] = pack2<BF>(o[2 * j] * inv, o[2 * j + 1] * inv);
               if (p.out_vec) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                  if (j0 + 8 * j < p.d.D) reinterpret_cast<uint4*>(dst)[j] = make_uint4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+                  if (j0 + 16 * j < p.d.D) st_256(dst + j0 + 16 * j, y + 8 * j);
               } else {
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                  if (j0 + j < p.d.D) dst[j] = (unsigned short)(y[j >> 1] >> ((j & 1) * 16));
+                for (int j = 0; j < 32; ++j)
+                  if (j0 + j < p.d.D) dst[j0 + j] = (unsigned short)(y[j >> 1] >> ((j & 1) * 16));
               }
-            } else {
-              float4* dst = reinterpret_cast<float4*>(p.part + ((long long)slot * 256 + part_row) * DP + j0);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
             }
           }
         }
-        if (live && half == 0 && (two || s == 0)) {
+        if (live && (two || s == 0)) {
           if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m * c, l);   // c > 0: -inf stays
           else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m * c + log2f(l)) * kLn2;
         }
@@ -1146,7 +1140,7 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
   p.c = d->scale * kLog2e;
   if (p.c < 1e-30f) p.c = 1e-30f;   // a scale of zero: weights all 1 without 0 * infinity for masked scores
-  p.out_vec = ((uintptr_t)d->out & 15u) == 0 && d->o_tok % 8 == 0 && d->o_head % 8 == 0;
+  p.out_vec = ((uintptr_t)d->out & 31u) == 0 && d->o_tok % 16 == 0 && d->o_head % 16 == 0 && d->D % 16 == 0;
   p.part = (float*)d->workspace;
   p.part_ml = (float2*)((char*)d->workspace + part_bytes(DP));
   p.head = (int*)((char*)d->workspace + part_bytes(DP) + ml_bytes());
