@@ -381,7 +381,8 @@ enum {
   SPECSTEER_REQ_NO_ROOM = 64,   /* plan: the chunk does not fit max_tokens; the request gets no tokens this time */
   SPECSTEER_REQ_NO_PAGES = 128, /* plan: the pool has too few free pages; no tokens this time, pages as they were */
   SPECSTEER_REQ_BAD_POOL = 256, /* plan: ring_pos does not describe a ring of n_pages entries; nothing is moved */
-  SPECSTEER_REQ_TIMEOUT = 512   /* attention: a bounded device-side wait gave up; outputs of the call are undefined */
+  SPECSTEER_REQ_TIMEOUT = 512   /* attention (on request 0): a bounded device-side wait gave up; the call's outputs are
+                                   undefined */
 };
 
 /* Block tables and slot maps from request lengths.  Per request b, in this order:
@@ -457,8 +458,7 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *   - req_status may be NULL; bits are OR-ed into it (clear it first; specsteer_cache_plan writes it).
  *   - scale >= 0 and finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
  *     caches and out.  Strides in elements, innermost axis dense.
- *   - The tensor-core kernel takes D <= 128 in multiples of 8, page_size a divisor or a multiple of 128 and a multiple of
- *     8, up to 128 query heads per kv head, and 16-byte aligned pointers and strides of q and the caches; everything else
+ *   - The tensor-core kernel takes D <= 128 in multiples of 8, page_size a multiple of 64, or 8, 16 or 32, up to 128 query heads per kv head, and 16-byte aligned pointers and strides of q and the caches; everything else
  *     runs on a slower generic kernel.
  *   - workspace: 32-byte aligned device memory of at least specsteer_chunk_attention_workspace(desc) bytes, whose content
  *     before and after the call means nothing; calls that may overlap (two streams, two graphs) need one each.

@@ -9,9 +9,11 @@
 // cut needs nothing from the host: every CTA sums the lengths itself.  A unit that a cut goes through leaves partial
 // results (unnormalised sums, maximum and sum of weights per row) that attention_join_kernel puts together.
 //
-// Inside a CTA: warp 8 walks the list and issues the TMA loads (a ring of stages of one 128-key tile of K or V; a page or
-// its part of 128 keys is a box), warp 9 issues tcgen05.mma, warps 0..3 and 4..7 are two softmax groups (streams), one row
-// a thread.  Stream s has scores S_s (two blocks of 64 keys, 64 columns of tensor memory each, overwritten by the 16-bit
+// Inside a CTA: warps 8 and 9 issue the TMA loads of keys and of values, each into a ring of blocks of 64 keys (a page, or
+// its part of 64 keys, is a box; one warp for both could not issue the boxes of small pages fast enough), warp 8 also walks
+// the list; warps 0..3 and 4..7 are two softmax groups (streams), one row
+// a thread, and warps 10 and 11 issue the tcgen05.mma of one stream each (one warp for both spent its time on waits and
+// commits).  Stream s has scores S_s (two blocks of 64 keys, 64 columns of tensor memory each, overwritten by the 16-bit
 // weights P_s, which the second product reads from tensor memory) and sums O_s (128 columns).  The product that gives a
 // block's next scores is issued behind the one that takes its weights, so while a group weighs one block the tensor cores
 // work on the other.  With two query tiles each stream owns one and both use every key tile; with one query tile the
@@ -33,20 +35,23 @@ namespace specsteer {
 namespace {
 
 constexpr int kKeys = 128;          // keys per tile
+constexpr int kBlock = 64;          // keys per block: half a tile, what a barrier or a box covers
+constexpr int kMaxStages = 10;
 constexpr int kSoftmaxWarps = 8;
-constexpr int kProducerWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
-constexpr int kTcThreads = 32 * (kSoftmaxWarps + 2);
+constexpr int kKeyWarp = kSoftmaxWarps, kValueWarp = kSoftmaxWarps + 1, kMmaWarp = kSoftmaxWarps + 2;
+constexpr int kTcThreads = 32 * (kSoftmaxWarps + 4);
 constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
 constexpr int kPolyPairs = 0;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
 constexpr float kMostSum = 32768.f; // of the weights of a row and block before the reference is raised
 constexpr int kPieces = 4;          // pieces of work the producer may be ahead
 
 template <int DP> struct TcLayout {
-  static constexpr int kStageBytes = kKeys * DP * 2;
-  static constexpr int kStages = DP == 128 ? 5 : 12;
+  static constexpr int kStageBytes = kBlock * DP * 2;
+  static constexpr int kStages = DP == 128 ? 5 : 10;              // of each of the two rings
   static constexpr int kQBytes = 128 * DP * 2;
-  static constexpr int kRing = 2 * kQBytes;                       // offset of the ring behind the two query tiles
-  static constexpr int kControl = kRing + kStages * kStageBytes;  // offset of TcShared
+  static constexpr int kKeyRing = 2 * kQBytes;                    // offsets: two query tiles, the rings, TcShared
+  static constexpr int kValueRing = kKeyRing + kStages * kStageBytes;
+  static constexpr int kControl = kValueRing + kStages * kStageBytes;
 };
 
 // A piece of work: key tiles [first, first + take) of one unit (see Unit).
@@ -59,25 +64,21 @@ struct Piece {
   int first, take;             // take = 0: no more pieces
   int starts, ends;            // the piece holds the unit's first / last key tile
   int index;                   // of the pieces of this CTA
-  // Ring items: the keys of the first `ahead` tiles, then per tile its values and the keys `ahead` tiles on.
-  __device__ __forceinline__ int ahead() const { return min(two ? 1 : 2, take); }
-  __device__ __forceinline__ int item_of_v(int t) const { return ahead() + min(t, take - ahead()) + t; }
 };
 
 struct TcShared {
-  uint64_t full[12], empty[12];
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
   uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2][2], p_full[2][2];   // [s][h]: scores, weights of stream s, first / last 64 keys of a tile
-  uint64_t o_full, half_done[2];         // a piece's sums; those of the stream but for the last 64 keys
+  uint64_t o_full[2], half_done[2];      // a piece's sums; those of the stream but for the last 64 keys
   uint64_t piece_full[kPieces], piece_empty[kPieces];
-  uint64_t both, group[2], drain;
+  uint64_t both, group[2], drain[2];
   uint32_t tmem_slot;
-  int abort_flag;
   int nonfinite;           // an infinity or NaN was taken out of a tile of values
   int start_b, start_hk, start_u, start_off;
   long long end;           // where this CTA's range ends, from the beginning of its first unit (0: it has none)
   Piece piece[kPieces];
-  uint32_t bad[16];        // per key tile (counted modulo 16): the boxes of it that lie outside the pool
+  uint32_t bad[32];        // per block of keys (counted modulo 32): the boxes of it that lie outside the pool
   union {
     long long scan[kTcThreads / 32];
     float2 exch[2][128];   // reference and sum of each stream's rows
@@ -89,8 +90,8 @@ static_assert(tc_smem_bytes<128>() <= 232448 && tc_smem_bytes<64>() <= 232448, "
 struct TcParams {
   specsteer_attention_desc d;
   int G, box_tok, box_rows, tile_tok;  // query box: tokens and rows; tokens of a query tile
-  int page_rows, boxes, page_shift;    // key box: keys, boxes per key tile, log2 of its keys
-  int page_tiles;                      // key tiles per page (1 when a tile has several pages)
+  int page_rows, boxes, page_shift;    // key box: keys, boxes per block, log2 of its keys
+  int page_blocks;                     // blocks per page (1 when a block has several pages)
   float c;                             // scale * log2(e)
   int out_vec;                         // out rows are 32-byte aligned and a multiple of 32 bytes long
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
@@ -213,9 +214,9 @@ __device__ __forceinline__ void tm_st_wait() { asm volatile("tcgen05.wait::st.sy
 // Shared-memory descriptors of 128-byte swizzled operands, in units of 16 bytes: low words (address, leading offset); the
 // high word is the stride offset (groups of 8 rows 1024 bytes apart), the version 1 and the swizzle mode 2.  K and Q (rows
 // of 64 elements along the summed axis) have no leading offset (1); of V (the summed axis, keys, runs over the rows) it is
-// the distance of blocks of 64 columns, one chunk of 128 rows.
+// the distance of blocks of 64 columns, one chunk of 64 rows.
 __device__ __forceinline__ uint32_t desc_rows(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | (1u << 16); }
-__device__ __forceinline__ uint32_t desc_cols(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | ((uint32_t)((kKeys * 128) >> 4) << 16); }
+__device__ __forceinline__ uint32_t desc_cols(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | ((uint32_t)((kBlock * 128) >> 4) << 16); }
 // Instruction descriptor: float32 accumulator, operands bf16 or f16, M = 128.
 __device__ __forceinline__ uint32_t instr_desc(bool bf16, int n, bool b_by_columns) {
   const uint32_t f = bf16 ? 1u : 0u;
@@ -281,7 +282,6 @@ template <bool BF> __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t
   return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
 }
 
-__device__ __forceinline__ bool aborted(const TcShared* sh) { return *reinterpret_cast<const volatile int*>(&sh->abort_flag) != 0; }
 // One poll of a barrier's phase in the form without a time hint: the hardware parks the thread until the phase completes
 // or a time of its own has passed.  (With a hint the compiler makes a loop of naps of it, and a waiting warp wakes late.)
 __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
@@ -293,9 +293,9 @@ __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait of a whole warp (or, WARP false, of a single thread) for a phase of a barrier.  2^24 polls are a second or
-// much more, which no healthy run comes near.
-constexpr int kPolls = 1 << 24;
+// Bounded wait of a whole warp (or, WARP false, of a single thread) for a phase of a barrier.  2^21 polls are between
+// a twentieth of a second (if the hardware never parks the thread) and seconds; healthy waits are microseconds.
+constexpr int kPolls = 1 << 21;
 template <bool WARP> __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity) {
 #pragma unroll 1
   for (int n = kPolls; n > 0; --n) {
@@ -304,9 +304,10 @@ template <bool WARP> __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint
   }
   return false;
 }
-__device__ __noinline__ void give_up(TcShared* sh, int* status) {
-  *reinterpret_cast<volatile int*>(&sh->abort_flag) = 1;
-  if (status) atomicOr(status, SPECSTEER_REQ_TIMEOUT);
+
+// A wait ran out: say so (request 0 of the call) and leave; the other warps' waits run out too.
+__device__ __forceinline__ void gave_up(const TcParams& p) {
+  if (p.d.req_status) atomicOr(p.d.req_status, SPECSTEER_REQ_TIMEOUT);
 }
 
 // ---- units ----------------------------------------------------------------------------------------------------------
@@ -421,18 +422,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
   pdl_launch_dependents();   // attention_join_kernel may come up; it waits for the end of this kernel before it reads
   if (tid == 0) {
-    for (int i = 0; i < L::kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
+    for (int i = 0; i < L::kStages; ++i) {
+      mbar_init(&sh->k_full[i], 1); mbar_init(&sh->k_empty[i], 2);
+      mbar_init(&sh->v_full[i], 1); mbar_init(&sh->v_empty[i], 2);
+    }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 1);
+      mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 2);
       for (int h = 0; h < 2; ++h) { mbar_init(&sh->s_full[i][h], 1); mbar_init(&sh->p_full[i][h], 4); }
-      mbar_init(&sh->half_done[i], 1);
+      mbar_init(&sh->half_done[i], 1); mbar_init(&sh->o_full[i], 1);
       mbar_init(&sh->group[i], kSoftmaxWarps / 2);
     }
-    for (int i = 0; i < kPieces; ++i) { mbar_init(&sh->piece_full[i], 1); mbar_init(&sh->piece_empty[i], kSoftmaxWarps + 1); }
+    for (int i = 0; i < kPieces; ++i) { mbar_init(&sh->piece_full[i], 1); mbar_init(&sh->piece_empty[i], kSoftmaxWarps + 3); }
     mbar_init(&sh->both, kSoftmaxWarps);
-    mbar_init(&sh->o_full, 1);
-    mbar_init(&sh->drain, 1);
-    sh->abort_flag = 0;
+    for (int i = 0; i < 2; ++i) mbar_init(&sh->drain[i], 1);
     sh->nonfinite = 0;
     sh->end = 0;
     fence_barrier_init();
@@ -478,138 +480,138 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sh->tmem_slot);
 
-  if (warp == kProducerWarp) {
+  if (warp == kKeyWarp || warp == kValueWarp) {
     // ================= work list and TMA =================
-    const int chunks = DP / 64;
+    const bool keys = warp == kKeyWarp;
+    constexpr int chunks = DP / 64;
     const int box = lane / chunks, chunk = lane % chunks;
     const bool loads = box < p.boxes;
-    const uint32_t lane_off = smem0 + L::kRing + (uint32_t)chunk * (kKeys * 128) + (uint32_t)box * p.page_rows * 128;
-    int item = 0, st = 0, qi = 0, tiles = 0;   // st: stage of the item
+    const uint32_t lane_off = smem0 + (keys ? L::kKeyRing : L::kValueRing) + (uint32_t)chunk * (kBlock * 128) + (uint32_t)box * p.page_rows * 128;
+    const CUtensorMap* tm = keys ? &tm_k : &tm_v;
+    uint64_t* full = keys ? sh->k_full : sh->v_full;
+    uint64_t* empty = keys ? sh->k_empty : sh->v_empty;
+    int st = 0, blocks = 0, qi = 0, pc = 0;   // st: stage of the next block
     uint32_t st_phase = 1;
     bool ok = true;
     Walk w;
     w.begin(sh);
-    const int* table = nullptr;
-    // page of this lane's box of key tile t: the id, or n_pages (a coordinate outside, which reads zeros) for none
-    auto page_of = [&](int t) -> int {
-      const int key = t * kKeys + box * p.page_rows;
-      int page = p.d.n_pages;
-      if (loads && key < w.rq.kv) page = __ldg(table + (p.boxes > 1 ? t * p.boxes + box : t / p.page_tiles));
-      return page;
-    };
-    auto load_tile = [&](const CUtensorMap* tm, int t, int page) {
-      if (!ok) return;
-      ok = tc_wait<true>(&sh->empty[st], st_phase);
-      if (!ok) return;
-      if (lane == 0) mbar_arrive_expect_tx(&sh->full[st], L::kStageBytes);
-      __syncwarp();
-      if (loads)
-        tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, p.page_tiles > 1 ? t % p.page_tiles * kKeys : 0, w.hk,
-               (page < 0 || page >= p.d.n_pages) ? p.d.n_pages : page, &sh->full[st]);
-      ++item;
-      if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
-    };
-    auto load_k = [&](int t, int page) {
-      const bool outside = loads && t * kKeys + box * p.page_rows < w.rq.kv && (page < 0 || page >= p.d.n_pages);
-      const uint32_t votes = __ballot_sync(kFullMask, outside);
-      if (lane == 0) {
-        uint32_t bad = 0;
-        if (votes) {
-          for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (i * chunks)) & 1u) << i;
-          if (p.d.req_status) atomicOr(p.d.req_status + w.b, SPECSTEER_REQ_BAD_PAGE);
-        }
-        // the word is read by the softmax warps up to a ring's length of tiles later, well under 16
-        *reinterpret_cast<volatile uint32_t*>(&sh->bad[tiles & 15]) = bad;
-      }
-      ++tiles;
-      load_tile(&tm_k, t, page);
-    };
-    int pc = 0;
 #pragma unroll 1
     for (;; ++pc) {
-      w.load(p);
-      ok = tc_wait<true>(&sh->piece_empty[pc % kPieces], (uint32_t)((pc / kPieces) & 1) ^ 1u);
-      if (!ok) break;
-      if (lane == 0) {
-        if (w.take > 0) w.publish(&sh->piece[pc % kPieces]);
-        else sh->piece[pc % kPieces].take = 0;
-        mbar_arrive(&sh->piece_full[pc % kPieces]);
+      Piece* const x = &sh->piece[pc % kPieces];
+      const uint32_t turn = (uint32_t)((pc / kPieces) & 1);
+      if (keys) {
+        w.load(p);
+        ok = tc_wait<true>(&sh->piece_empty[pc % kPieces], turn ^ 1u);
+        if (!ok) break;
+        if (lane == 0) {
+          if (w.take > 0) w.publish(x);
+          else x->take = 0;
+          mbar_arrive(&sh->piece_full[pc % kPieces]);
+        }
+        __syncwarp();
+      } else {
+        ok = tc_wait<true>(&sh->piece_full[pc % kPieces], turn);
+        if (!ok) break;
       }
-      __syncwarp();
-      if (w.take <= 0) break;
-      table = p.d.block_table + (long long)w.b * p.d.ld_table;
-      const int first = w.x.t0 + w.off, take = w.take, ahead = min(w.x.two ? 1 : 2, take);
-      int pg0 = page_of(first), pg1 = take > 1 ? page_of(first + 1) : 0, pg2 = take > 2 ? page_of(first + 2) : 0;
+      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, n_blocks = 2 * take;
+      if (take <= 0) break;
+      const int n_q = !keys ? 0 : x->two ? 2 : 1;
+      const int* table = p.d.block_table + (long long)b * p.d.ld_table;
+      // page of this lane's box of block j of the piece: the id, or n_pages (a coordinate outside, which reads zeros) for none
+      auto page_of = [&](int j) -> int {
+        int page = p.d.n_pages;
+        if (loads && j < n_blocks && (first + j) * kBlock + box * p.page_rows < kv)
+          page = __ldg(table + (p.boxes > 1 ? (first + j) * p.boxes + box : (first + j) / p.page_blocks));
+        return page;
+      };
+      int page = page_of(0), page1 = page_of(1), page2 = page_of(2), q_done = 0;
 #pragma unroll 1
-      for (int t = -ahead; t < take && ok; ++t) {
-        // values of tile t, then keys of tile t + ahead; the queries behind the first keys, whose stages are free sooner
+      for (int j = 0; j < n_blocks; ++j) {
+        // The queries go behind the first keys, whose stages are free sooner: once their place is, or at the latest when the
+        // ring may be full of keys that wait for them.
 #pragma unroll 1
-        for (int s = 0; t == 0 && s < (w.x.two ? 2 : 1) && ok; ++s, ++qi) {
+        while (j > 0 && q_done < n_q && ok) {
           const int slot = qi & 1;
-          ok = tc_wait<true>(&sh->q_empty[slot], (uint32_t)((qi >> 1) & 1) ^ 1u);
+          const uint32_t q_turn = (uint32_t)((qi >> 1) & 1) ^ 1u;
+          if (j < L::kStages && j + 1 < n_blocks && !__all_sync(kFullMask, mbar_test_nonblocking(&sh->q_empty[slot], q_turn))) break;
+          ok = tc_wait<true>(&sh->q_empty[slot], q_turn);
           if (!ok) break;
-          const int tok = w.x.tok0 + s * p.tile_tok, cnt = min(p.tile_tok, w.x.tok1 - tok);
+          const int tok = x->tok0 + q_done * p.tile_tok, cnt = min(p.tile_tok, x->tok1 - tok);
           const int nb = (cnt + p.box_tok - 1) / p.box_tok;
           if (lane == 0) mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
           __syncwarp();
           if (box < nb)
-            tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + box * p.box_rows * 128, &tm_q, chunk * 64, w.hk * p.G,
-                   w.rq.row0 + tok + box * p.box_tok, &sh->q_full[slot]);
+            tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + box * p.box_rows * 128, &tm_q, chunk * 64, hk * p.G,
+                   x->row0 + tok + box * p.box_tok, &sh->q_full[slot]);
+          ++qi;
+          ++q_done;
         }
         if (!ok) break;
-        const int pg3 = t >= 0 && t + 3 < take ? page_of(first + t + 3) : 0;
-        if (t >= 0) load_tile(&tm_v, first + t, pg0);
-        if (t + ahead < take && ok) load_k(first + t + ahead, t + ahead == 0 ? pg0 : (t + ahead == 1 && t < 0) || ahead == 1 ? pg1 : pg2);
-        if (t >= 0) { pg0 = pg1; pg1 = pg2; pg2 = pg3; }
+        const bool outside = page < 0 || page >= p.d.n_pages;
+        if (keys) {
+          const uint32_t votes = __ballot_sync(kFullMask, loads && outside && (first + j) * kBlock + box * p.page_rows < kv);
+          if (lane == 0) {
+            uint32_t bad = 0;
+            if (votes) {
+#pragma unroll 1
+              for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (i * chunks)) & 1u) << i;
+              if (p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_PAGE);
+            }
+            // the softmax warps read the word at most the ring and the blocks in work later, well under 32
+            *reinterpret_cast<volatile uint32_t*>(&sh->bad[blocks & 31]) = bad;
+          }
+        }
+        const int page3 = page_of(j + 3);
+        ok = tc_wait<true>(&empty[st], st_phase);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&full[st], L::kStageBytes);
+        __syncwarp();
+        if (loads)
+          tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, p.page_blocks > 1 ? (first + j) % p.page_blocks * kBlock : 0, hk,
+                 outside ? p.d.n_pages : page, &full[st]);
+        ++blocks;
+        if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
+        page = page1; page1 = page2; page2 = page3;
       }
       if (!ok) break;
-      w.next(p);
+      if (keys) w.next(p);
+      else if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
     }
     if (!ok && lane == 0) {
-      give_up(sh, p.d.req_status ? p.d.req_status + w.b : nullptr);
+      gave_up(p);
       // copies already issued may still be landing: wait for them (bounded) before the CTA exits
-      for (int i = item > L::kStages ? item - L::kStages : 0; i < item; ++i) tc_wait<false>(&sh->full[i % L::kStages], (uint32_t)((i / L::kStages) & 1));
+      for (int i = blocks > L::kStages ? blocks - L::kStages : 0; i < blocks; ++i) tc_wait<false>(&full[i % L::kStages], (uint32_t)((i / L::kStages) & 1));
       for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_wait<false>(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1));
     }
-  } else if (warp == kMmaWarp) {
-    // ================= tensor-core issuer =================
+  } else if (warp >= kMmaWarp) {
+    // ================= tensor-core issuers, one a stream =================
     // The whole warp runs the loop, so that addresses and descriptors stay in uniform registers.
     // All columns were allocated, so tensor memory begins at column 0.
-    constexpr uint32_t t_base = 0;
-    const uint32_t id_qk = instr_desc(BF, 64, false), id_pv = instr_desc(BF, DP, true);
-    int st = 0, qi = 0, pc = 0, b = 0;   // st: stage of the next ring item
-    uint32_t st_phase = 0, p_phase = 0;  // p_phase: bit 2 s + h, of the weights of block h of stream s
+    const int s = warp - kMmaWarp;
+    const uint32_t t_s = s * 128, t_o = 256 + s * 128;
+    const uint32_t id_qk = instr_desc(BF, kBlock, false), id_pv = instr_desc(BF, DP, true);
+    int qi = 0, pc = 0, blocks0 = 0;
+    uint32_t p_phase = 0;
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (ok) ok = tc_wait<true>(bar, parity);
       fence_after();
     };
-    // the next ring item has landed; its stage
-    auto item = [&]() -> int {
-      wait(&sh->full[st], st_phase);
-      const int got = st;
-      if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
-      return got;
-    };
-    // Scores of block h of stream s.  The commit also says that the product with the block's values before it is complete.
-    auto scores = [&](int s, int h, int slot, int stage) {
-      if (!ok) return;
-      const uint32_t a = desc_rows(smem0 + slot * L::kQBytes), b = desc_rows(smem0 + L::kRing + stage * L::kStageBytes) + h * (64 * 128 >> 4);
-#pragma unroll
-      for (int k = 0; k < DP / 16; ++k) {
-        const uint32_t step = (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2);
-        mma_ss(t_base + s * 128 + h * 64, a + step, b + step, id_qk, k != 0);
+    // Block `it` of a ring.  Both issuers pass over every block in order, so that neither can mistake a phase of a barrier for
+    // one two uses later: a block of the other stream's tile is let go as soon as it has landed.
+    int k_next = 0, v_next = 0;
+    auto pass = [&](uint64_t* full, uint64_t* empty, int& next, int until) {
+#pragma unroll 1
+      for (; next < until && ok; ++next) {
+        wait(&full[next % L::kStages], (uint32_t)((next / L::kStages) & 1));
+        if (ok && lane == 0) mbar_arrive(&empty[next % L::kStages]);
+        __syncwarp();
       }
-      mma_commit(&sh->s_full[s][h]);
     };
-    auto values = [&](int s, int h, int stage, bool accumulate) {
-      const uint32_t b = desc_cols(smem0 + L::kRing + stage * L::kStageBytes) + h * (64 * 128 >> 4);
-      wait(&sh->p_full[s][h], (p_phase >> (2 * s + h)) & 1u);
-      p_phase ^= 1u << (2 * s + h);
-      if (!ok) return;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        mma_ts(t_base + 256 + s * 128, t_base + s * 128 + h * 64 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, k != 0 || accumulate);
+    auto reach = [&](uint64_t* full, uint64_t* empty, int& next, int it) {
+      pass(full, empty, next, it);
+      wait(&full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
+      next = it + 1;
     };
 #pragma unroll 1
     for (;; ++pc) {
@@ -617,49 +619,64 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!ok) break;
       const Piece* q = &sh->piece[pc % kPieces];
       // (through a reduction, whose result the compiler knows to be the same in the whole warp)
-      const int take = __reduce_max_sync(kFullMask, q->take), two = __reduce_max_sync(kFullMask, q->two), ahead = min(two ? 1 : 2, take);
-      b = q->b;
+      const int take = __reduce_max_sync(kFullMask, q->take), two = __reduce_max_sync(kFullMask, q->two);
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
       if (take <= 0) break;
-      const int q0 = qi & 1, q1 = two ? q0 ^ 1 : q0;
-      wait(&sh->q_full[q0], (uint32_t)((qi >> 1) & 1));
-      if (two) wait(&sh->q_full[q1], (uint32_t)(((qi + 1) >> 1) & 1));
-      // t < 0: keys of the first tiles only
+      const int qs = two ? (qi + s) & 1 : qi & 1;
+      // both tiles if there are two, so that no phase of either barrier is passed unseen
+      wait(&sh->q_full[qi & 1], (uint32_t)((qi >> 1) & 1));
+      if (two) wait(&sh->q_full[(qi + 1) & 1], (uint32_t)(((qi + 1) >> 1) & 1));
+      const int step = two ? 1 : 2, t_from = two ? 0 : s;
+      const uint32_t q_desc = desc_rows(smem0 + qs * L::kQBytes);
+      // Scores of block h of tile t.  The commit also says that the product with the block's values before it is complete.
+      auto scores = [&](int t, int h) {
+        const int it = blocks0 + 2 * t + h, stage = it % L::kStages;
+        reach(sh->k_full, sh->k_empty, k_next, it);
+        if (!ok) return;
+        const uint32_t b = desc_rows(smem0 + L::kKeyRing + stage * L::kStageBytes);
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+          mma_ss(t_s + h * 64, q_desc + (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2), b + (uint32_t)((k >> 2) * ((kBlock * 128) >> 4) + (k & 3) * 2),
+                 id_qk, k != 0);
+        mma_commit(&sh->s_full[s][h]);
+        mma_commit(&sh->k_empty[stage]);
+      };
 #pragma unroll 1
-      for (int t = -ahead; t < take && ok; ++t) {
-        const bool next_k = t + ahead < take;
-        const int v = t >= 0 ? item() : 0;
-        int k = 0;
-        // the streams of tile t, which are those of tile t + ahead if there is one
-        const int s0 = two ? 0 : (t >= 0 ? t : t + ahead) & 1, s1 = two ? 1 : s0;
+      for (int t = t_from - step; t < take && ok; t += step) {   // the first turn forms the first scores alone
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll 1
-          for (int s = s0; s <= s1; ++s) {
-            if (t >= 0) values(s, h, v, t >= ahead || h > 0);
-            if (next_k) {
-              if (h == 0 && s == s0) k = item();
-              scores(s, h, s ? q1 : q0, k);
-            } else if (h == 0 && ok) {
-              mma_commit(&sh->half_done[s]);
-            }
+        for (int h = 0; h < 2 && ok; ++h) {
+          const int it = blocks0 + 2 * t + h, stage = it % L::kStages;
+          if (t >= t_from) {
+            reach(sh->v_full, sh->v_empty, v_next, it);
+            wait(&sh->p_full[s][h], (p_phase >> h) & 1u);
+            p_phase ^= 1u << h;
+            if (!ok) break;
+            const uint32_t b = desc_cols(smem0 + L::kValueRing + stage * L::kStageBytes);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_ts(t_o, t_s + h * 64 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, k != 0 || t > t_from || h > 0);
           }
+          if (t + step < take) scores(t + step, h);
+          else if (h == 0 && t >= t_from) mma_commit(&sh->half_done[s]);
+          if (t >= t_from && ok) mma_commit(&sh->v_empty[stage]);
         }
-        if (t >= 0 && ok) mma_commit(&sh->empty[v]);
-        if (next_k && ok) mma_commit(&sh->empty[k]);
       }
       if (!ok) break;
-      mma_commit(&sh->o_full);
-      mma_commit(&sh->q_empty[q0]);
-      if (two) mma_commit(&sh->q_empty[q1]);
+      // (a stream that had no tile says nothing: it could come by twice before anybody looks)
+      if (t_from < take) mma_commit(&sh->o_full[s]);
+      mma_commit(&sh->q_empty[qs]);
+      if (two) mma_commit(&sh->q_empty[qs]);   // (its barrier counts both issuers, and this tile is the stream's alone)
       qi += two ? 2 : 1;
+      blocks0 += 2 * take;
+      pass(sh->k_full, sh->k_empty, k_next, blocks0);   // what the other stream had last
+      pass(sh->v_full, sh->v_empty, v_next, blocks0);
     }
     if (!ok) {   // let everything issued finish before tensor memory is given back
-      if (lane == 0) give_up(sh, p.d.req_status ? p.d.req_status + b : nullptr);
+      if (lane == 0) gave_up(p);
       __syncwarp();
-      mma_commit(&sh->drain);
-      tc_wait<true>(&sh->drain, 0);
+      mma_commit(&sh->drain[s]);
+      tc_wait<true>(&sh->drain[s], 0);
     }
   } else {
     // ================= softmax: one row a thread =================
@@ -668,14 +685,15 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
     const int r_tok = r / p.G, r_head = r - r_tok * p.G;
     const float c = p.c;
+    uint32_t o_phase = 0;                   // bit s: of stream s
     uint32_t s_phase = 0, half_phase = 0;   // s_phase: of both blocks at the beginning of a tile
     uint32_t group_phase = 0, both_phase = 0;
-    int item0 = 0, tiles0 = 0, pc = 0, b = 0;
+    int blocks0 = 0, pc = 0;     // blocks0: of the pieces before
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (ok && !tc_wait<true>(bar, parity)) {
         ok = false;
-        if (lane == 0) give_up(sh, p.d.req_status ? p.d.req_status + b : nullptr);
+        if (lane == 0) gave_up(p);
       }
       fence_after();
     };
@@ -701,7 +719,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const Piece& x = sh->piece[pc % kPieces];
       const int take = x.take, two = x.two, first = x.first;
       if (take <= 0) break;
-      b = x.b;
       const int tok = x.tok0 + (two ? s * p.tile_tok : 0) + r_tok;
       const bool live = r_tok < p.tile_tok && tok < x.tok1;
       const bool warp_live = __any_sync(kFullMask, live);
@@ -715,58 +732,56 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const int step = two ? 1 : 2, t_from = two ? 0 : s;
 #pragma unroll 1
       for (int t = t_from; t < take; t += step) {
-        const int k0 = (first + t) * kKeys;
-        wait(&sh->s_full[s][0], s_phase);   // the tile's keys have landed, and what was loaded before them
-        if (!ok) break;
-        const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(tiles0 + t) & 15]);
-        const bool edge = k0 + kKeys > hi_first || k0 < lo_last || bad != 0;
-        if (edge) {
-          // Values of keys that some row of the unit does not see.  What lies behind the last key in its page becomes zero
-          // (whole pages behind it, and pages outside the pool, were loaded as zeros); an infinity or NaN among the others is
-          // taken out here, where it would reach rows with weight 0, and added in the epilogue to the rows that see it.
-          const int it = item0 + x.item_of_v(t);
-          wait(&sh->full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
-          if (!ok) break;
-          unsigned char* vt = smem_raw + L::kRing + (it % L::kStages) * L::kStageBytes;
-          const int kv_here = min(kKeys, x.kv - k0);
-          const int from = min(kv_here, max(0, lo_last - k0)), to = min(kv_here, max(from, hi_first - k0));
-          const int zero_to = min(kKeys, (kv_here + p.page_rows - 1) & -p.page_rows);
-          auto vector = [&](int j, int vec) {
-            return reinterpret_cast<uint4*>(vt + (vec >> 3) * (kKeys * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
-          };
-          // two query tiles: the groups share the work
-          const int me = two ? tid : tid & 127, team = two ? 256 : 128;
-          constexpr int kVec = DP / 8;
-#pragma unroll 1
-          for (int e = kv_here * kVec + me; e < zero_to * kVec; e += team) *vector(e / kVec, e % kVec) = make_uint4(0u, 0u, 0u, 0u);
-          const int n_vec = (from + (kv_here - to)) * kVec;          // of keys [0, from) and [to, kv)
-          bool found = false;
-#pragma unroll 2
-          for (int e = me; e < n_vec; e += team) {
-            const int j = e / kVec;
-            const uint4 y = *vector(j < from ? j : j - from + to, e % kVec);
-            found = found || (nonfinite_halves<BF>(y.x) | nonfinite_halves<BF>(y.y) | nonfinite_halves<BF>(y.z) | nonfinite_halves<BF>(y.w));
-          }
-          if (found) *reinterpret_cast<volatile int*>(&sh->nonfinite) = 1;
-          fence_async_proxy();
-          meet(two);   // everybody has looked before anything is taken out
-          if (!ok) break;
-          if (*reinterpret_cast<volatile int*>(&sh->nonfinite)) {   // (or in an earlier tile: then there is nothing to find)
-#pragma unroll 1
-            for (int e = tid & 127; e < n_vec; e += 128) {
-              const int j = e / kVec;
-              uint4* at = vector(j < from ? j : j - from + to, e % kVec);
-              const uint4 y = *at;
-              const uint32_t n0 = nonfinite_halves<BF>(y.x), n1 = nonfinite_halves<BF>(y.y), n2 = nonfinite_halves<BF>(y.z), n3 = nonfinite_halves<BF>(y.w);
-              if (n0 | n1 | n2 | n3) *at = make_uint4(y.x & ~n0, y.y & ~n1, y.z & ~n2, y.w & ~n3);
-            }
-            fence_async_proxy();
-          }
-        }
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
-          if (h) wait(&sh->s_full[s][1], s_phase);
+          const int k0 = (first + t) * kKeys + h * kBlock;
+          wait(&sh->s_full[s][h], s_phase);   // the block's keys have landed, and what was loaded before them
           if (!ok) break;
+          const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(blocks0 + 2 * t + h) & 31]);
+          const bool edge = k0 + kBlock > hi_first || k0 < lo_last || bad != 0;
+          if (edge) {
+            // Values of keys that some row of the unit does not see.  What lies behind the last key in its page becomes zero
+            // (whole pages behind it, and pages outside the pool, were loaded as zeros); an infinity or NaN among the others is
+            // taken out here, where it would reach rows with weight 0, and added in the epilogue to the rows that see it.
+            const int it = blocks0 + 2 * t + h;
+            wait(&sh->v_full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
+            if (!ok) break;
+            unsigned char* vt = smem_raw + L::kValueRing + (it % L::kStages) * L::kStageBytes;
+            const int kv_here = min(kBlock, max(0, x.kv - k0));
+            const int from = min(kv_here, max(0, lo_last - k0)), to = min(kv_here, max(from, hi_first - k0));
+            const int zero_to = min(kBlock, (kv_here + p.page_rows - 1) & -p.page_rows);
+            auto vector = [&](int j, int vec) {
+              return reinterpret_cast<uint4*>(vt + (vec >> 3) * (kBlock * 128) + j * 128 + (((vec & 7) ^ (j & 7)) << 4));
+            };
+            // two query tiles: the groups share the work
+            const int me = two ? tid : tid & 127, team = two ? 256 : 128;
+            constexpr int kVec = DP / 8;
+#pragma unroll 1
+            for (int e = kv_here * kVec + me; e < zero_to * kVec; e += team) *vector(e / kVec, e % kVec) = make_uint4(0u, 0u, 0u, 0u);
+            const int n_vec = (from + (kv_here - to)) * kVec;          // of keys [0, from) and [to, kv)
+            bool found = false;
+#pragma unroll 2
+            for (int e = me; e < n_vec; e += team) {
+              const int j = e / kVec;
+              const uint4 y = *vector(j < from ? j : j - from + to, e % kVec);
+              found = found || (nonfinite_halves<BF>(y.x) | nonfinite_halves<BF>(y.y) | nonfinite_halves<BF>(y.z) | nonfinite_halves<BF>(y.w));
+            }
+            if (found) *reinterpret_cast<volatile int*>(&sh->nonfinite) = 1;
+            fence_async_proxy();
+            meet(two);   // everybody has looked before anything is taken out
+            if (!ok) break;
+            if (*reinterpret_cast<volatile int*>(&sh->nonfinite)) {   // (or in an earlier tile: then there is nothing to find)
+#pragma unroll 1
+              for (int e = tid & 127; e < n_vec; e += 128) {
+                const int j = e / kVec;
+                uint4* at = vector(j < from ? j : j - from + to, e % kVec);
+                const uint4 y = *at;
+                const uint32_t n0 = nonfinite_halves<BF>(y.x), n1 = nonfinite_halves<BF>(y.y), n2 = nonfinite_halves<BF>(y.z), n3 = nonfinite_halves<BF>(y.w);
+                if (n0 | n1 | n2 | n3) *at = make_uint4(y.x & ~n0, y.y & ~n1, y.z & ~n2, y.w & ~n3);
+              }
+              fence_async_proxy();
+            }
+          }
           if (warp_live) {
             float v[64];
             tm_ld32(t_s + h * 64, v);
@@ -777,12 +792,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
               for (int i = 0; i < 64; i += 32) {
                 // the columns of 32 that the row sees, as bits
-                const int j0 = h * 64 + i, from = max(lo - k0 - j0, 0), to = min(hi - k0 - j0, 32);
+                const int from = max(lo - k0 - i, 0), to = min(hi - k0 - i, 32);
                 uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
                 if (bad) {
 #pragma unroll 1
                   for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
-                    if ((bad >> ((j0 + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
+                    if ((bad >> ((i + j) >> p.page_shift)) & 1u) keep &= ~(0xffu << j);
                 }
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[i + j] = (keep & (1u << j)) ? v[i + j] : kNegInf;
@@ -861,7 +876,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const int n1 = two ? take : take / 2;   // tiles of the second stream
       const bool whole = x.starts && x.ends;
       const int slot = 2 * blockIdx.x + (x.index == 0 ? 0 : 1);
-      wait(&sh->o_full, (uint32_t)pc & 1u);
+      // the sums of the stream, with one query tile of both (if the second had a tile)
+      if (s == 0 || !two) wait(&sh->o_full[0], o_phase & 1u);
+      if (n1 > 0 && (s == 1 || !two)) wait(&sh->o_full[1], o_phase >> 1);
+      o_phase ^= n1 > 0 ? 3u : 1u;
       if (!ok) break;
       if (m == kNegInf && l == l) l = 0.f;   // no key, or only scores of -inf: nothing was weighed
       float f0 = 1.f, f1 = 1.f;
@@ -953,8 +971,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         else h[1] = x.ends ? 1 : 2;
       }
       if (!two) meet(true);   // both halves of the sums are read before either stream goes on
-      item0 += 2 * take;
-      tiles0 += take;
+      blocks0 += 2 * take;
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
     }
@@ -1112,8 +1129,8 @@ bool attention_tc_takes(const specsteer_attention_desc* d) {
   auto a16 = [](const void* q) { return ((uintptr_t)q & 15u) == 0; };
   // strides of axes longer than one: positive multiples of 16 bytes below the tensor map's limit
   auto ok = [](long long stride, long long extent) { return extent <= 1 || (stride > 0 && stride % 8 == 0 && stride < (1ll << 38)); };
-  const int pr = d->page_size < kKeys ? d->page_size : kKeys;
-  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->D >= 64 && d->D <= 128 && d->D % 8 == 0 && pr % 8 == 0 && kKeys % pr == 0 && d->page_size % pr == 0 &&
+  const int pr = d->page_size < kBlock ? d->page_size : kBlock;
+  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->D >= 64 && d->D <= 128 && d->D % 8 == 0 && pr % 8 == 0 && kBlock % pr == 0 && d->page_size % pr == 0 &&
          query_box(d->Hq / d->Hkv, &tok, &boxes) && a16(d->q) && a16(d->k_cache) && a16(d->v_cache) && ok(d->q_tok, d->T) && ok(d->q_head, d->Hq) &&
          ok(d->kc_page, d->n_pages) && ok(d->kc_slot, d->page_size) && ok(d->kc_head, d->Hkv) && ok(d->vc_page, d->n_pages) &&
          ok(d->vc_slot, d->page_size) && ok(d->vc_head, d->Hkv);
@@ -1133,9 +1150,9 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   query_box(p.G, &p.box_tok, &boxes);
   p.box_rows = p.box_tok * p.G;
   p.tile_tok = boxes * p.box_tok;
-  p.page_rows = d->page_size < kKeys ? d->page_size : kKeys;
-  p.boxes = kKeys / p.page_rows;
-  p.page_tiles = d->page_size / p.page_rows;
+  p.page_rows = d->page_size < kBlock ? d->page_size : kBlock;
+  p.boxes = kBlock / p.page_rows;
+  p.page_blocks = d->page_size / p.page_rows;
   p.page_shift = 0;
   while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
   p.c = d->scale * kLog2e;
