@@ -296,17 +296,18 @@ __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
 // Bounded wait of a whole warp (or, WARP false, of a single thread) for a phase of a barrier.  2^21 polls are between
 // a twentieth of a second (if the hardware never parks the thread) and seconds; healthy waits are microseconds.
 constexpr int kPolls = 1 << 21;
-template <bool WARP> __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity) {
+// A warp's waits share a limit: once one has run out, the later ones do not wait any more.  Products and weights then go on
+// over whatever there is, every access in its place, to the end of the piece, where the warp leaves.
+template <bool WARP> __device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, int& limit) {
+  int n = limit;
 #pragma unroll 1
-  for (int n = kPolls; n > 0; --n) {
+  for (;;) {
     const bool got = poll(bar, parity);
-    if (WARP ? __all_sync(kFullMask, got) : got) return true;
+    if (WARP ? __all_sync(kFullMask, got) : got) break;
+    if (--n <= 0) { limit = 0; break; }
   }
-  return false;
 }
-
-// A wait ran out: say so (request 0 of the call) and leave; the other warps' waits run out too.
-__device__ __forceinline__ void gave_up(const TcParams& p) {
+__device__ __forceinline__ void gave_up(const TcParams& p) {   // said of request 0 of the call
   if (p.d.req_status) atomicOr(p.d.req_status, SPECSTEER_REQ_TIMEOUT);
 }
 
@@ -492,7 +493,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint64_t* empty = keys ? sh->k_empty : sh->v_empty;
     int st = 0, blocks = 0, qi = 0, pc = 0;   // st: stage of the next block
     uint32_t st_phase = 1;
-    bool ok = true;
+    int limit = kPolls;
     Walk w;
     w.begin(sh);
 #pragma unroll 1
@@ -501,8 +502,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const uint32_t turn = (uint32_t)((pc / kPieces) & 1);
       if (keys) {
         w.load(p);
-        ok = tc_wait<true>(&sh->piece_empty[pc % kPieces], turn ^ 1u);
-        if (!ok) break;
+        tc_wait<true>(&sh->piece_empty[pc % kPieces], turn ^ 1u, limit);
+        if (limit == 0) break;
         if (lane == 0) {
           if (w.take > 0) w.publish(x);
           else x->take = 0;
@@ -510,8 +511,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         __syncwarp();
       } else {
-        ok = tc_wait<true>(&sh->piece_full[pc % kPieces], turn);
-        if (!ok) break;
+        tc_wait<true>(&sh->piece_full[pc % kPieces], turn, limit);
+        if (limit == 0) break;
       }
       const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, n_blocks = 2 * take;
       if (take <= 0) break;
@@ -530,12 +531,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         // The queries go behind the first keys, whose stages are free sooner: once their place is, or at the latest when the
         // ring may be full of keys that wait for them.
 #pragma unroll 1
-        while (j > 0 && q_done < n_q && ok) {
+        while (j > 0 && q_done < n_q && limit) {
           const int slot = qi & 1;
           const uint32_t q_turn = (uint32_t)((qi >> 1) & 1) ^ 1u;
           if (j < L::kStages && j + 1 < n_blocks && !__all_sync(kFullMask, mbar_test_nonblocking(&sh->q_empty[slot], q_turn))) break;
-          ok = tc_wait<true>(&sh->q_empty[slot], q_turn);
-          if (!ok) break;
+          tc_wait<true>(&sh->q_empty[slot], q_turn, limit);
+          if (limit == 0) break;
           const int tok = x->tok0 + q_done * p.tile_tok, cnt = min(p.tile_tok, x->tok1 - tok);
           const int nb = (cnt + p.box_tok - 1) / p.box_tok;
           if (lane == 0) mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
@@ -546,7 +547,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           ++qi;
           ++q_done;
         }
-        if (!ok) break;
+        if (limit == 0) break;
         const bool outside = page < 0 || page >= p.d.n_pages;
         if (keys) {
           const uint32_t votes = __ballot_sync(kFullMask, loads && outside && (first + j) * kBlock + box * p.page_rows < kv);
@@ -562,8 +563,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
         }
         const int page3 = page_of(j + 3);
-        ok = tc_wait<true>(&empty[st], st_phase);
-        if (!ok) break;
+        tc_wait<true>(&empty[st], st_phase, limit);
+        if (limit == 0) break;
         if (lane == 0) mbar_arrive_expect_tx(&full[st], L::kStageBytes);
         __syncwarp();
         if (loads)
@@ -573,15 +574,16 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
         page = page1; page1 = page2; page2 = page3;
       }
-      if (!ok) break;
+      if (limit == 0) break;
       if (keys) w.next(p);
       else if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
     }
-    if (!ok && lane == 0) {
+    if (limit == 0 && lane == 0) {
       gave_up(p);
+      limit = kPolls;
       // copies already issued may still be landing: wait for them (bounded) before the CTA exits
-      for (int i = blocks > L::kStages ? blocks - L::kStages : 0; i < blocks; ++i) tc_wait<false>(&full[i % L::kStages], (uint32_t)((i / L::kStages) & 1));
-      for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_wait<false>(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1));
+      for (int i = blocks > L::kStages ? blocks - L::kStages : 0; i < blocks; ++i) tc_wait<false>(&full[i % L::kStages], (uint32_t)((i / L::kStages) & 1), limit);
+      for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_wait<false>(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1), limit);
     }
   } else if (warp >= kMmaWarp) {
     // ================= tensor-core issuers, one a stream =================
@@ -592,31 +594,24 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t id_qk = instr_desc(BF, kBlock, false), id_pv = instr_desc(BF, DP, true);
     int qi = 0, pc = 0, blocks0 = 0;
     uint32_t p_phase = 0;
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok) ok = tc_wait<true>(bar, parity);
-      fence_after();
-    };
+    int limit = kPolls;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { tc_wait<true>(bar, parity, limit); };
     // Block `it` of a ring.  Both issuers pass over every block in order, so that neither can mistake a phase of a barrier for
     // one two uses later: a block of the other stream's tile is let go as soon as it has landed.
     int k_next = 0, v_next = 0;
     auto pass = [&](uint64_t* full, uint64_t* empty, int& next, int until) {
 #pragma unroll 1
-      for (; next < until && ok; ++next) {
+      for (; next < until; ++next) {
         wait(&full[next % L::kStages], (uint32_t)((next / L::kStages) & 1));
-        if (ok && lane == 0) mbar_arrive(&empty[next % L::kStages]);
+        if (lane == 0) mbar_arrive(&empty[next % L::kStages]);
         __syncwarp();
       }
-    };
-    auto reach = [&](uint64_t* full, uint64_t* empty, int& next, int it) {
-      pass(full, empty, next, it);
-      wait(&full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
-      next = it + 1;
+      next = until + 1;
     };
 #pragma unroll 1
     for (;; ++pc) {
       wait(&sh->piece_full[pc % kPieces], (uint32_t)((pc / kPieces) & 1));
-      if (!ok) break;
+      if (limit == 0) break;
       const Piece* q = &sh->piece[pc % kPieces];
       // (through a reduction, whose result the compiler knows to be the same in the whole warp)
       const int take = __reduce_max_sync(kFullMask, q->take), two = __reduce_max_sync(kFullMask, q->two);
@@ -629,40 +624,42 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (two) wait(&sh->q_full[(qi + 1) & 1], (uint32_t)(((qi + 1) >> 1) & 1));
       const int step = two ? 1 : 2, t_from = two ? 0 : s;
       const uint32_t q_desc = desc_rows(smem0 + qs * L::kQBytes);
-      // Scores of block h of tile t.  The commit also says that the product with the block's values before it is complete.
-      auto scores = [&](int t, int h) {
-        const int it = blocks0 + 2 * t + h, stage = it % L::kStages;
-        reach(sh->k_full, sh->k_empty, k_next, it);
-        if (!ok) return;
-        const uint32_t b = desc_rows(smem0 + L::kKeyRing + stage * L::kStageBytes);
+#pragma unroll 1
+      for (int t = t_from - step; t < take; t += step) {   // the first turn forms the first scores alone
+        const bool now = t >= t_from, next = t + step < take;
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          mma_ss(t_s + h * 64, q_desc + (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2), b + (uint32_t)((k >> 2) * ((kBlock * 128) >> 4) + (k & 3) * 2),
-                 id_qk, k != 0);
-        mma_commit(&sh->s_full[s][h]);
-        mma_commit(&sh->k_empty[stage]);
-      };
-#pragma unroll 1
-      for (int t = t_from - step; t < take && ok; t += step) {   // the first turn forms the first scores alone
-#pragma unroll 1
-        for (int h = 0; h < 2 && ok; ++h) {
+        for (int h = 0; h < 2; ++h) {
           const int it = blocks0 + 2 * t + h, stage = it % L::kStages;
-          if (t >= t_from) {
-            reach(sh->v_full, sh->v_empty, v_next, it);
-            wait(&sh->p_full[s][h], (p_phase >> h) & 1u);
-            p_phase ^= 1u << h;
-            if (!ok) break;
+          if (now) {
+            pass(sh->v_full, sh->v_empty, v_next, it);
+            wait(&sh->v_full[stage], (uint32_t)((it / L::kStages) & 1));
+            wait(&sh->p_full[s][h], p_phase);
+            fence_after();
             const uint32_t b = desc_cols(smem0 + L::kValueRing + stage * L::kStageBytes);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              mma_ts(t_o, t_s + h * 64 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, k != 0 || t > t_from || h > 0);
+              mma_ts(t_o, t_s + h * 64 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, h > 0 || k > 0 || t > t_from);
           }
-          if (t + step < take) scores(t + step, h);
-          else if (h == 0 && t >= t_from) mma_commit(&sh->half_done[s]);
-          if (t >= t_from && ok) mma_commit(&sh->v_empty[stage]);
+          if (next) {
+            // Scores of block h of tile t + step.  The commit also says that the product with the block's values before it
+            // is complete.
+            const int it2 = it + 2 * step, stage2 = it2 % L::kStages;
+            pass(sh->k_full, sh->k_empty, k_next, it2);
+            wait(&sh->k_full[stage2], (uint32_t)((it2 / L::kStages) & 1));
+            const uint32_t b = desc_rows(smem0 + L::kKeyRing + stage2 * L::kStageBytes);
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k)
+              mma_ss(t_s + h * 64, q_desc + (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2), b + (uint32_t)((k >> 2) * ((kBlock * 128) >> 4) + (k & 3) * 2),
+                     id_qk, k != 0);
+            mma_commit(&sh->s_full[s][h]);
+            mma_commit(&sh->k_empty[stage2]);
+          } else if (h == 0 && now) {
+            mma_commit(&sh->half_done[s]);
+          }
+          if (now) mma_commit(&sh->v_empty[stage]);
         }
+        if (now) p_phase ^= 1u;
       }
-      if (!ok) break;
       // (a stream that had no tile says nothing: it could come by twice before anybody looks)
       if (t_from < take) mma_commit(&sh->o_full[s]);
       mma_commit(&sh->q_empty[qs]);
@@ -671,12 +668,15 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       blocks0 += 2 * take;
       pass(sh->k_full, sh->k_empty, k_next, blocks0);   // what the other stream had last
       pass(sh->v_full, sh->v_empty, v_next, blocks0);
+      k_next = v_next = blocks0;
+      if (limit == 0) break;
     }
-    if (!ok) {   // let everything issued finish before tensor memory is given back
+    if (limit == 0) {   // let everything issued finish before tensor memory is given back
       if (lane == 0) gave_up(p);
       __syncwarp();
       mma_commit(&sh->drain[s]);
-      tc_wait<true>(&sh->drain[s], 0);
+      limit = kPolls;
+      wait(&sh->drain[s], 0);
     }
   } else {
     // ================= softmax: one row a thread =================
@@ -689,17 +689,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t s_phase = 0, half_phase = 0;   // s_phase: of both blocks at the beginning of a tile
     uint32_t group_phase = 0, both_phase = 0;
     int blocks0 = 0, pc = 0;     // blocks0: of the pieces before
-    bool ok = true;
+    int limit = kPolls;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok && !tc_wait<true>(bar, parity)) {
-        ok = false;
-        if (lane == 0) gave_up(p);
-      }
+      tc_wait<true>(bar, parity, limit);
       fence_after();
     };
     // barriers among the softmax warps: of this stream, of both (bounded like every wait)
     auto meet = [&](bool all) {
-      if (!ok) return;
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(all ? &sh->both : &sh->group[s]);
@@ -713,9 +709,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       h[1] = 0;    // its part of a unit that began in a CTA before: 0 none, 1 the end, 2 some in between
     }
 #pragma unroll 1
-    for (; ok; ++pc) {
+    for (; limit; ++pc) {
       wait(&sh->piece_full[pc % kPieces], (uint32_t)((pc / kPieces) & 1));
-      if (!ok) break;
+      if (limit == 0) break;
       const Piece& x = sh->piece[pc % kPieces];
       const int take = x.take, two = x.two, first = x.first;
       if (take <= 0) break;
@@ -729,6 +725,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       const int hi_first = x.hi_first, lo_last = x.lo_last;
       float m = live ? kNegInf : 0.f, l = 0.f;       // reference (raw score; none yet: -inf), sum
+      bool none = true;                 // some row of the warp has no reference yet
       const int step = two ? 1 : 2, t_from = two ? 0 : s;
 #pragma unroll 1
       for (int t = t_from; t < take; t += step) {
@@ -736,7 +733,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         for (int h = 0; h < 2; ++h) {
           const int k0 = (first + t) * kKeys + h * kBlock;
           wait(&sh->s_full[s][h], s_phase);   // the block's keys have landed, and what was loaded before them
-          if (!ok) break;
           const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(blocks0 + 2 * t + h) & 31]);
           const bool edge = k0 + kBlock > hi_first || k0 < lo_last || bad != 0;
           if (edge) {
@@ -745,7 +741,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // taken out here, where it would reach rows with weight 0, and added in the epilogue to the rows that see it.
             const int it = blocks0 + 2 * t + h;
             wait(&sh->v_full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
-            if (!ok) break;
             unsigned char* vt = smem_raw + L::kValueRing + (it % L::kStages) * L::kStageBytes;
             const int kv_here = min(kBlock, max(0, x.kv - k0));
             const int from = min(kv_here, max(0, lo_last - k0)), to = min(kv_here, max(from, hi_first - k0));
@@ -769,7 +764,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (found) *reinterpret_cast<volatile int*>(&sh->nonfinite) = 1;
             fence_async_proxy();
             meet(two);   // everybody has looked before anything is taken out
-            if (!ok) break;
             if (*reinterpret_cast<volatile int*>(&sh->nonfinite)) {   // (or in an earlier tile: then there is nothing to find)
 #pragma unroll 1
               for (int e = tid & 127; e < n_vec; e += 128) {
@@ -803,7 +797,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 for (int j = 0; j < 32; ++j) v[i + j] = (keep & (1u << j)) ? v[i + j] : kNegInf;
               }
             }
-            bool raise = __any_sync(kFullMask, m == kNegInf);
+            bool raise = none;
 #pragma unroll 1
             for (;;) {
               if (raise) {
@@ -821,7 +815,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                   if (h == 0) wait(&sh->s_full[s][1], s_phase);
                   else if (t + step < take) wait(&sh->s_full[s][0], s_phase ^ 1u);
                   else wait(&sh->half_done[s], half_phase);
-                  if (!ok) break;
 #pragma unroll 1
                   for (int j0 = 0; j0 < DP; j0 += 16) {
                     float o[16];
@@ -834,6 +827,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 }
                 l *= alpha;
                 m = top;
+                none = __any_sync(kFullMask, m == kNegInf);
               }
               const float ref = m == kNegInf ? 0.f : m * c;
               const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
@@ -860,17 +854,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               }
               raise = true;
             }
-            if (!ok) break;
             tm_st_wait();
             fence_before();
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh->p_full[s][h]);
         }
-        if (!ok) break;
         s_phase ^= 1u;
       }
-      if (!ok) break;
       if (t_from < take) half_phase ^= 1u;
       // ---- end of the piece
       const int n1 = two ? take : take / 2;   // tiles of the second stream
@@ -880,13 +871,11 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (s == 0 || !two) wait(&sh->o_full[0], o_phase & 1u);
       if (n1 > 0 && (s == 1 || !two)) wait(&sh->o_full[1], o_phase >> 1);
       o_phase ^= n1 > 0 ? 3u : 1u;
-      if (!ok) break;
       if (m == kNegInf && l == l) l = 0.f;   // no key, or only scores of -inf: nothing was weighed
       float f0 = 1.f, f1 = 1.f;
       if (!two) {
         sh->exch[s][r] = make_float2(m, l);
         meet(true);
-        if (!ok) break;
         const float2 e0 = sh->exch[0][r], e1 = sh->exch[1][r];
         m = fmaxf(e0.x, e1.x);
         f0 = e0.x == kNegInf ? 0.f : ex2((e0.x - m) * c);
@@ -975,6 +964,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
     }
+    if (limit == 0 && lane == 0) gave_up(p);
   }
   fence_before();
   __syncthreads();
