@@ -41,7 +41,7 @@ constexpr int kSoftmaxWarps = 8;
 constexpr int kKeyWarp = kSoftmaxWarps, kValueWarp = kSoftmaxWarps + 1, kMmaWarp = kSoftmaxWarps + 2;
 constexpr int kTcThreads = 32 * (kSoftmaxWarps + 4);
 constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
-constexpr int kPolyPairs = 0;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
+constexpr int kPolyPairs = 6;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
 constexpr float kMostSum = 32768.f; // of the weights of a row and block before the reference is raised
 constexpr int kPieces = 4;          // pieces of work the producer may be ahead
 
@@ -1101,7 +1101,7 @@ cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStrea
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, 4);
+  cfg.gridDim = dim3(grid, 16);   // up to 256 rows a unit, two a warp
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
