@@ -495,53 +495,68 @@ def verify_recover_round(ctx: Context, inputs, *, accept_mode=ACCEPT_RATIO, reco
 
 
 # ---- the paged key/value cache in front of the round -----------------------------------------------------------------
+# These calls are made once a layer or a round, so their checks are kept short: a tensor is compared by dtype object, element
+# count, contiguity and device index, about a third of a microsecond each.
 _CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_I32, _I64 = torch.int32, torch.int64
 
 
-def _launch(fn, name: str, desc, device):
-    """Call an entry point that works on the current device, on the tensors' device and its current stream."""
-    if device.type != "cuda":
+def _launch(fn, name: str, desc, dev: int):
+    """Call an entry point that works on the current device, on the tensors' device `dev` and its current stream."""
+    if dev < 0:
         raise RuntimeError("specsteer needs tensors on a CUDA device; there is no CPU fallback")
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        code = fn(desc, stream)
+    if torch.cuda.current_device() == dev:
+        code = fn(desc, torch._C._cuda_getCurrentRawStream(dev))
     else:
-        with torch.cuda.device(device):
-            code = fn(desc, stream)
+        with torch.cuda.device(dev):
+            code = fn(desc, torch._C._cuda_getCurrentRawStream(dev))
     if code != OK:
         raise SpecSteerError(code, name)
 
 
-def _flat(t: torch.Tensor, name: str, dtype, n: int, device) -> int:
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
-        raise ValueError("%s must be a contiguous %s tensor of %d elements on %s" % (name, dtype, n, device))
+def _flat(t: torch.Tensor, dtype, n: int, dev: int) -> int:
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("bad tensor: dtype %s, %d elements, device %d (want contiguous %s, %d, %d)" %
+                         (t.dtype, t.numel(), t.get_device(), dtype, n, dev))
     return t.data_ptr()
 
 
-def _table(block_table: torch.Tensor, device):
-    if block_table.dim() != 2 or block_table.dtype != torch.int32 or block_table.device != device or block_table.shape[1] < 1 or \
-            (block_table.stride(1) != 1 and block_table.shape[1] > 1 and block_table.shape[0] > 0):
-        raise ValueError("block_table must be an int32 tensor [B, width] with dense rows on %s" % device)
-    B, width = block_table.shape
-    return block_table.data_ptr(), B, width, (block_table.stride(0) if B > 1 else width)
+def _table(block_table: torch.Tensor, dev: int):
+    """(pointer, requests, entries a row, stride of a row) of a block table."""
+    shape = block_table.shape
+    if len(shape) != 2 or block_table.dtype is not _I32 or block_table.get_device() != dev or shape[1] < 1:
+        raise ValueError("block_table must be an int32 tensor [B, width] on the device of the others")
+    ld, one = block_table.stride()
+    B, width = shape
+    if one != 1 and width > 1 and B > 0:
+        raise ValueError("block_table needs dense rows")
+    return block_table.data_ptr(), B, width, (ld if B > 1 else width)
 
 
 def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor):
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.device != v_cache.device:
+    """(shape, strides of each, device, dtype code) of two caches that go together."""
+    shape, dtype, dev = k_cache.shape, k_cache.dtype, k_cache.get_device()
+    if len(shape) != 4 or shape != v_cache.shape or dtype is not v_cache.dtype or dev != v_cache.get_device():
         raise ValueError("k_cache and v_cache must share shape [n_pages, page_size, Hkv, D], dtype and device")
-    if k_cache.dtype not in _CACHE_DTYPES:
+    code = _CACHE_DTYPES.get(dtype)
+    if code is None:
         raise ValueError("the caches must be float32, bfloat16 or float16")
-    if k_cache.shape[3] > 1 and (k_cache.stride(3) != 1 or v_cache.stride(3) != 1):
+    e, f = k_cache.stride(), v_cache.stride()
+    if shape[3] > 1 and (e[3] != 1 or f[3] != 1):
         raise ValueError("the caches need a contiguous last axis")
+    return shape, e, f, dev, code
 
 
-def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
-    if t.dim() != 3 or t.dtype != like.dtype or t.device != like.device or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError("%s must be a [tokens, heads, D] %s tensor with a contiguous last axis on %s" % (name, like.dtype, like.device))
+def _heads(t: torch.Tensor, shape, dtype, dev: int):
+    """Strides of a [tokens, heads, D] tensor."""
+    st = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or (shape[2] > 1 and st[2] != 1):
+        raise ValueError("bad tensor: %s %s (want %s %s with a contiguous last axis, on the caches' device)" % (tuple(t.shape), t.dtype, tuple(shape), dtype))
+    return st
 
 
-_PLAN_OUT = (("seq_len", torch.int32), ("pages_held", torch.int32), ("ring_pos", torch.int64), ("cu_new", torch.int32), ("kv_len", torch.int32),
-             ("slot_map", torch.int64), ("positions", torch.int32), ("token_req", torch.int32), ("status", torch.int32))
+_PLAN_OUT = (("seq_len", _I32), ("pages_held", _I32), ("ring_pos", _I64), ("cu_new", _I32), ("kv_len", _I32),
+             ("slot_map", _I64), ("positions", _I32), ("token_req", _I32), ("status", _I32))
 
 
 def cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, pages_held: torch.Tensor, block_table: torch.Tensor, free_ring: torch.Tensor,
@@ -557,19 +572,19 @@ def cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, pages_held: torch.T
     if stream is not None:   # what is allocated on the way belongs to that stream too
         with torch.cuda.stream(stream):
             return cache_plan(seq_len, new_len, pages_held, block_table, free_ring, ring_pos, page_size=page_size, max_tokens=max_tokens, advance=advance, out=out)
-    dev = block_table.device
+    dev = block_table.get_device()
     table, B, width, ld = _table(block_table, dev)
-    max_tokens, n_pages = int(max_tokens), free_ring.numel()
-    sizes = (B, B, 2, B + 1, B, max_tokens, max_tokens, max_tokens, B)
+    T, n_pages = int(max_tokens), free_ring.numel()
     if out is None:
-        out = {name: torch.empty(n, dtype=dt, device=dev) for (name, dt), n in zip(_PLAN_OUT, sizes)}
-    outs = [_flat(out[name], name, dt, n, dev) for (name, dt), n in zip(_PLAN_OUT, sizes)]
-    i32 = torch.int32
-    d = CachePlanDesc(B, int(page_size), n_pages, width, max_tokens, ld,
-                      _flat(seq_len, "seq_len", i32, B, dev), None if advance is None else _flat(advance, "advance", i32, B, dev),
-                      _flat(new_len, "new_len", i32, B, dev), _flat(pages_held, "pages_held", i32, B, dev),
-                      _flat(ring_pos, "ring_pos", torch.int64, 2, dev), table, _flat(free_ring, "free_ring", i32, n_pages, dev), *outs)
-    _launch(load_library().specsteer_cache_plan, "specsteer_cache_plan", d, dev)
+        sizes = (B, B, 2, B + 1, B, T, T, T, B)
+        out = {name: torch.empty(n, dtype=dt, device=block_table.device) for (name, dt), n in zip(_PLAN_OUT, sizes)}
+    d = CachePlanDesc(B, int(page_size), n_pages, width, T, ld,
+                      _flat(seq_len, _I32, B, dev), None if advance is None else _flat(advance, _I32, B, dev), _flat(new_len, _I32, B, dev),
+                      _flat(pages_held, _I32, B, dev), _flat(ring_pos, _I64, 2, dev), table, _flat(free_ring, _I32, n_pages, dev),
+                      _flat(out["seq_len"], _I32, B, dev), _flat(out["pages_held"], _I32, B, dev), _flat(out["ring_pos"], _I64, 2, dev),
+                      _flat(out["cu_new"], _I32, B + 1, dev), _flat(out["kv_len"], _I32, B, dev), _flat(out["slot_map"], _I64, T, dev),
+                      _flat(out["positions"], _I32, T, dev), _flat(out["token_req"], _I32, T, dev), _flat(out["status"], _I32, B, dev))
+    _launch((_lib or load_library()).specsteer_cache_plan, "specsteer_cache_plan", d, dev)
     return out
 
 
@@ -577,20 +592,17 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     """Store the keys and values of T tokens, [T, Hkv, D], in their slots of the caches, [n_pages, page_size, Hkv, D] (any
     strides with a contiguous last axis; a cache laid out by heads is passed as a transposed view).  slot_map [T] int64:
     page * page_size + offset; a slot outside the cache (-1) drops its token."""
-    if stream is not None:   # what is allocated on the way belongs to that stream too
+    if stream is not None:
         with torch.cuda.stream(stream):
             return cache_append(k, v, k_cache, v_cache, slot_map)
-    _caches(k_cache, v_cache)
-    _heads(k, "k", k_cache)
-    _heads(v, "v", k_cache)
-    n_pages, page_size, H, D = k_cache.shape
-    if k.shape != v.shape or k.shape[1] != H or k.shape[2] != D:
-        raise ValueError("k and v must be [T, %d, %d]" % (H, D))
-    T, dev = k.shape[0], k_cache.device
-    a, b, e, f = k.stride(), v.stride(), k_cache.stride(), v_cache.stride()
-    d = CacheAppendDesc(T, H, D, page_size, n_pages, _CACHE_DTYPES[k_cache.dtype], a[0], a[1], b[0], b[1], e[0], e[1], e[2], f[0], f[1], f[2],
-                        k.data_ptr(), v.data_ptr(), _flat(slot_map, "slot_map", torch.int64, T, dev), k_cache.data_ptr(), v_cache.data_ptr())
-    _launch(load_library().specsteer_cache_append, "specsteer_cache_append", d, dev)
+    shape, e, f, dev, code = _caches(k_cache, v_cache)
+    n_pages, page_size, H, D = shape
+    T = slot_map.numel()
+    want, dtype = (T, H, D), k_cache.dtype
+    a, b = _heads(k, want, dtype, dev), _heads(v, want, dtype, dev)
+    d = CacheAppendDesc(T, H, D, page_size, n_pages, code, a[0], a[1], b[0], b[1], e[0], e[1], e[2], f[0], f[1], f[2],
+                        k.data_ptr(), v.data_ptr(), _flat(slot_map, _I64, T, dev), k_cache.data_ptr(), v_cache.data_ptr())
+    _launch((_lib or load_library()).specsteer_cache_append, "specsteer_cache_append", d, dev)
 
 
 def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
@@ -605,40 +617,36 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     Returns (out [T, Hq, D], lse [T, Hq] float32); rows of no request are left as they are in out and lse.  A workspace (uint8)
     is allocated from torch's pool when none is given; a call captured into a graph, or overlapping others, keeps its
     own.  Formulas, limits and refusals: specsteer_chunk_attention."""
-    if stream is not None:   # what is allocated on the way belongs to that stream too
+    if stream is not None:
         with torch.cuda.stream(stream):
             return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
                                    workspace=workspace, generic=generic)
-    _caches(k_cache, v_cache)
-    _heads(q, "q", k_cache)
-    dev = q.device
-    n_pages, page_size, Hkv, D = k_cache.shape
-    T, Hq, Dq = q.shape
-    if Dq != D or k_cache.dtype == torch.float32:
-        raise ValueError("q and the caches must share D and be bfloat16 or float16")
+    shape, e, f, dev, code = _caches(k_cache, v_cache)
+    n_pages, page_size, Hkv, D = shape
+    want, dtype = q.shape, k_cache.dtype
+    if code == F32 or len(want) != 3 or want[2] != D:
+        raise ValueError("q must be [T, Hq, D] with the caches' D, all of them bfloat16 or float16")
+    a = _heads(q, want, dtype, dev)
+    T, Hq, _ = want
     table, B, width, ld = _table(block_table, dev)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
-    else:
-        _heads(out, "out", k_cache)
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
+        out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
+    o = _heads(out, want, dtype, dev)
     if lse is None:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
-    a, o, e, f = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
-    d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, _CACHE_DTYPES[q.dtype], int(window),
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, code, int(window),
                       1.0 / math.sqrt(D) if scale is None else float(scale), ATTENTION_GENERIC if generic else 0, ld,
                       a[0], a[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
-                      q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, "cu_new", torch.int32, B + 1, dev),
-                      _flat(kv_len, "kv_len", torch.int32, B, dev), out.data_ptr(), _flat(lse, "lse", torch.float32, T * Hq, dev),
-                      None if status is None else _flat(status, "status", torch.int32, B, dev), None, 0)
-    lib = load_library()
-    need = lib.specsteer_chunk_attention_workspace(d)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    if workspace is not None:
-        if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
-            raise ValueError("workspace must be a contiguous uint8 tensor on %s" % dev)
-        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel()
+                      q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev),
+                      out.data_ptr(), _flat(lse, torch.float32, T * Hq, dev), None if status is None else _flat(status, _I32, B, dev), None, 0)
+    lib = _lib or load_library()
+    if workspace is None:
+        need = lib.specsteer_chunk_attention_workspace(d)
+        if need and dev >= 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            d.workspace, d.workspace_bytes = workspace.data_ptr(), need
+    else:
+        d.workspace_bytes = workspace.numel()
+        d.workspace = _flat(workspace, torch.uint8, d.workspace_bytes, dev)
     _launch(lib.specsteer_chunk_attention, "specsteer_chunk_attention", d, dev)
     return out, lse

@@ -484,15 +484,16 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   if (warp == kKeyWarp || warp == kValueWarp) {
     // ================= work list and TMA =================
     const bool keys = warp == kKeyWarp;
+    // A tile's two blocks are issued together, by the two halves of the warp: a block has at most 16 boxes (pages of 8 keys,
+    // two chunks of 64 columns).
     constexpr int chunks = DP / 64;
-    const int box = lane / chunks, chunk = lane % chunks;
+    const int half = lane >> 4, box = (lane & 15) / chunks, chunk = lane % chunks;
     const bool loads = box < p.boxes;
     const uint32_t lane_off = smem0 + (keys ? L::kKeyRing : L::kValueRing) + (uint32_t)chunk * (kBlock * 128) + (uint32_t)box * p.page_rows * 128;
     const CUtensorMap* tm = keys ? &tm_k : &tm_v;
     uint64_t* full = keys ? sh->k_full : sh->v_full;
     uint64_t* empty = keys ? sh->k_empty : sh->v_empty;
-    int st = 0, blocks = 0, qi = 0, pc = 0;   // st: stage of the next block
-    uint32_t st_phase = 1;
+    int blocks = 0, qi = 0, pc = 0;
     int limit = kPolls;
     Walk w;
     w.begin(sh);
@@ -514,65 +515,67 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tc_wait<true>(&sh->piece_full[pc % kPieces], turn, limit);
         if (limit == 0) break;
       }
-      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, n_blocks = 2 * take;
+      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2;
       if (take <= 0) break;
       const int n_q = !keys ? 0 : x->two ? 2 : 1;
       const int* table = p.d.block_table + (long long)b * p.d.ld_table;
-      // page of this lane's box of block j of the piece: the id, or n_pages (a coordinate outside, which reads zeros) for none
-      auto page_of = [&](int j) -> int {
+      // page of this lane's box of tile t of the piece: the id, or n_pages (a coordinate outside, which reads zeros) for none
+      auto page_of = [&](int t) -> int {
+        const int blk = first + 2 * t + half;
         int page = p.d.n_pages;
-        if (loads && j < n_blocks && (first + j) * kBlock + box * p.page_rows < kv)
-          page = __ldg(table + (p.boxes > 1 ? (first + j) * p.boxes + box : (first + j) / p.page_blocks));
+        if (loads && t < take && blk * kBlock + box * p.page_rows < kv) page = __ldg(table + (p.boxes > 1 ? blk * p.boxes + box : blk / p.page_blocks));
         return page;
       };
-      int page = page_of(0), page1 = page_of(1), page2 = page_of(2), q_done = 0;
+      int page = page_of(0), page1 = page_of(1), q_done = 0;
 #pragma unroll 1
-      for (int j = 0; j < n_blocks; ++j) {
+      for (int t = 0; t <= take; ++t) {
         // The queries go behind the first keys, whose stages are free sooner: once their place is, or at the latest when the
         // ring may be full of keys that wait for them.
 #pragma unroll 1
-        while (j > 0 && q_done < n_q && limit) {
+        while (t > 0 && q_done < n_q && limit) {
           const int slot = qi & 1;
           const uint32_t q_turn = (uint32_t)((qi >> 1) & 1) ^ 1u;
-          if (j < L::kStages && j + 1 < n_blocks && !__all_sync(kFullMask, mbar_test_nonblocking(&sh->q_empty[slot], q_turn))) break;
+          if (t < L::kStages / 2 && t < take && !__all_sync(kFullMask, mbar_test_nonblocking(&sh->q_empty[slot], q_turn))) break;
           tc_wait<true>(&sh->q_empty[slot], q_turn, limit);
           if (limit == 0) break;
           const int tok = x->tok0 + q_done * p.tile_tok, cnt = min(p.tile_tok, x->tok1 - tok);
-          const int nb = (cnt + p.box_tok - 1) / p.box_tok;
+          const int nb = (cnt + p.box_tok - 1) / p.box_tok, q_box = lane / chunks;
           if (lane == 0) mbar_arrive_expect_tx(&sh->q_full[slot], (uint32_t)(nb * p.box_rows * 128 * chunks));
           __syncwarp();
-          if (box < nb)
-            tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + box * p.box_rows * 128, &tm_q, chunk * 64, hk * p.G,
-                   x->row0 + tok + box * p.box_tok, &sh->q_full[slot]);
+          if (q_box < nb)
+            tma_3d(smem0 + slot * L::kQBytes + chunk * (128 * 128) + q_box * p.box_rows * 128, &tm_q, chunk * 64, hk * p.G,
+                   x->row0 + tok + q_box * p.box_tok, &sh->q_full[slot]);
           ++qi;
           ++q_done;
         }
-        if (limit == 0) break;
+        if (limit == 0 || t == take) break;
+        const int blk = first + 2 * t + half;
         const bool outside = page < 0 || page >= p.d.n_pages;
         if (keys) {
-          const uint32_t votes = __ballot_sync(kFullMask, loads && outside && (first + j) * kBlock + box * p.page_rows < kv);
-          if (lane == 0) {
+          const uint32_t votes = __ballot_sync(kFullMask, loads && outside && blk * kBlock + box * p.page_rows < kv);
+          if ((lane & 15) == 0) {
             uint32_t bad = 0;
             if (votes) {
 #pragma unroll 1
-              for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (i * chunks)) & 1u) << i;
-              if (p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_PAGE);
+              for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (16 * half + i * chunks)) & 1u) << i;
+              if (bad && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_PAGE);
             }
             // the softmax warps read the word at most the ring and the blocks in work later, well under 32
-            *reinterpret_cast<volatile uint32_t*>(&sh->bad[blocks & 31]) = bad;
+            *reinterpret_cast<volatile uint32_t*>(&sh->bad[(blocks + half) & 31]) = bad;
           }
         }
-        const int page3 = page_of(j + 3);
-        tc_wait<true>(&empty[st], st_phase, limit);
+        const int page2 = page_of(t + 2);
+        const int st0 = blocks % L::kStages, st1 = (blocks + 1) % L::kStages, st = half ? st1 : st0;
+        tc_wait<true>(&empty[st0], (uint32_t)((blocks / L::kStages) & 1) ^ 1u, limit);
+        tc_wait<true>(&empty[st1], (uint32_t)(((blocks + 1) / L::kStages) & 1) ^ 1u, limit);
         if (limit == 0) break;
-        if (lane == 0) mbar_arrive_expect_tx(&full[st], L::kStageBytes);
+        if ((lane & 15) == 0) mbar_arrive_expect_tx(&full[st], L::kStageBytes);
         __syncwarp();
         if (loads)
-          tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, p.page_blocks > 1 ? (first + j) % p.page_blocks * kBlock : 0, hk,
+          tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, p.page_blocks > 1 ? blk % p.page_blocks * kBlock : 0, hk,
                  outside ? p.d.n_pages : page, &full[st]);
-        ++blocks;
-        if (++st == L::kStages) { st = 0; st_phase ^= 1u; }
-        page = page1; page1 = page2; page2 = page3;
+        blocks += 2;
+        page = page1; page1 = page2;
       }
       if (limit == 0) break;
       if (keys) w.next(p);
