@@ -977,62 +977,79 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   }
 }
 
-// Puts the parts of a cut unit together: block x takes the unit that begins in CTA x and goes on in the CTAs behind it.
+// Puts the parts of a cut unit together: blocks x take the unit that begins in CTA x and goes on in the CTAs behind it.
 // One warp a row; the parts are added in their order, so the bits do not depend on who came first.
 template <int DP, bool BF>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
   pdl_wait();
   const int cta = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int* h = p.head + cta * 8;
-  const int slot0 = h[0];
+  const int4 h = *reinterpret_cast<const int4*>(p.head + cta * 8);
+  const int slot0 = h.x;
   if (slot0 < 0) return;
-  const int b = h[2], hk = h[3], u = h[4];
-  const AttnRequest rq = attn_request(p.d, b);
+  const int u = p.head[cta * 8 + 4];
+  const AttnRequest rq = attn_request(p.d, h.z);
   const Unit x = make_unit(p, rq, u);
-  // the parts: the first one in slot0, then slot 2*(cta + i) of every CTA behind that has one, to the unit's end
-  int span = 1;
-  while (cta + span < n_cta) {
-    const int kind = p.head[(cta + span) * 8 + 1];
-    ++span;
-    if (kind == 1) break;
-  }
-  const int rows = (x.tok1 - x.tok0) * p.G;
+  const int rows = (x.tok1 - x.tok0) * p.G, tile_rows = p.tile_tok * p.G;
   for (int q = blockIdx.y * 8 + warp; q < rows; q += gridDim.y * 8) {
-    const int tile_rows = p.tile_tok * p.G;
     const int part_row = q < tile_rows ? q : 128 + q - tile_rows;
-    auto slot_of = [&](int i) { return (long long)(i == 0 ? slot0 : 2 * (cta + i)) * 256 + part_row; };
-    auto has = [&](int i) { return i == 0 || p.head[(cta + i) * 8 + 1] != 0; };
-    float m = kNegInf;
-    for (int i = lane; i < span; i += 32)
-      if (has(i)) m = fmaxf(m, p.part_ml[slot_of(i)].x);
-    m = warp_max(m);
-    float l = 0.f, o[DP / 32];
+    float m = kNegInf, l = 0.f, o[DP / 32];
 #pragma unroll
     for (int j = 0; j < DP / 32; ++j) o[j] = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < span; ++i) {
-      if (!has(i)) continue;
-      const long long at = slot_of(i);
-      const float2 ml = p.part_ml[at];
-      const float f = ml.x == kNegInf ? 0.f : ex2(ml.x - m);
-      l = fmaf(ml.y, f, l);
-      const float* src = p.part + at * DP + lane * (DP / 32);
-      if (DP == 128) {
-        const float4 y = *reinterpret_cast<const float4*>(src);
-        o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]); o[2 % (DP / 32)] = fmaf(y.z, f, o[2 % (DP / 32)]); o[3 % (DP / 32)] = fmaf(y.w, f, o[3 % (DP / 32)]);
-      } else {
-        const float2 y = *reinterpret_cast<const float2*>(src);
-        o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]);
+    // The parts: the first one in slot0, then slot 2*i of every CTA i behind that has one, to the unit's end.  32 CTAs at a
+    // time, a lane each, for the references and sums; then the parts themselves with the warp side by side.
+    bool more = true;
+    for (int base = cta; more && base < n_cta; base += 32) {
+      const int i = base + lane;
+      const int kind = i == cta ? 2 : i < n_cta ? p.head[i * 8 + 1] : 1;
+      const uint32_t ends = __ballot_sync(kFullMask, kind == 1);
+      const uint32_t upto = ends ? (2u << (__ffs(ends) - 1)) - 1u : 0xffffffffu;   // lanes up to the first end (all: shift to 0)
+      const bool has = kind != 0 && i < n_cta && ((upto >> lane) & 1u);
+      more = ends == 0;
+      const long long at = (long long)(i == cta ? slot0 : 2 * i) * 256 + part_row;
+      const float2 ml = has ? p.part_ml[at] : make_float2(kNegInf, 0.f);
+      const float top = fmaxf(m, warp_max(ml.x));
+      const float keep = m == kNegInf ? 0.f : ex2(m - top), f = ml.x == kNegInf ? 0.f : ex2(ml.x - top);
+      l = l * keep + warp_sum(ml.y * f);
+#pragma unroll
+      for (int j = 0; j < DP / 32; ++j) o[j] *= keep;
+      m = top;
+      uint32_t todo = __ballot_sync(kFullMask, has);
+      while (todo) {
+        // four parts in flight
+        float2 y[4][DP / 64];
+        float w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          w[k] = 0.f;
+#pragma unroll
+          for (int j = 0; j < DP / 64; ++j) y[k][j] = make_float2(0.f, 0.f);
+          if (todo) {
+            const int src = __ffs(todo) - 1;
+            todo &= todo - 1;
+            w[k] = __shfl_sync(kFullMask, f, src);
+            const float* part = p.part + __shfl_sync(kFullMask, at, src) * DP + 2 * lane;
+#pragma unroll
+            for (int j = 0; j < DP / 64; ++j) y[k][j] = *reinterpret_cast<const float2*>(part + 64 * j);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+          for (int j = 0; j < DP / 64; ++j) {
+            o[2 * j] = fmaf(y[k][j].x, w[k], o[2 * j]);
+            o[2 * j + 1] = fmaf(y[k][j].y, w[k], o[2 * j + 1]);
+          }
+        }
       }
     }
-    const int tok = x.tok0 + q / p.G, head = hk * p.G + q % p.G;
+    const int tok = x.tok0 + q / p.G, head = h.w * p.G + q % p.G;
     const long long row = (long long)rq.row0 + tok;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head;
 #pragma unroll
-    for (int j = 0; j < DP / 32; j += 2) {
-      const int d = lane * (DP / 32) + j;
-      const uint32_t y = pack2<BF>(o[j] * inv, o[j + 1] * inv);
+    for (int j = 0; j < DP / 64; ++j) {
+      const int d = 64 * j + 2 * lane;
+      const uint32_t y = pack2<BF>(o[2 * j] * inv, o[2 * j + 1] * inv);
       if (d < p.d.D) dst[d] = (unsigned short)y;
       if (d + 1 < p.d.D) dst[d + 1] = (unsigned short)(y >> 16);
     }
@@ -1104,7 +1121,7 @@ cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStrea
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, 16);   // up to 256 rows a unit, two a warp
+  cfg.gridDim = dim3(grid, 8);
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
