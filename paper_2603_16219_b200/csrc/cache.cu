@@ -3,8 +3,9 @@
 //
 //   cache_plan_kernel    one thread-block cluster; every CTA forms the same running sums over the requests (tokens,
 //                        pages taken, pages given back) in its own shared memory, then the cluster shares the page
-//                        moves and the rows of the slot map.  Two cluster barriers order the three steps that touch the
-//                        same memory: pages given back -> pages taken -> slots.
+//                        moves and the rows of the slot map.  Cluster barriers order the steps that touch the
+//                        same memory: pages given back -> pages taken -> slots -> the in-place outputs.  Latency is what
+//                        it costs, so a small plan gets one CTA of few threads: its barriers are cheaper.
 //   cache_append_kernel  a copy by slot, 16 bytes a thread where alignment allows.
 #include <atomic>
 
@@ -16,9 +17,7 @@ namespace specsteer {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-// CTAs per cluster when there is much to write.  The sums are latency and are repeated by every CTA; the rows of the
-// slot map (16 bytes a token) and the page moves are shared.
-constexpr int kPlanCluster = 8;
+constexpr int kPlanCluster = 8;      // CTAs at most: the portable cluster size
 
 typedef long long i64;
 
@@ -37,32 +36,36 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return r;
 }
 
-// Exclusive sum of v over the threads of the block in thread order; *total receives the sum.  Ends with a barrier, so
-// the scratch may be used again at once.
-__device__ __forceinline__ i64 block_exclusive_sum(i64 v, i64* scratch, i64* total) {
+// Exclusive sums of a pair over the threads of the block in thread order; *total receives the sums.  One barrier: `scratch`
+// ([32] pairs) must not be written again before the next one.
+struct Pair { i64 a, b; };
+__device__ __forceinline__ Pair block_exclusive_sums(Pair v, Pair* scratch, Pair* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  i64 x = v;
+  Pair x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const i64 y = __shfl_up_sync(kFullMask, x, o);
-    if (lane >= o) x += y;
+    const i64 a = __shfl_up_sync(kFullMask, x.a, o), b = __shfl_up_sync(kFullMask, x.b, o);
+    if (lane >= o) { x.a += a; x.b += b; }
   }
-  if (lane == 31) scratch[warp] = x;
-  __syncthreads();
-  if (warp == 0) {
-    i64 w = lane < nw ? scratch[lane] : 0;
+  if (nw > 1) {
+    if (lane == 31) scratch[warp] = x;
+    __syncthreads();
+    // every warp sums the warps' totals for itself
+    Pair w = lane < nw ? scratch[lane] : Pair{0, 0};
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const i64 y = __shfl_up_sync(kFullMask, w, o);
-      if (lane >= o) w += y;
+      const i64 a = __shfl_up_sync(kFullMask, w.a, o), b = __shfl_up_sync(kFullMask, w.b, o);
+      if (lane >= o) { w.a += a; w.b += b; }
     }
-    scratch[lane] = w;
+    total->a = __shfl_sync(kFullMask, w.a, 31);
+    total->b = __shfl_sync(kFullMask, w.b, 31);
+    const i64 a = __shfl_sync(kFullMask, w.a, warp ? warp - 1 : 0), b = __shfl_sync(kFullMask, w.b, warp ? warp - 1 : 0);
+    if (warp) { x.a += a; x.b += b; }
+  } else {
+    total->a = __shfl_sync(kFullMask, x.a, 31);
+    total->b = __shfl_sync(kFullMask, x.b, 31);
   }
-  __syncthreads();
-  const i64 before = warp ? scratch[warp - 1] : 0;
-  *total = scratch[31];
-  __syncthreads();
-  return before + x - v;
+  return Pair{x.a - v.a, x.b - v.b};
 }
 
 // The request that element i of a flattened list belongs to: the last b < B with cum[b] <= i (cum ascending, cum[0] = 0).
@@ -79,13 +82,21 @@ __device__ __forceinline__ int owner_of(const int* cum, int B, int i) {
 template <int IPT>
 __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const specsteer_cache_plan_desc p) {
   extern __shared__ int plan_smem[];
-  __shared__ i64 scratch[32];
+  __shared__ Pair scratch[3][32];
   const int B = p.B, tid = threadIdx.x;
-  int* cum_tok = plan_smem;                // [B+1]
+  int* cum_tok = plan_smem;                // [B+1] running sums: tokens, pages given back, pages taken
   int* cum_give = cum_tok + (B + 1);       // [B+1]
   int* cum_take = cum_give + (B + 1);      // [B+1]
+  int* kept_s = cum_take + (B + 1);        // [B] tokens kept
+  int* from_s = kept_s + B;                // [B] table entry where the request's pages taken or given back begin
   const uint32_t rank = cluster_rank(), n_cta = cluster_size();
   const int first_thread = (int)rank * blockDim.x + tid, n_threads = (int)n_cta * blockDim.x;
+
+  // (a cluster barrier makes every store visible to the other SMs first, which one CTA does not need)
+  auto sync_all = [&] {
+    if (n_cta == 1) __syncthreads();
+    else cluster_sync_all();
+  };
 
   const i64 head = p.ring_pos[0], tail = p.ring_pos[1], P = p.n_pages;
   const bool pool_ok = head >= 0 && tail >= head && tail - head <= P;
@@ -93,7 +104,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const specstee
 
   int seq[IPT], asked[IPT], held[IPT], status[IPT];
   i64 kept[IPT];
-  i64 sum = 0;
+  Pair sum{0, 0}, total;
 #pragma unroll
   for (int k = 0; k < IPT; ++k) {
     const int b = tid * IPT + k;
@@ -109,102 +120,79 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const specstee
         status[k] = SPECSTEER_REQ_BAD_LEN;
       if (!pool_ok) status[k] |= SPECSTEER_REQ_BAD_POOL;
       if (status[k]) asked[k] = 0;
-      sum += asked[k];
+      sum.a += asked[k];
     }
   }
-  i64 total;
-  i64 run = block_exclusive_sum(sum, scratch, &total);
+  Pair run = block_exclusive_sums(sum, scratch[0], &total);
   // tokens beyond max_tokens are refused; then the pages each request gives back or wants
-  i64 give_sum = 0, take_sum = 0;
+  Pair pages{0, 0}, page_total;            // given back, wanted
   int target[IPT];
 #pragma unroll
   for (int k = 0; k < IPT; ++k) {
-    run += asked[k];
-    if (asked[k] > 0 && run > p.max_tokens) { status[k] |= SPECSTEER_REQ_NO_ROOM; asked[k] = 0; }
+    run.a += asked[k];
+    if (asked[k] > 0 && run.a > p.max_tokens) { status[k] |= SPECSTEER_REQ_NO_ROOM; asked[k] = 0; }
     const bool passed_on = status[k] & (SPECSTEER_REQ_BAD_LEN | SPECSTEER_REQ_BAD_POOL);
     target[k] = passed_on ? held[k] : (int)((kept[k] + asked[k] + p.page_size - 1) / p.page_size);
     const int d = target[k] - held[k];
-    if (d > 0) take_sum += d; else give_sum -= d;
+    if (d > 0) pages.b += d; else pages.a -= d;
   }
-  i64 give_total, take_total, tok_total;
-  i64 give_run = block_exclusive_sum(give_sum, scratch, &give_total);
-  i64 take_run = block_exclusive_sum(take_sum, scratch, &take_total);
+  Pair page_run = block_exclusive_sums(pages, scratch[1], &page_total);
   const i64 room = pool_ok ? P - (tail - head) : 0;
-  const int given = (int)(give_total < room ? give_total : room);   // more would mean that a page was handed out twice
+  const int given = (int)(page_total.a < room ? page_total.a : room);   // more would mean that a page was handed out twice
   const i64 avail = pool_ok ? tail - head + given : 0;
-  i64 tok_sum = 0, served_sum = 0;
+  Pair served{0, 0}, served_total;         // tokens, pages taken
 #pragma unroll
   for (int k = 0; k < IPT; ++k) {
     const int b = tid * IPT + k;
     const int d = target[k] - held[k];
     if (b < B) {
-      cum_give[b] = (int)(give_run < 0x7fffffff ? give_run : 0x7fffffff);
-      cum_take[b] = (int)(take_run < avail ? take_run : avail);
+      cum_give[b] = (int)(page_run.a < 0x7fffffff ? page_run.a : 0x7fffffff);
+      cum_take[b] = (int)(page_run.b < avail ? page_run.b : avail);
+      kept_s[b] = (int)kept[k];
+      from_s[b] = d > 0 ? held[k] : target[k];
     }
-    if (d < 0) give_run -= d;
+    if (d < 0) page_run.a -= d;
     if (d > 0) {
-      take_run += d;
+      page_run.b += d;
       // sums only grow: once a request is refused, every later one that wants pages is too, so the takers that are
       // served are a prefix and their running sum above is right
-      if (take_run > avail) { status[k] |= SPECSTEER_REQ_NO_PAGES; asked[k] = 0; target[k] = held[k]; }
-      else served_sum += d;
+      if (page_run.b > avail) { status[k] |= SPECSTEER_REQ_NO_PAGES; asked[k] = 0; target[k] = held[k]; }
+      else served.b += d;
     }
-    tok_sum += asked[k];
+    served.a += asked[k];
   }
-  i64 tok_run = block_exclusive_sum(tok_sum, scratch, &tok_total);
-  i64 served_total;
-  (void)block_exclusive_sum(served_sum, scratch, &served_total);
+  Pair tok_run = block_exclusive_sums(served, scratch[2], &served_total);
 #pragma unroll
   for (int k = 0; k < IPT; ++k) {
     const int b = tid * IPT + k;
-    if (b < B) cum_tok[b] = (int)tok_run;
-    tok_run += asked[k];
+    if (b < B) cum_tok[b] = (int)tok_run.a;
+    tok_run.a += asked[k];
   }
+  const int n_tok = (int)served_total.a, taken = (int)served_total.b;
   if (tid == 0) {
-    cum_tok[B] = (int)tok_total;
-    cum_give[B] = (int)(give_total < 0x7fffffff ? give_total : 0x7fffffff);
-    cum_take[B] = (int)served_total;
+    cum_tok[B] = n_tok;
+    cum_give[B] = (int)(page_total.a < 0x7fffffff ? page_total.a : 0x7fffffff);
+    cum_take[B] = taken;
   }
   __syncthreads();
 
-  // pages given back: entry target + r' of the request's table to place tail + r of the ring.  The inputs held the old
-  // pages_held; the first entry of a giver is its target, recovered from the lengths.
+  const i64 head0 = pool_ok ? head % P : 0, tail0 = pool_ok ? tail % P : 0;
+  auto ring_at = [&](i64 base, int r) { return base + r < P ? base + r : base + r - P; };   // r < P
+  // pages given back: entry target + i of the request's table to place tail + r of the ring
   for (int r = first_thread; r < given; r += n_threads) {
     const int b = owner_of(cum_give, B, r);
-    const int n = p.new_len[b];
-    const i64 kept_b = n == -1 ? 0 : (i64)p.seq_len[b] + (p.advance ? p.advance[b] : 0);
-    const i64 len = kept_b + (cum_tok[b + 1] - cum_tok[b]);
-    const int first = (int)((len + p.page_size - 1) / p.page_size);
-    p.free_ring[(tail + r) % P] = p.block_table[(i64)b * p.ld_table + first + (r - cum_give[b])];
-  }
-  cluster_sync_all();   // the ring is whole, and no CTA reads pages_held, seq_len or ring_pos for the sums any more
-  for (int r = first_thread; r < (int)served_total; r += n_threads) {
-    const int b = owner_of(cum_take, B, r);
-    const int have = p.pages_held[b];
-    p.block_table[(i64)b * p.ld_table + have + (r - cum_take[b])] = __ldcg(p.free_ring + (head + r) % P);
+    p.free_ring[ring_at(tail0, r)] = p.block_table[(i64)b * p.ld_table + from_s[b] + (r - cum_give[b])];
   }
   if (rank == 0) {
 #pragma unroll
     for (int k = 0; k < IPT; ++k)
       if (tid * IPT + k < B) p.req_status[tid * IPT + k] = status[k];
   }
-  cluster_sync_all();   // the tables are whole; the status words are there for the slots to add to
-  const int n_tok = (int)tok_total;
-  for (int i = first_thread; i < p.max_tokens; i += n_threads) {
-    i64 slot = -1;
-    int pos = -1, b = -1;
-    if (i < n_tok) {
-      b = owner_of(cum_tok, B, i);
-      pos = (int)((i64)p.seq_len[b] + (p.advance ? p.advance[b] : 0)) + (i - cum_tok[b]);
-      const int page = __ldcg(p.block_table + (i64)b * p.ld_table + pos / p.page_size);
-      if (page >= 0 && page < p.n_pages) slot = (i64)page * p.page_size + pos % p.page_size;
-      else atomicOr(p.req_status + b, SPECSTEER_REQ_BAD_PAGE);
-    }
-    p.slot_map[i] = slot;
-    if (p.positions) p.positions[i] = pos;
-    if (p.token_req) p.token_req[i] = b;
+  sync_all();   // the ring is whole; nobody reads the inputs any more, which the outputs may be in place of
+  for (int r = first_thread; r < taken; r += n_threads) {
+    const int b = owner_of(cum_take, B, r);
+    p.block_table[(i64)b * p.ld_table + from_s[b] + (r - cum_take[b])] = __ldcg(p.free_ring + ring_at(head0, r));
   }
-  cluster_sync_all();   // nobody reads an input any more: the in-place outputs may be written
   if (rank == 0) {
 #pragma unroll
     for (int k = 0; k < IPT; ++k) {
@@ -219,8 +207,41 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const specstee
     }
     if (tid == 0) {
       p.cu_new[B] = n_tok;
-      p.ring_pos_out[0] = head + served_total;
+      p.ring_pos_out[0] = head + taken;
       p.ring_pos_out[1] = tail + given;
+    }
+  }
+  sync_all();   // the tables are whole; the status words are there for the slots to add to
+  // Four rows of the slot map a thread, their page ids on the way together.  Pages of a power of two need no division.
+  const int shift = (p.page_size & (p.page_size - 1)) == 0 ? __ffs(p.page_size) - 1 : -1;
+  auto page_of = [&](int pos) { return shift >= 0 ? pos >> shift : pos / p.page_size; };
+  constexpr int kRows = 4;
+  for (i64 i0 = first_thread; i0 < p.max_tokens; i0 += kRows * n_threads) {
+    int b[kRows], pos[kRows], page[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const i64 at = i0 + (i64)k * n_threads;
+      b[k] = pos[k] = -1;
+      page[k] = 0;
+      if (at < n_tok) {
+        const int i = (int)at;
+        b[k] = owner_of(cum_tok, B, i);
+        pos[k] = kept_s[b[k]] + (i - cum_tok[b[k]]);
+        page[k] = __ldcg(p.block_table + (i64)b[k] * p.ld_table + page_of(pos[k]));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const i64 i = i0 + (i64)k * n_threads;
+      if (i >= p.max_tokens) break;
+      i64 slot = -1;
+      if (b[k] >= 0) {
+        if (page[k] >= 0 && page[k] < p.n_pages) slot = (i64)page[k] * p.page_size + (pos[k] - page_of(pos[k]) * p.page_size);
+        else atomicOr(p.req_status + b[k], SPECSTEER_REQ_BAD_PAGE);
+      }
+      p.slot_map[i] = slot;
+      if (p.positions) p.positions[i] = pos[k];
+      if (p.token_req) p.token_req[i] = b[k];
     }
   }
 }
@@ -284,22 +305,31 @@ extern "C" specsteer_status specsteer_cache_plan(const specsteer_cache_plan_desc
     return SPECSTEER_ERR_INVALID_ARG;
   if (d->max_tokens > 0 && !d->slot_map) return SPECSTEER_ERR_INVALID_ARG;
   if (d->B > SPECSTEER_PLAN_MAX_B) return SPECSTEER_ERR_UNSUPPORTED;
-  const size_t smem = (size_t)3 * (d->B + 1) * sizeof(int);
+  const size_t smem = ((size_t)5 * d->B + 3) * sizeof(int);
   auto kernel = d->B <= kPlanThreads ? cache_plan_kernel<1> : cache_plan_kernel<SPECSTEER_PLAN_MAX_B / kPlanThreads>;
-  if (smem > 48 * 1024 - 512) {
+  // A plan is bound by its barriers and by the slot map's dependent steps (owner, table entry, slot), never by its bytes.
+  // Up to 256 requests and 4096 rows one CTA serves: 32 threads for a handful of requests (one request and 5 rows 3.8 us,
+  // with 256 threads 4.7), else 256.  Larger plans get a CTA for every 512 rows up to the cluster (512 requests and 3584
+  // rows 8.1 us, in four CTAs 8.9, in one 13.6; 24 prompts with 49 thousand rows 14 us, 18 and 47), of 512 threads while
+  // there is a thread a request (the first of the two with 1024: 10.4 us).
+  const bool small = d->B <= 256 && d->max_tokens <= 4096;
+  const int threads = !small ? (d->B <= 512 ? 512 : kPlanThreads) : d->B <= 32 && d->max_tokens <= 256 ? 32 : 256;
+  const int wanted = d->max_tokens / 512 + (d->max_tokens % 512 != 0);
+  const int ctas = small || wanted < 1 ? 1 : wanted < kPlanCluster ? wanted : kPlanCluster;
+  if (smem > 40 * 1024) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
       cudaGetLastError();
       return SPECSTEER_ERR_CUDA;
     }
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kPlanCluster);
-  cfg.blockDim = dim3(kPlanThreads);
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = (cudaStream_t)cuda_stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kPlanCluster;
+  attr[0].val.clusterDim.x = ctas;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
