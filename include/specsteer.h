@@ -449,17 +449,21 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  * Row i of request b's n = cu_new[b+1] - cu_new[b] rows stands at position p = kv_len[b] - n + i and sees the keys
  * j <= p, and with window > 0 only j > p - window.  For every query head h, with kv head h / (Hq/Hkv):
  *   out[row][h] = sum_j softmax_j(scale * q[row][h] . k[j]) v[j],   lse[row][h] = log sum_j exp(scale * q[row][h] . k[j])
- * One token per request is plain decoding.  A row that sees no key (p < 0) gets 0 and -inf.  Keys that a row does not see
- * do not reach it, whatever they hold (NaN included).  Products are formed in float32 from the inputs' type, sums and
- * maxima are float32, the weights of a tile are rounded to the inputs' type for the product with v.
- *   - Requests with cu_new outside [0, T] or decreasing, or kv_len outside [0, table_width*page_size]: BAD_LEN, nothing
- *     written.  Rows of no request are left as they are.
+ * One token per request is plain decoding.  A row that sees no key (p < 0), or only keys whose scores are -inf, gets 0
+ * and -inf.  Keys that a row does not see do not reach it, whatever they hold (NaN included).  Products are formed in
+ * float32 from the inputs' type, sums and maxima are float32, and the tensor-core kernel rounds the weights to the
+ * inputs' type for the product with v.
+ *   - out and lse overlap no input.
+ *   - Requests with cu_new outside [0, T] or decreasing, or kv_len outside [0, table_width*page_size] or above 2^31 - 4097:
+ *     BAD_LEN, nothing written.  Rows of no request are left as they are.
  *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.
  *   - req_status may be NULL; bits are OR-ed into it (clear it first; specsteer_cache_plan writes it).
  *   - scale >= 0 and finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
  *     caches and out.  Strides in elements, innermost axis dense.
- *   - The tensor-core kernel takes D <= 128 in multiples of 8, page_size a multiple of 64, or 8, 16 or 32, up to 128 query heads per kv head, and 16-byte aligned pointers and strides of q and the caches; everything else
- *     runs on a slower generic kernel.
+ *   - The tensor-core kernel takes D <= 128 in multiples of 8; page_size 8, 16, 32 or a multiple of 64; up to 128 query
+ *     heads per kv head (G), of which G * 8 / gcd(G, 8) <= 128; scale >= 1e-30; pointers of q and the caches on 16-byte
+ *     boundaries and their strides (of axes longer than one) positive multiples of 16 bytes.  Everything else runs on a
+ *     slower generic kernel.
  *   - workspace: 32-byte aligned device memory of at least specsteer_chunk_attention_workspace(desc) bytes, whose content
  *     before and after the call means nothing; calls that may overlap (two streams, two graphs) need one each.
  * Same inputs give the same bits.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE (too small), CUDA. */

@@ -19,7 +19,7 @@
 // work on the other.  With two query tiles each stream owns one and both use every key tile; with one query tile the
 // streams take the key tiles in turn and are put together at the end.
 //
-// Maximum.  Weights are 2^(c s - c m) with a reference m per row.  A block is weighed against the reference there is; only
+// Maximum.  Weights are 2^(c s - c m + lift) with a reference m per row.  A block is weighed against the reference there is; only
 // if that makes its weights sum to more than 2^15 (or there is none yet) the block's maximum is formed, the reference raised,
 // O_s rescaled in tensor memory and the block weighed again.  Weights are then at most 2^15, which float16 holds, and after
 // the first tile hardly any block needs its maximum, a sixth of the work.
@@ -43,6 +43,10 @@ constexpr int kTcThreads = 32 * (kSoftmaxWarps + 4);
 constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
 constexpr int kPolyPairs = 6;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
 constexpr float kMostSum = 32768.f; // of the weights of a row and block before the reference is raised
+constexpr float kMostArg = 15.f;    // the exponent that no such weight exceeds
+// The largest weight is 2^kLift: with float16 the weights below 2^-22 of the largest are subnormal, not those below 2^-14,
+// and a whole block of largest ones still sums to less than kMostSum.
+template <bool BF> constexpr float kLift = BF ? 0.f : 8.f;
 constexpr int kPieces = 4;          // pieces of work the producer may be ahead
 
 template <int DP> struct TcLayout {
@@ -834,8 +838,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 m = top;
                 none = __any_sync(kFullMask, m == kNegInf);
               }
-              const float ref = m == kNegInf ? 0.f : m * c;
-              const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
+              const float up = m == kNegInf ? 0.f : fmaf(m, -c, kLift<BF>);
+              const float2 c2 = make_float2(c, c), ref2 = make_float2(up, up);
+              float poly_top = kNegInf;   // ex2_poly takes no more than 127
               float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
               // The weights go to the second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
 #pragma unroll
@@ -845,6 +850,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 for (int j = 0; j < 16; ++j) {
                   const float2 x2 = fma2(make_float2(v[i + 2 * j], v[i + 2 * j + 1]), c2, ref2);
                   const bool poly = ((i / 2 + j) * kPolyPairs) % 32 < kPolyPairs;
+                  if (poly) poly_top = max3(poly_top, x2.x, x2.y);
                   const float2 y = poly ? ex2_poly(x2) : make_float2(ex2(x2.x), ex2(x2.y));
                   sum[j & 3] = add2(sum[j & 3], y);
                   w16[j] = pack2<BF>(y.x, y.y);
@@ -853,7 +859,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               }
               sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
               const float total = sum[0].x + sum[0].y;
-              if (raise || __all_sync(kFullMask, !live || total <= kMostSum)) {
+              if (raise || __all_sync(kFullMask, !live || (total <= kMostSum && poly_top <= kMostArg))) {
                 l += total;
                 break;
               }
@@ -955,8 +961,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
         }
         if (live && (two || s == 0)) {
-          if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m * c, l);   // c > 0: -inf stays
-          else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m * c + log2f(l)) * kLn2;
+          if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m * c - kLift<BF>, l);   // c > 0: -inf stays
+          else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m * c - kLift<BF> + log2f(l)) * kLn2;
         }
       }
       if (tid == 0 && !whole) {
@@ -1136,13 +1142,16 @@ cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStrea
 
 }  // namespace
 
+// From here on scale times a reference is an ordinary number (masked scores are -inf before the scale is applied, so zero is none).
+constexpr float kLeastScale = 1e-30f;
+
 bool attention_tc_takes(const specsteer_attention_desc* d) {
   int tok, boxes;
   auto a16 = [](const void* q) { return ((uintptr_t)q & 15u) == 0; };
   // strides of axes longer than one: positive multiples of 16 bytes below the tensor map's limit
   auto ok = [](long long stride, long long extent) { return extent <= 1 || (stride > 0 && stride % 8 == 0 && stride < (1ll << 38)); };
   const int pr = d->page_size < kBlock ? d->page_size : kBlock;
-  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->D >= 64 && d->D <= 128 && d->D % 8 == 0 && pr % 8 == 0 && kBlock % pr == 0 && d->page_size % pr == 0 &&
+  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->D <= 128 && d->D % 8 == 0 && d->scale >= kLeastScale && pr % 8 == 0 && kBlock % pr == 0 && d->page_size % pr == 0 &&
          query_box(d->Hq / d->Hkv, &tok, &boxes) && a16(d->q) && a16(d->k_cache) && a16(d->v_cache) && ok(d->q_tok, d->T) && ok(d->q_head, d->Hq) &&
          ok(d->kc_page, d->n_pages) && ok(d->kc_slot, d->page_size) && ok(d->kc_head, d->Hkv) && ok(d->vc_page, d->n_pages) &&
          ok(d->vc_slot, d->page_size) && ok(d->vc_head, d->Hkv);
@@ -1168,7 +1177,6 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   p.page_shift = 0;
   while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
   p.c = d->scale * kLog2e;
-  if (p.c < 1e-30f) p.c = 1e-30f;   // a scale of zero: weights all 1 without 0 * infinity for masked scores
   p.out_vec = ((uintptr_t)d->out & 31u) == 0 && d->o_tok % 16 == 0 && d->o_head % 16 == 0 && d->D % 16 == 0;
   p.part = (float*)d->workspace;
   p.part_ml = (float2*)((char*)d->workspace + part_bytes(DP));

@@ -212,6 +212,12 @@ SHAPES = [
     ("width_80", [(5, 200), (40, 200)], 6, 2, 80, 16, BF16, 0, "joined"),
     ("width_96", [(5, 200), (130, 150)], 4, 4, 96, 64, F16, 0, "nhd"),
     ("width_33", [(4, 60)], 4, 2, 33, 16, BF16, 0, "nhd"),
+    ("width_8", [(4, 60), (1, 300), (200, 200)], 4, 2, 8, 16, F16, 0, "nhd"),
+    ("width_40", [(5, 200), (130, 150)], 4, 2, 40, 64, BF16, 0, "hnd"),
+    ("page_of_192", [(5, 700), (130, 385), (2, 192)], 8, 2, 128, 192, BF16, 0, "nhd"),
+    ("group_of_128", [(3, 200)], 128, 1, 64, 16, BF16, 0, "nhd"),
+    ("group_of_136", [(2, 70)], 136, 1, 64, 16, BF16, 0, "nhd"),
+    ("window_past_all", [(5, 300), (1, 1)], 4, 2, 64, 16, BF16, 2 ** 31 - 1, "nhd"),
     ("width_256", [(3, 90), (20, 50)], 4, 2, 256, 16, BF16, 0, "nhd"),
     ("groups_of_5", [(5, 200), (60, 333)], 10, 2, 128, 16, BF16, 0, "nhd"),
     ("groups_of_7", [(9, 150), (50, 150)], 14, 2, 64, 16, BF16, 0, "hnd"),
@@ -317,6 +323,62 @@ def test_attention_strided_q_and_out(binding):
         assert (buf[..., :3] == 7).all() and (buf[..., 131:] == 7).all()
 
 
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+@pytest.mark.parametrize("above", [100.0, 140.0, 200.0, 300.0])
+def test_attention_one_key_far_above_those_before_it(binding, above, generic):
+    """A key anywhere in a block of keys whose score is a hundred or more above every score so far takes all the weight."""
+    kc, vc, table, cu, kv, T, g = build_cache([(1, 900)] * 64 + [(3, 640)] * 2, 16, 1, 64, BF16, "cuda", 21)
+    kc[torch.isfinite(kc)] = 0
+    for b in range(66):
+        j = 576 + b % 64
+        kc[int(table[b, j // 16]), j % 16, 0, 0] = above
+    q = torch.zeros(T, 2, 64, dtype=BF16, device="cuda")
+    q[..., 0] = 1
+    out, lse = torch.full_like(q, 7.0), torch.full((T, 2), 7.0, device="cuda")
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), scale=1.0, out=out, lse=lse, generic=generic)
+    _compare(out, lse, attention_reference(q, kc, vc, table, cu, kv, 1.0))
+
+
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+def test_attention_many_small_weights_of_float16(binding, generic):
+    """In every 128 keys one that takes nearly all the weight, with value 0, and 127 of 2^-25.2 of its weight, which are all
+    that the result consists of.
+
+    With the weights held 2^8 up, a weight below float16's normal range is off by 2^-25 against a largest one of 2^8, so
+    the reference's term for it shrinks by 2^8."""
+    n = 1280
+    kc, vc, table, cu, kv, T, g = build_cache([(1, n)], 64, 1, 64, F16, "cuda", 22)
+    used = torch.isfinite(kc)
+    kc[used], vc[used] = 0, 100.0
+    for j in range(0, n, 128):
+        page = int(table[0, j // 64])
+        kc[page, 0, 0, 0] = 17.5
+        vc[page, 0] = 0
+    q = torch.zeros(T, 1, 64, dtype=F16, device="cuda")
+    q[..., 0] = 1
+    out, lse = torch.full_like(q, 7.0), torch.full((T, 1), 7.0, device="cuda")
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), scale=1.0, out=out, lse=lse, generic=generic)
+    want, want_lse, tol, tol_lse, written = attention_reference(q, kc, vc, table, cu, kv, 1.0)
+    tol = tol - n * 2.0 ** -25 * 100.0 * (1 - 2.0 ** -8)
+    assert want.min() > 2e-4 and tol.max() < 2e-5
+    _compare(out, lse, (want, want_lse, tol, tol_lse, written))
+
+
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+def test_attention_tiny_scale(binding, generic):
+    """Huge queries and keys with a scale that brings their products back to ordinary scores, and one that makes them nothing."""
+    kc, vc, table, cu, kv, T, g = build_cache([(5, 300), (1, 200)], 16, 2, 64, BF16, "cuda", 23)
+    kc *= 3e17
+    q = (torch.randn(T, 4, 64, generator=g) * 3e17).to(BF16).cuda()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    for scale in (1e-35, 0.0):
+        out, lse = torch.full_like(q, 7.0), torch.full((T, 4), 7.0, device="cuda")
+        binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), scale=scale, out=out, lse=lse, generic=generic)
+        _compare(out, lse, attention_reference(q, kc, vc, table, cu, kv, float(np.float32(scale))))
+
+
 def test_attention_same_bits_again_and_beside_other_work(binding):
     lens = [(5, 2000), (5, 70), (1, 900), (300, 700)]
     kc, vc, table, cu, kv, T, g = build_cache(lens, 16, 2, 128, BF16, "cuda", 13)
@@ -352,6 +414,105 @@ def test_attention_refuses_small_workspace_and_bad_arguments(binding):
     with pytest.raises(binding.SpecSteerError) as e:
         binding.chunk_attention(q[:, :7], kc, vc, table, cu_t, kv_t)          # 7 heads over 2
     assert e.value.code == binding.ERR_INVALID_ARG
+
+
+def test_attention_workspaces_that_do_not_serve(binding):
+    lens = [(5, 100)]
+    kc, vc, table, cu, kv, T, g = build_cache(lens, 16, 2, 128, BF16, "cuda", 14)
+    q = torch.randn(T, 8, 128, generator=g).to(BF16).cuda()
+    cu_t, kv_t = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in (cu, kv))
+    want, want_lse = binding.chunk_attention(q, kc, vc, table, cu_t, kv_t)
+    room = torch.empty(200 << 20, dtype=torch.uint8, device="cuda")
+    got, lse = binding.chunk_attention(q, kc, vc, table, cu_t, kv_t, workspace=room[64:])
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    for bad in (room[:1 << 20], room[8:], room[:0]):
+        with pytest.raises(binding.SpecSteerError) as e:
+            binding.chunk_attention(q, kc, vc, table, cu_t, kv_t, workspace=bad)
+        assert e.value.code == binding.ERR_WORKSPACE
+    binding.chunk_attention(q, kc, vc, table, cu_t, kv_t, workspace=room[:0], generic=True)     # needs none
+
+
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+def test_cache_beyond_32_bit_offsets(binding, generic):
+    """Pools of more than 2^31 elements, of which only the last pages are used."""
+    P, page, Hkv, D, n, kv = 140_000, 16, 8, 128, 6, 150
+    kc, vc = (torch.empty(P, page, Hkv, D, dtype=BF16, device="cuda") for _ in range(2))
+    assert kc.numel() > 2 ** 31
+    g = torch.Generator().manual_seed(31)
+    pages = [P - 1 - 3 * i for i in range(-(-kv // page))]
+    table = torch.tensor([pages], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(kv, Hkv, D, generator=g).to(BF16) for _ in range(2))
+    slots = torch.tensor([pages[i // page] * page + i % page for i in range(kv)], device="cuda")
+    binding.cache_append(k.cuda(), v.cuda(), kc, vc, slots)
+    assert torch.equal(kc[pages[0], :, 3].cpu(), k[:page, 3]) and torch.equal(vc[pages[-1], 0].cpu(), v[(len(pages) - 1) * page])
+    vc[pages[-1], (kv - 1) % page, 2, 9] = float("inf")          # seen by the last row alone
+    v[kv - 1, 2, 9] = 0
+    q = torch.randn(n, 16, D, generator=g).to(BF16).cuda()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    out, lse = binding.chunk_attention(q, kc, vc, table, i32([0, n]), i32([kv]), generic=generic)
+    assert torch.isposinf(out[n - 1, 4:6, 9]).all() and torch.isposinf(out).sum() == 2
+    out[n - 1, 4:6, 9] = 0
+    ref = list(attention_reference(q, k[None], v[None], torch.zeros(1, 1, dtype=torch.int32), [0, n], [kv], 1 / math.sqrt(D)))
+    ref[0][n - 1, 4:6, 9] = 0
+    _compare(out, lse, ref)
+
+
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+def test_attention_thousands_of_requests(binding, generic):
+    """More requests than a block has threads several times over, many of them idle."""
+    lens = [((0, 1, 0, 3, 1)[i % 5], (i * 7) % 45 + 3) for i in range(5001)]
+    out, lse, status, ref = _attend(binding, lens, 2, 1, 64, 16, BF16, seed=32, generic=generic)
+    _compare(out, lse, ref)
+    assert (status == 0).all()
+
+
+def test_calls_of_several_host_threads(binding):
+    """Threads with a stream each, different shapes at once: every result is what a call alone gives."""
+    import threading
+    cases = []
+    for i, (lens, Hq, Hkv, D, page, dtype) in enumerate([([(5, 900), (5, 30)], 8, 2, 128, 16, BF16), ([(1, 700)] * 9, 4, 4, 64, 32, F16), ([(200, 300)], 4, 1, 96, 64, BF16), ([(3, 90)], 2, 1, 200, 16, BF16)]):
+        kc, vc, table, cu, kv, T, g = build_cache(lens, page, Hkv, D, dtype, "cuda", 40 + i)
+        q = torch.randn(T, Hq, D, generator=g).to(dtype).cuda()
+        args = (q, kc, vc, table) + tuple(torch.tensor(v, dtype=torch.int32, device="cuda") for v in (cu, kv))
+        cases.append((args, binding.chunk_attention(*args)))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(args, want):
+        s = torch.cuda.Stream()
+        for _ in range(30):
+            out, lse = binding.chunk_attention(*args, stream=s)
+            s.synchronize()
+            if not (torch.equal(out, want[0]) and torch.equal(lse, want[1])):
+                wrong.append(args[0].shape)
+    threads = [threading.Thread(target=work, args=c) for c in cases]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_two_captured_calls_replayed_at_once(binding):
+    """Two graphs of the attention, each with a workspace of its own, replayed on two streams at the same time."""
+    graphs = []
+    for seed, lens in ((50, [(5, 3000), (5, 40)]), (51, [(150, 900)])):
+        kc, vc, table, cu, kv, T, g = build_cache(lens, 16, 2, 128, BF16, "cuda", seed)
+        q = torch.randn(T, 8, 128, generator=g).to(BF16).cuda()
+        args = (q, kc, vc, table) + tuple(torch.tensor(v, dtype=torch.int32, device="cuda") for v in (cu, kv))
+        want = binding.chunk_attention(*args)
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=stream):
+            got = binding.chunk_attention(*args)
+        graphs.append((graph, stream, args, want, got))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, stream, *_ in graphs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, _, _, want, got in graphs:
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
 
 
 # ---- a run of them together -------------------------------------------------------------------------------------------
