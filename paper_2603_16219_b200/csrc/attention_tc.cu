@@ -1129,7 +1129,7 @@ cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStrea
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, 8);
+  cfg.gridDim = dim3(grid, 16);
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
