@@ -36,12 +36,11 @@ namespace {
 
 constexpr int kKeys = 128;          // keys per tile
 constexpr int kBlock = 64;          // keys per block: half a tile, what a barrier or a box covers
-constexpr int kMaxStages = 10;
 constexpr int kSoftmaxWarps = 8;
 constexpr int kKeyWarp = kSoftmaxWarps, kValueWarp = kSoftmaxWarps + 1, kMmaWarp = kSoftmaxWarps + 2;
 constexpr int kTcThreads = 32 * (kSoftmaxWarps + 4);
 constexpr uint32_t kTcCols = 512;   // S0, S1, O0, O1 of 128 columns each
-constexpr int kPolyPairs = 6;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit
+constexpr int kPolyPairs = 5;       // of 32 pairs of weights, how many ex2_poly takes off the special-function unit (4 to 6 are alike)
 constexpr float kMostSum = 32768.f; // of the weights of a row and block before the reference is raised
 constexpr float kMostArg = 15.f;    // the exponent that no such weight exceeds
 // The largest weight is 2^kLift: with float16 the weights below 2^-22 of the largest are subnormal, not those below 2^-14,
@@ -70,8 +69,17 @@ struct Piece {
   int index;                   // of the pieces of this CTA
 };
 
+// Barriers of the two rings, per stage.  A block of a piece with one query tile is one stream's alone: barriers of its own
+// (full 0, 1) say that it has landed, and one arrival frees it; with two query tiles both streams wait for it (full 2) and
+// free it.  So every barrier is waited for each time it comes around by all that it concerns, and no phase is mistaken for
+// another.  (With one set for all, each
+// stream had to wait for the other's blocks too: contexts of 30 to 120 thousand took 162 us instead of 158.)
+template <int DP> struct RingBars {
+  uint64_t k_full[3][TcLayout<DP>::kStages], v_full[3][TcLayout<DP>::kStages];
+  uint64_t k_empty[2][TcLayout<DP>::kStages], v_empty[2][TcLayout<DP>::kStages];   // one stream's, both streams'
+};
+
 struct TcShared {
-  uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
   uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2][2], p_full[2][2];   // [s][h]: scores, weights of stream s, first / last 64 keys of a tile
   uint64_t o_full[2], half_done[2];      // a piece's sums; those of the stream but for the last 64 keys
@@ -82,20 +90,20 @@ struct TcShared {
   int start_b, start_hk, start_u, start_off;
   long long end;           // where this CTA's range ends, from the beginning of its first unit (0: it has none)
   Piece piece[kPieces];
-  uint32_t bad[32];        // per block of keys (counted modulo 32): the boxes of it that lie outside the pool
+  uint8_t bad[32];         // per block of keys (counted modulo 32): the boxes of it that lie outside the pool
   union {
     long long scan[kTcThreads / 32];
     float2 exch[2][128];   // reference and sum of each stream's rows
   };
 };
-template <int DP> constexpr int tc_smem_bytes() { return TcLayout<DP>::kControl + (int)sizeof(TcShared); }
-static_assert(tc_smem_bytes<128>() <= 232448 && tc_smem_bytes<64>() <= 232448, "shared memory of one CTA");
+template <int DP> constexpr int tc_smem_bytes() { return TcLayout<DP>::kControl + (int)(sizeof(TcShared) + sizeof(RingBars<DP>)); }
+static_assert(sizeof(TcShared) % 8 == 0 && tc_smem_bytes<128>() <= 232448 && tc_smem_bytes<64>() <= 232448, "shared memory of one CTA");
 
 struct TcParams {
   specsteer_attention_desc d;
   int G, box_tok, box_rows, tile_tok;  // query box: tokens and rows; tokens of a query tile
   int page_rows, boxes, page_shift;    // key box: keys, boxes per block, log2 of its keys
-  int page_blocks;                     // blocks per page (1 when a block has several pages)
+  int page_blocks, pb_shift;           // blocks per page (1 when a block has several pages), log2 of them or -1
   float c;                             // scale * log2(e)
   int out_vec;                         // out rows are 32-byte aligned and a multiple of 32 bytes long
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
@@ -425,13 +433,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t smem0 = smem_u32(smem_raw);
   TcShared* sh = reinterpret_cast<TcShared*>(smem_raw + L::kControl);
+  RingBars<DP>* ring = reinterpret_cast<RingBars<DP>*>(sh + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   pdl_launch_dependents();   // attention_join_kernel may come up; it waits for the end of this kernel before it reads
   if (tid == 0) {
     for (int i = 0; i < L::kStages; ++i) {
-      mbar_init(&sh->k_full[i], 1); mbar_init(&sh->k_empty[i], 2);
-      mbar_init(&sh->v_full[i], 1); mbar_init(&sh->v_empty[i], 2);
+      for (int j = 0; j < 3; ++j) { mbar_init(&ring->k_full[j][i], 1); mbar_init(&ring->v_full[j][i], 1); }
+      for (int j = 0; j < 2; ++j) { mbar_init(&ring->k_empty[j][i], 1 + j); mbar_init(&ring->v_empty[j][i], 1 + j); }
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 2);
@@ -446,6 +455,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     sh->end = 0;
     fence_barrier_init();
   }
+  if (warp == kKeyWarp) sh->bad[lane] = 0;
   if (warp == kMmaWarp) tc_alloc(&sh->tmem_slot);
 
   // ---- this CTA's range of the list of key tiles
@@ -497,9 +507,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const bool loads = box < p.boxes;
     const uint32_t lane_off = smem0 + (keys ? L::kKeyRing : L::kValueRing) + (uint32_t)chunk * (kBlock * 128) + (uint32_t)box * p.page_rows * 128;
     const CUtensorMap* tm = keys ? &tm_k : &tm_v;
-    uint64_t* full = keys ? sh->k_full : sh->v_full;
-    uint64_t* empty = keys ? sh->k_empty : sh->v_empty;
-    int blocks = 0, qi = 0, pc = 0;
+    uint64_t (*full)[L::kStages] = keys ? ring->k_full : ring->v_full;
+    uint64_t (*empty)[L::kStages] = keys ? ring->k_empty : ring->v_empty;
+    // Bits per stage: the parity to wait for next of its two empty barriers (a stage not used before is free: parity 1 of the
+    // first), whether its last block was for both streams, of which stream it was else, the parity of its full barriers.
+    uint32_t free_one = ~0u, free_two = 0, last_two = 0, last_own = 0, landed0 = 0, landed1 = 0, landed2 = 0;
+    bool any_bad = false;
+    int stage = 0, qi = 0, pc = 0, blocks = 0;
     int limit = kPolls;
     Walk w;
     w.begin(sh);
@@ -521,15 +535,16 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tc_wait<true>(&sh->piece_full[pc % kPieces], turn, limit);
         if (limit == 0) break;
       }
-      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2;
+      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, two = x->two;
       if (take <= 0) break;
-      const int n_q = !keys ? 0 : x->two ? 2 : 1;
+      const int n_q = !keys ? 0 : two ? 2 : 1;
       const int* table = p.d.block_table + (long long)b * p.d.ld_table;
+      auto page_at = [&](int blk) { return p.pb_shift >= 0 ? blk >> p.pb_shift : blk / p.page_blocks; };   // pages of 64 keys or more
       // page of this lane's box of tile t of the piece: the id, or n_pages (a coordinate outside, which reads zeros) for none
       auto page_of = [&](int t) -> int {
         const int blk = first + 2 * t + half;
         int page = p.d.n_pages;
-        if (loads && t < take && blk * kBlock + box * p.page_rows < kv) page = __ldg(table + (p.boxes > 1 ? blk * p.boxes + box : blk / p.page_blocks));
+        if (loads && t < take && blk * kBlock + box * p.page_rows < kv) page = __ldg(table + (p.boxes > 1 ? blk * p.boxes + box : page_at(blk)));
         return page;
       };
       int page = page_of(0), page1 = page_of(1), q_done = 0;
@@ -559,28 +574,39 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const bool outside = page < 0 || page >= p.d.n_pages;
         if (keys) {
           const uint32_t votes = __ballot_sync(kFullMask, loads && outside && blk * kBlock + box * p.page_rows < kv);
-          if ((lane & 15) == 0) {
+          any_bad = any_bad || votes;   // (until then the words are zero)
+          if (any_bad && (lane & 15) == 0) {
             uint32_t bad = 0;
-            if (votes) {
 #pragma unroll 1
-              for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (16 * half + i * chunks)) & 1u) << i;
-              if (bad && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_PAGE);
-            }
+            for (int i = 0; i < p.boxes; ++i) bad |= ((votes >> (16 * half + i * chunks)) & 1u) << i;
+            if (bad && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_PAGE);
             // the softmax warps read the word at most the ring and the blocks in work later, well under 32
-            *reinterpret_cast<volatile uint32_t*>(&sh->bad[(blocks + half) & 31]) = bad;
+            *reinterpret_cast<volatile uint8_t*>(&sh->bad[(blocks + half) & 31]) = (uint8_t)bad;   // at most 8 boxes
           }
         }
         const int page2 = page_of(t + 2);
-        const int st0 = blocks % L::kStages, st1 = (blocks + 1) % L::kStages, st = half ? st1 : st0;
-        tc_wait<true>(&empty[st0], (uint32_t)((blocks / L::kStages) & 1) ^ 1u, limit);
-        tc_wait<true>(&empty[st1], (uint32_t)(((blocks + 1) / L::kStages) & 1) ^ 1u, limit);
+        // each half of the warp waits for its block's stage
+        const int stage1 = stage + 1 < L::kStages ? stage + 1 : 0, st = half ? stage1 : stage;
+        const uint32_t bits = (1u << stage) | (1u << stage1);
+        const bool was_two = (last_two >> st) & 1u;
+        tc_wait<true>(&empty[was_two][st], ((was_two ? free_two : free_one) >> st) & 1u, limit);
         if (limit == 0) break;
-        if ((lane & 15) == 0) mbar_arrive_expect_tx(&full[st], L::kStageBytes);
+        free_two ^= bits & last_two;
+        free_one ^= bits & ~last_two;
+        const int set = two ? 2 : t & 1;
+        last_two = two ? last_two | bits : last_two & ~bits;
+        last_own = t & 1 ? last_own | bits : last_own & ~bits;
+        if (set == 0) landed0 ^= bits;
+        if (set == 1) landed1 ^= bits;
+        if (set == 2) landed2 ^= bits;
+        if ((lane & 15) == 0) mbar_arrive_expect_tx(&full[set][st], L::kStageBytes);
         __syncwarp();
-        if (loads)
-          tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, p.page_blocks > 1 ? blk % p.page_blocks * kBlock : 0, hk,
-                 outside ? p.d.n_pages : page, &full[st]);
+        if (loads) {
+          const int in_page = p.page_blocks > 1 ? (blk - page_at(blk) * p.page_blocks) * kBlock : 0;
+          tma_4d(lane_off + st * L::kStageBytes, tm, chunk * 64, in_page, hk, outside ? p.d.n_pages : page, &full[set][st]);
+        }
         blocks += 2;
+        stage = stage1 + 1 < L::kStages ? stage1 + 1 : 0;
         page = page1; page1 = page2;
       }
       if (limit == 0) break;
@@ -591,7 +617,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       gave_up(p);
       limit = kPolls;
       // copies already issued may still be landing: wait for them (bounded) before the CTA exits
-      for (int i = blocks > L::kStages ? blocks - L::kStages : 0; i < blocks; ++i) tc_wait<false>(&full[i % L::kStages], (uint32_t)((i / L::kStages) & 1), limit);
+      for (int i = 0; i < min(blocks, L::kStages); ++i) {
+        const bool t2 = (last_two >> i) & 1u, t1 = (last_own >> i) & 1u;
+        tc_wait<false>(&full[t2 ? 2 : t1 ? 1 : 0][i], (((t2 ? landed2 : t1 ? landed1 : landed0) >> i) & 1u) ^ 1u, limit);
+      }
       for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_wait<false>(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1), limit);
     }
   } else if (warp >= kMmaWarp) {
@@ -605,18 +634,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t p_phase = 0;
     int limit = kPolls;
     auto wait = [&](uint64_t* bar, uint32_t parity) { tc_wait<true>(bar, parity, limit); };
-    // Block `it` of a ring.  Both issuers pass over every block in order, so that neither can mistake a phase of a barrier for
-    // one two uses later: a block of the other stream's tile is let go as soon as it has landed.
-    int k_next = 0, v_next = 0;
-    auto pass = [&](uint64_t* full, uint64_t* empty, int& next, int until) {
-#pragma unroll 1
-      for (; next < until; ++next) {
-        wait(&full[next % L::kStages], (uint32_t)((next / L::kStages) & 1));
-        if (lane == 0) mbar_arrive(&empty[next % L::kStages]);
-        __syncwarp();
-      }
-      next = until + 1;
-    };
+    uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // parity of each stage's full barriers, a bit a stage
 #pragma unroll 1
     for (;; ++pc) {
       wait(&sh->piece_full[pc % kPieces], (uint32_t)((pc / kPieces) & 1));
@@ -631,17 +649,21 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       // both tiles if there are two, so that no phase of either barrier is passed unseen
       wait(&sh->q_full[qi & 1], (uint32_t)((qi >> 1) & 1));
       if (two) wait(&sh->q_full[(qi + 1) & 1], (uint32_t)(((qi + 1) >> 1) & 1));
-      const int step = two ? 1 : 2, t_from = two ? 0 : s;
+      const int step = two ? 1 : 2, t_from = two ? 0 : s, set = two ? 2 : s;
+      uint32_t k_par = two ? k_both : k_own, v_par = two ? v_both : v_own;
+      int k_stage = (blocks0 + 2 * t_from) % L::kStages, v_stage = k_stage;   // of this stream's next block
+      auto advance = [&](int& stage, int by) { stage = stage + by >= L::kStages ? stage + by - L::kStages : stage + by; };
       const uint32_t q_desc = desc_rows(smem0 + qs * L::kQBytes);
 #pragma unroll 1
       for (int t = t_from - step; t < take; t += step) {   // the first turn forms the first scores alone
         const bool now = t >= t_from, next = t + step < take;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int it = blocks0 + 2 * t + h, stage = it % L::kStages;
+          const int stage = v_stage;
           if (now) {
-            pass(sh->v_full, sh->v_empty, v_next, it);
-            wait(&sh->v_full[stage], (uint32_t)((it / L::kStages) & 1));
+            wait(&ring->v_full[set][stage], (v_par >> stage) & 1u);
+            v_par ^= 1u << stage;
+            advance(v_stage, h == 0 ? 1 : 2 * step - 1);
             wait(&sh->p_full[s][h], p_phase);
             fence_after();
             const uint32_t b = desc_cols(smem0 + L::kValueRing + stage * L::kStageBytes);
@@ -652,20 +674,21 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (next) {
             // Scores of block h of tile t + step.  The commit also says that the product with the block's values before it
             // is complete.
-            const int it2 = it + 2 * step, stage2 = it2 % L::kStages;
-            pass(sh->k_full, sh->k_empty, k_next, it2);
-            wait(&sh->k_full[stage2], (uint32_t)((it2 / L::kStages) & 1));
+            const int stage2 = k_stage;
+            wait(&ring->k_full[set][stage2], (k_par >> stage2) & 1u);
+            k_par ^= 1u << stage2;
+            advance(k_stage, h == 0 ? 1 : 2 * step - 1);
             const uint32_t b = desc_rows(smem0 + L::kKeyRing + stage2 * L::kStageBytes);
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k)
               mma_ss(t_s + h * 64, q_desc + (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2), b + (uint32_t)((k >> 2) * ((kBlock * 128) >> 4) + (k & 3) * 2),
                      id_qk, k != 0);
             mma_commit(&sh->s_full[s][h]);
-            mma_commit(&sh->k_empty[stage2]);
+            mma_commit(&ring->k_empty[two][stage2]);
           } else if (h == 0 && now) {
             mma_commit(&sh->half_done[s]);
           }
-          if (now) mma_commit(&sh->v_empty[stage]);
+          if (now) mma_commit(&ring->v_empty[two][stage]);
         }
         if (now) p_phase ^= 1u;
       }
@@ -675,9 +698,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (two) mma_commit(&sh->q_empty[qs]);   // (its barrier counts both issuers, and this tile is the stream's alone)
       qi += two ? 2 : 1;
       blocks0 += 2 * take;
-      pass(sh->k_full, sh->k_empty, k_next, blocks0);   // what the other stream had last
-      pass(sh->v_full, sh->v_empty, v_next, blocks0);
-      k_next = v_next = blocks0;
+      if (two) { k_both = k_par; v_both = v_par; }
+      else { k_own = k_par; v_own = v_par; }
       if (limit == 0) break;
     }
     if (limit == 0) {   // let everything issued finish before tensor memory is given back
@@ -698,6 +720,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t s_phase = 0, half_phase = 0;   // s_phase: of both blocks at the beginning of a tile
     uint32_t group_phase = 0, both_phase = 0;
     int blocks0 = 0, pc = 0;     // blocks0: of the pieces before
+    uint32_t v_own = 0, v_both = 0;         // as the issuer's
     int limit = kPolls;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       tc_wait<true>(bar, parity, limit);
@@ -736,21 +759,23 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       float m = live ? kNegInf : 0.f, l = 0.f;       // reference (raw score; none yet: -inf), sum
       bool none = true;                 // some row of the warp has no reference yet
       const int step = two ? 1 : 2, t_from = two ? 0 : s;
+      uint32_t v_par = two ? v_both : v_own;
+      int v_first = (blocks0 + 2 * t_from) % L::kStages;   // stage of the tile's first block
 #pragma unroll 1
       for (int t = t_from; t < take; t += step) {
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           const int k0 = (first + t) * kKeys + h * kBlock;
           wait(&sh->s_full[s][h], s_phase);   // the block's keys have landed, and what was loaded before them
-          const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sh->bad[(blocks0 + 2 * t + h) & 31]);
+          const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&sh->bad[(blocks0 + 2 * t + h) & 31]);
           const bool edge = k0 + kBlock > hi_first || k0 < lo_last || bad != 0;
           if (edge) {
             // Values of keys that some row of the unit does not see.  What lies behind the last key in its page becomes zero
             // (whole pages behind it, and pages outside the pool, were loaded as zeros); an infinity or NaN among the others is
             // taken out here, where it would reach rows with weight 0, and added in the epilogue to the rows that see it.
-            const int it = blocks0 + 2 * t + h;
-            wait(&sh->v_full[it % L::kStages], (uint32_t)((it / L::kStages) & 1));
-            unsigned char* vt = smem_raw + L::kValueRing + (it % L::kStages) * L::kStageBytes;
+            const int v_stage = v_first + h < L::kStages ? v_first + h : 0;
+            wait(&ring->v_full[two ? 2 : s][v_stage], (v_par >> v_stage) & 1u);
+            unsigned char* vt = smem_raw + L::kValueRing + v_stage * L::kStageBytes;
             const int kv_here = min(kBlock, max(0, x.kv - k0));
             const int from = min(kv_here, max(0, lo_last - k0)), to = min(kv_here, max(from, hi_first - k0));
             const int zero_to = min(kBlock, (kv_here + p.page_rows - 1) & -p.page_rows);
@@ -871,9 +896,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh->p_full[s][h]);
         }
+        v_par ^= (1u << v_first) | (1u << (v_first + 1 < L::kStages ? v_first + 1 : 0));
+        v_first += 2 * step;
+        if (v_first >= L::kStages) v_first -= L::kStages;
         s_phase ^= 1u;
       }
       if (t_from < take) half_phase ^= 1u;
+      if (two) v_both = v_par;
+      else v_own = v_par;
       // ---- end of the piece
       const int n1 = two ? take : take / 2;   // tiles of the second stream
       const bool whole = x.starts && x.ends;
@@ -1174,6 +1204,8 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   p.page_rows = d->page_size < kBlock ? d->page_size : kBlock;
   p.boxes = kBlock / p.page_rows;
   p.page_blocks = d->page_size / p.page_rows;
+  p.pb_shift = p.page_blocks & (p.page_blocks - 1) ? -1 : 0;
+  while (p.pb_shift >= 0 && (1 << p.pb_shift) < p.page_blocks) ++p.pb_shift;
   p.page_shift = 0;
   while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
   p.c = d->scale * kLog2e;
