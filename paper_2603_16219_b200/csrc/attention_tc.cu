@@ -24,12 +24,14 @@
 // reference raised, O_s rescaled in tensor memory and the block weighed again.  Weights are then at most 2^15, which
 // float16 holds, and after the first tile hardly any block needs its maximum, a sixth of the work.
 //
-// Measured (float16 or bfloat16, D = 128 unless said, whole call): 3 requests of 30 to 120 thousand keys with 9 tokens of 64
-// heads 158 to 165 us, 5.6 to 5.8 TB/s; 256 requests of up to 4000 keys with 5 tokens of 64 heads 373 to 395 us, 5.6 to 5.9 TB/s:
-// bound by HBM.  One prompt of 8192 tokens of 32 heads 0.55 to 0.61 ms, 0.90 to 1.0 PFLOP/s, the tensor pipe busy for 45 % of
-// the cycles: bound by the issue of the softmax warps, and by the power limit's clock.  64 single tokens of D = 64 over up to
-// 4000 keys 77 us, 3.4 TB/s: the few rows of a request sit in one warp of each stream, whose 2000 clocks for a block of 64 keys
-// (1500 of arithmetic and tensor-memory latency, 500 of handshakes) bound it.
+// Measured (bfloat16 and D = 128 unless said, the whole call):
+//   3 requests of 30 to 120 thousand keys, 9 tokens of 64 heads        158 to 165 us, 5.6 to 5.8 TB/s: bound by HBM
+//   256 requests of up to 4000 keys, 5 tokens of 64 heads              373 to 395 us, 5.6 to 5.9 TB/s: bound by HBM
+//   a prompt of 8192 tokens of 32 heads                                0.55 to 0.61 ms, 0.90 to 1.0 PFLOP/s: bound by the issue of
+//     the softmax warps and by the clock that the power limit leaves (tensor pipe busy for 45 % of the cycles)
+//   64 single tokens, up to 4000 keys, 32 heads of 64, float16         77 us, 3.4 TB/s: the few rows of a request sit in one warp
+//     of each stream, whose 2000 clocks a block of 64 keys (1500 of arithmetic and tensor-memory latency, 500 of
+//     handshakes) bound it
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1025,7 +1027,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 // Puts the parts of a cut unit together: blocks x take the unit that begins in CTA x and goes on in the CTAs behind it.
 // One warp a row; the parts are added in their order, so the bits do not depend on who came first.
 // It waits on latency (about ten dependent trips to L2): 4 to 8 us behind the main kernel, 15 to 17 us where every CTA's
-// range cuts a unit of 256 rows (35 MB of parts); with 8 or 32 blocks a unit instead of 16 long contexts took 3 us more.
+// range cuts a unit of 256 rows (35 MB of parts); with 8 blocks a unit instead of 16 long contexts took 3 us
+// more, with 32 the same.
 template <int DP, bool BF>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
   pdl_wait();
