@@ -445,7 +445,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   RingBars<DP>* ring = reinterpret_cast<RingBars<DP>*>(sh + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-  pdl_launch_dependents();   // attention_join_kernel may come up; it waits for the end of this kernel before it reads
   if (tid == 0) {
     for (int i = 0; i < L::kStages; ++i) {
       for (int j = 0; j < 3; ++j) { mbar_init(&ring->k_full[j][i], 1); mbar_init(&ring->v_full[j][i], 1); }
@@ -466,6 +465,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   }
   if (warp == kKeyWarp) sh->bad[lane] = 0;
   if (warp == kMmaWarp) tc_alloc(&sh->tmem_slot);
+  pdl_wait();                // so far nothing touched what the kernels before wrote or read
+  pdl_launch_dependents();   // attention_join_kernel may come up; it waits for the end of this kernel before it reads
 
   // ---- this CTA's range of the list of key tiles
   {
@@ -1031,12 +1032,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 // more, with 32 the same.
 template <int DP, bool BF>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
+  pdl_launch_dependents();   // the next call's main kernel may set itself up meanwhile
   pdl_wait();
   const int cta = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // what every row begins with, on its way before anything is known to be needed (the addresses are the workspace's own)
   const int4 h = *reinterpret_cast<const int4*>(p.head + cta * 8);
+  const int u = p.head[cta * 8 + 4], first_kind = lane == 0 ? 2 : cta + lane < n_cta ? p.head[(cta + lane) * 8 + 1] : 1;
   const int slot0 = h.x;
   if (slot0 < 0) return;
-  const int u = p.head[cta * 8 + 4];
   const AttnRequest rq = attn_request(p.d, h.z);
   const Unit x = make_unit(p, rq, u);
   const int rows = (x.tok1 - x.tok0) * p.G, tile_rows = p.tile_tok * p.G;
@@ -1050,7 +1053,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
     bool more = true;
     for (int base = cta; more && base < n_cta; base += 32) {
       const int i = base + lane;
-      const int kind = i == cta ? 2 : i < n_cta ? p.head[i * 8 + 1] : 1;
+      const int kind = base == cta ? first_kind : i < n_cta ? p.head[i * 8 + 1] : 1;
       const uint32_t ends = __ballot_sync(kFullMask, kind == 1);
       const uint32_t upto = ends ? (2u << (__ffs(ends) - 1)) - 1u : 0xffffffffu;   // lanes up to the first end (all: shift to 0)
       const bool has = kind != 0 && i < n_cta && ((upto >> lane) & 1u);
@@ -1167,18 +1170,23 @@ cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStrea
     if (e != cudaSuccess) return e;
     attr_set[dev & 63].store(true, std::memory_order_release);
   }
-  attention_tc_kernel<DP, BF><<<grid, kTcThreads, tc_smem_bytes<DP>(), s>>>(tm[0], tm[1], tm[2], p);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, 16);
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
+  // Both kernels may come up while the one before still runs (programmatic dependent launch); each waits for it before it
+  // reads or writes global memory.
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = tc_smem_bytes<DP>();
+  cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, attention_tc_kernel<DP, BF>, tm[0], tm[1], tm[2], p);
+  if (e != cudaSuccess) return e;
+  cfg.gridDim = dim3(grid, 16);
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, attention_join_kernel<DP, BF>, p, grid);
 }
 
