@@ -456,7 +456,8 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *   - out and lse overlap no input.
  *   - Requests with cu_new outside [0, T] or decreasing, or kv_len outside [0, table_width*page_size] or above 2^31 - 4097:
  *     BAD_LEN, nothing written.  Rows of no request are left as they are.
- *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.
+ *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.  Pages that end before the first key
+ *     that the request's first row sees (behind a window) may be gone: their ids do not matter.
  *   - req_status may be NULL; bits are OR-ed into it (clear it first; specsteer_cache_plan writes it).
  *   - scale >= 0 and finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
  *     caches and out.  Strides in elements, innermost axis dense.

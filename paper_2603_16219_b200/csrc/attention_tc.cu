@@ -72,7 +72,8 @@ struct Piece {
   int row0, n, kv;             // of the request
   int tok0, tok1;              // the unit's tokens
   int two;                     // two query tiles
-  int hi_first, lo_last;       // where the keys of the first row end, where those of the last row begin
+  int lo_first;                // where the keys of the first row begin
+  int hi_first, lo_last;       // where they end, where those of the last row begin
   int first, take;             // take = 0: no more pieces
   int starts, ends;            // the piece holds the unit's first / last key tile
   int index;                   // of the pieces of this CTA
@@ -406,7 +407,7 @@ struct Walk {
     q->b = b; q->hk = hk; q->u = u;
     q->row0 = rq.row0; q->n = rq.n; q->kv = rq.kv;
     q->tok0 = x.tok0; q->tok1 = x.tok1; q->two = x.two;
-    q->hi_first = x.hi_first; q->lo_last = x.lo_last;
+    q->lo_first = x.lo_first; q->hi_first = x.hi_first; q->lo_last = x.lo_last;
     q->first = x.t0 + off; q->take = take;
     q->starts = off == 0; q->ends = off + take == x.nt;
     q->index = index;
@@ -545,7 +546,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tc_wait<true>(&sh->piece_full[pc % kPieces], turn, limit);
         if (limit == 0) break;
       }
-      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, two = x->two;
+      const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, two = x->two, lo_first = x->lo_first;
       if (take <= 0) break;
       const int n_q = !keys ? 0 : two ? 2 : 1;
       const int* table = p.d.block_table + (long long)b * p.d.ld_table;
@@ -583,7 +584,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int blk = first + 2 * t + half;
         const bool outside = page < 0 || page >= p.d.n_pages;
         if (keys) {
-          const uint32_t votes = __ballot_sync(kFullMask, loads && outside && blk * kBlock + box * p.page_rows < kv);
+          // (pages that end before the first row's window may be gone: zeros were loaded for them, and no row sees those)
+          const int key = blk * kBlock + box * p.page_rows;
+          const uint32_t votes = __ballot_sync(kFullMask, loads && outside && key < kv && key + p.page_rows > lo_first);
           any_bad = any_bad || votes;   // (until then the words are zero)
           if (any_bad && (lane & 15) == 0) {
             uint32_t bad = 0;

@@ -69,6 +69,16 @@ def test_plan_matches_reference(binding, B, page, W, spare, in_place):
     _check_plan(_run_plan(binding, seq, adv, new, held, table, ring, pos, page, cap, in_place), ref)
 
 
+@pytest.mark.parametrize("B,page,W,max_new", [(1, 24, 300, 6000), (5, 16, 400, 3000), (24, 64, 80, 2500), (200, 7, 60, 130), (513, 32, 12, 70), (2000, 16, 9, 40)])
+def test_plan_of_long_chunks(binding, B, page, W, max_new):
+    """Prompts among the chunks: slot maps of thousands of rows, over one and several CTAs and pages of any size."""
+    rng = np.random.default_rng(B + page)
+    seq, adv, new, held, table, ring, pos, P = _random_state(rng, B, page, W, B * (max_new // page + 2), max_new)
+    for cap in (sum(max(n, 0) for n in new) + 700, sum(max(n, 0) for n in new) // 2):
+        ref = plan_reference(seq, adv, new, held, table, ring, pos, page, cap, P)
+        _check_plan(_run_plan(binding, seq, adv, new, held, table, ring, pos, page, cap), ref)
+
+
 def test_plan_refusals_are_per_request(binding):
     """Too many tokens, too few pages, lengths that make no sense: each refused request says so, the others go on."""
     rng = np.random.default_rng(5)
@@ -377,6 +387,53 @@ def test_attention_tiny_scale(binding, generic):
         out, lse = torch.full_like(q, 7.0), torch.full((T, 4), 7.0, device="cuda")
         binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), scale=scale, out=out, lse=lse, generic=generic)
         _compare(out, lse, attention_reference(q, kc, vc, table, cu, kv, float(np.float32(scale))))
+
+
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+@pytest.mark.parametrize("page", [8, 16, 64, 128])
+def test_attention_pages_behind_the_window_may_be_gone(binding, page, generic):
+    """With a window, pages that no row sees any more can have been given back: their entries are not looked at."""
+    lens, window = [(5, 700), (1, 90), (150, 600), (3, 333)], 70
+    kc, vc, table, cu, kv, T, g = build_cache(lens, page, 2, 64, BF16, "cuda", 60)
+    for b, (n, total) in enumerate(lens):
+        table[b, :max(0, total - n + 1 - window) // page] = -1
+    assert (table[0] == -1).any() and (table[2] == -1).any()
+    q = torch.randn(T, 8, 64, generator=g).to(BF16).cuda()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    out, lse, status = torch.full_like(q, 7.0), torch.full((T, 8), 7.0, device="cuda"), i32([0] * 4)
+    binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), window=window, out=out, lse=lse, status=status, generic=generic)
+    _compare(out, lse, attention_reference(q, kc, vc, table, cu, kv, 1 / 8, window))
+    assert status.tolist() == [0] * 4
+
+
+@pytest.mark.parametrize("seed", range(32))
+def test_attention_random_shapes(binding, seed):
+    """Shapes, lengths, windows, layouts and bad pages drawn at random over what the tensor-core kernel takes."""
+    rng = np.random.default_rng(1000 + seed)
+    pick = lambda *v: v[int(rng.integers(len(v)))]  # noqa: E731
+    Hkv, G, D, page = pick(1, 2, 3), pick(1, 2, 3, 4, 5, 8, 12, 16), 8 * int(rng.integers(1, 17)), pick(8, 16, 32, 64, 128, 192)
+    dtype, window, layout = pick(BF16, F16), pick(0, 0, int(rng.integers(1, 300))), pick("nhd", "hnd", "joined")
+    lens = []
+    for _ in range(int(rng.integers(1, 7))):
+        n = pick(0, 1, int(rng.integers(1, 10)), int(rng.integers(1, 90)), int(rng.integers(1, 400 // G + 2)))
+        lens.append((n, max(0, n + pick(-2, 0, int(rng.integers(0, 130)), int(rng.integers(0, 700))))))
+    kc, vc, table, cu, kv, T, g = build_cache(lens, page, Hkv, D, dtype, "cuda", seed, layout, width_extra=seed % 2)
+    want = []
+    for b, (n, total) in enumerate(lens):
+        first = max(0, total - n + 1 - window) if window else 0
+        used = list(range(first // page, -(-total // page))) if n and total > 0 else []
+        if used and rng.random() < 0.3:
+            table[b, used[int(rng.integers(len(used)))]] = pick(-1, kc.shape[0], 2 ** 31 - 1, -2 ** 31)
+            want.append(BAD_PAGE)
+        else:
+            want.append(0)
+    q = torch.randn(T + 2, Hkv * G, D, generator=g).to(dtype).cuda()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    out, lse, status = torch.full_like(q, 7.0), torch.full((T + 2, Hkv * G), 7.0, device="cuda"), i32([0] * len(lens))
+    binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), window=window, out=out, lse=lse, status=status)
+    with np.errstate(invalid="ignore"):
+        _compare(out, lse, attention_reference(q, kc, vc, table, cu, kv, 1 / math.sqrt(D), window))
+    assert status.tolist() == want
 
 
 def test_attention_same_bits_again_and_beside_other_work(binding):
