@@ -505,7 +505,7 @@ def _launch(fn, name: str, desc, dev: int):
     """Call an entry point that works on the current device, on the tensors' device `dev` and its current stream."""
     if dev < 0:
         raise RuntimeError("specsteer needs tensors on a CUDA device; there is no CPU fallback")
-    if torch.cuda.current_device() == dev:
+    if torch._C._cuda_getDevice() == dev:   # (a tensor is there, so CUDA is initialised)
         code = fn(desc, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
