@@ -2,6 +2,7 @@
 #pragma once
 #include "common.cuh"
 #include "internal.h"
+#include "paged.h"
 #include "specsteer.h"
 
 namespace specsteer {

@@ -12,6 +12,7 @@
 
 #include "common.cuh"
 #include "internal.h"
+#include "paged.h"
 #include "specsteer.h"
 
 namespace specsteer {

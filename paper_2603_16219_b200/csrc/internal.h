@@ -99,9 +99,6 @@ int sums_wanted(const specsteer_round_desc* d);
 // Every row of the three logit tensors starts on a 16-byte boundary (the bulk-copy path).
 bool rows_aligned(const specsteer_round_desc* d);
 
-// SM count of the current device (read once per device); 0 on failure.
-int current_sm_count();
-
 struct LaunchInfo {
   int device;
   int sm_count;
