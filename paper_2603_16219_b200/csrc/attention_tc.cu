@@ -22,7 +22,10 @@
 // Maximum.  Weights are 2^(c s - c m + lift) with a reference m per row.  A block is weighed against the reference there
 // is; only if that makes its weights sum to more than 2^15 (or there is none yet) the block's maximum is formed, the
 // reference raised, O_s rescaled in tensor memory and the block weighed again.  Weights are then at most 2^15, which
-// float16 holds, and after the first tile hardly any block needs its maximum, a sixth of the work.
+// float16 holds, and after the first tile hardly any block needs its maximum, a sixth of the work.  The exponent is one fused
+// multiply-add of s with the rounded lift - c m, off by half a step of c m: a common factor of the row, which cancels, as
+// long as it leaves the weights in range.  From |c m| = 2^24 on (half a step: 1) it is c (s - m) + lift instead, with m the
+// maximum so far, formed for every block: rare, and a branch of the warp that the other rows do not pay for.
 //
 // Measured (bfloat16 and D = 128 unless said, the whole call):
 //   3 requests of 30 to 120 thousand keys, 9 tokens of 64 heads        158 to 165 us, 5.6 to 5.8 TB/s: bound by HBM
@@ -55,6 +58,7 @@ constexpr float kMostArg = 15.f;    // the exponent that no such weight exceeds
 // The largest weight is 2^kLift: with float16 the weights below 2^-22 of the largest are subnormal, not those below 2^-14,
 // and a whole block of largest ones still sums to less than kMostSum.
 template <bool BF> constexpr float kLift = BF ? 0.f : 8.f;
+constexpr float kFar = 16777216.f;  // |c m| beyond which c s - c m is not formed from the two products (see Maximum)
 constexpr int kPieces = 4;          // pieces of work the producer may be ahead
 
 template <int DP> struct TcLayout {
@@ -117,7 +121,7 @@ struct TcParams {
   float c;                             // scale * log2(e)
   int out_vec;                         // out rows are 32-byte aligned and a multiple of 32 bytes long
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
-  float2* part_ml;                     // [2*gridDim][256] reference (powers of two) and sum
+  float2* part_ml;                     // [2*gridDim][256] reference (raw score) and sum
   int* head;                           // [gridDim][8] see write_head
 };
 
@@ -302,6 +306,11 @@ template <bool BF> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 template <bool BF> __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t w) {
   const uint32_t e = BF ? 0x7f80u : 0x7c00u;
   return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
+}
+
+// log sum exp of a row from its reference (raw score) and the sum of its weights
+template <bool BF> __device__ __forceinline__ float log_sum(const TcParams& p, float m, float l) {
+  return l == 0.f ? kNegInf : fmaf(m, p.d.scale, (log2f(l) - kLift<BF>) * kLn2);
 }
 
 // One poll of a barrier's phase in the form without a time hint: the hardware parks the thread until the phase completes
@@ -770,7 +779,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       const int hi_first = x.hi_first, lo_last = x.lo_last;
       float m = live ? kNegInf : 0.f, l = 0.f;       // reference (raw score; none yet: -inf), sum
-      bool none = true;                 // some row of the warp has no reference yet
+      bool none = true;                 // some row of the warp has no reference yet, or one beyond kFar
       const int step = two ? 1 : 2, t_from = two ? 0 : s;
       uint32_t v_par = two ? v_both : v_own;
       int v_first = (blocks0 + 2 * t_from) % L::kStages;   // stage of the tile's first block
@@ -874,9 +883,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 }
                 l *= alpha;
                 m = top;
-                none = __any_sync(kFullMask, m == kNegInf);
+                none = __any_sync(kFullMask, live && !(fabsf(m) * c <= kFar));
               }
-              const float up = m == kNegInf ? 0.f : fmaf(m, -c, kLift<BF>);
+              float up = m == kNegInf ? 0.f : fmaf(m, -c, kLift<BF>);
+              if (none) {   // (the block's last turn: it has just formed the maximum)
+                const float from = m == kNegInf ? 0.f : -m;
+#pragma unroll
+                for (int j = 0; j < 64; j += 2) {
+                  const float2 y = add2(make_float2(v[j], v[j + 1]), make_float2(from, from));
+                  v[j] = y.x;
+                  v[j + 1] = y.y;
+                }
+                up = kLift<BF>;
+              }
               const float2 c2 = make_float2(c, c), ref2 = make_float2(up, up);
               float poly_top = kNegInf;   // ex2_poly takes no more than 127
               float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -1004,8 +1023,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
         }
         if (live && (two || s == 0)) {
-          if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m * c - kLift<BF>, l);   // c > 0: -inf stays
-          else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m * c - kLift<BF> + log2f(l)) * kLn2;
+          if (!whole) p.part_ml[(long long)slot * 256 + part_row] = make_float2(m, l);
+          else if (p.d.lse) p.d.lse[row * p.d.Hq + head] = log_sum<BF>(p, m, l);
         }
       }
       if (tid == 0 && !whole) {
@@ -1064,7 +1083,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
       const long long at = (long long)(i == cta ? slot0 : 2 * i) * 256 + part_row;
       const float2 ml = has ? p.part_ml[at] : make_float2(kNegInf, 0.f);
       const float top = fmaxf(m, warp_max(ml.x));
-      const float keep = m == kNegInf ? 0.f : ex2(m - top), f = ml.x == kNegInf ? 0.f : ex2(ml.x - top);
+      const float keep = m == kNegInf ? 0.f : ex2((m - top) * p.c), f = ml.x == kNegInf ? 0.f : ex2((ml.x - top) * p.c);
       l = l * keep + warp_sum(ml.y * f);
 #pragma unroll
       for (int j = 0; j < DP / 32; ++j) o[j] *= keep;
@@ -1109,7 +1128,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
       if (d < p.d.D) dst[d] = (unsigned short)y;
       if (d + 1 < p.d.D) dst[d + 1] = (unsigned short)(y >> 16);
     }
-    if (lane == 0 && p.d.lse) p.d.lse[row * p.d.Hq + head] = l == 0.f ? kNegInf : (m + log2f(l)) * kLn2;
+    if (lane == 0 && p.d.lse) p.d.lse[row * p.d.Hq + head] = log_sum<BF>(p, m, l);
   }
 }
 

@@ -351,6 +351,45 @@ def test_attention_one_key_far_above_those_before_it(binding, above, generic):
 
 
 @pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+@pytest.mark.parametrize("dtype,size,scale", [(F16, 40.0, 1.0), (F16, 4000.0, 0.088), (F16, 8000.0, 1.0), (F16, 60000.0, 1.0), (F16, 60000.0, 1e9), (BF16, 1e5, 1.0), (BF16, 3e6, 0.125),
+                                              (BF16, 1e12, 1.0), (BF16, 1e19, 0.01), (BF16, 1.0, 1e38), (BF16, 1e-3, 1e38)])
+def test_attention_very_large_scores(binding, dtype, size, scale, generic):
+    """Scores of up to 1e38 and scales of up to 1e38: the largest key takes all the weight, keys of the same score share it.
+
+    Only one column of q and k is not zero, so that every score is one product of two numbers of 11 bits, exact in float32.
+    The keys below the largest are 0.1 size or more below it, so their scores are 0.05 size^2 scale (80 or more) below, their
+    weights less than 2^-115 of its, and the result is the mean of the values of the two largest, whose weights are alike.
+    What is left is the rounding of the result (u of it), of the weights to the inputs' type for the product with v (u of the
+    mean of |v|: the weight is 2^x with an x that carries half a step of the scaled maximum, so it need not be a power of
+    two), and 2^-20 for the division and the joining of parts."""
+    lens = [(1, 900), (5, 700), (1, 1), (150, 400), (3, 9001), (1, 130)]
+    kc, vc, table, cu, kv, T, g = build_cache(lens, 16, 2, 64, dtype, "cpu", 70)
+    used = torch.isfinite(kc)
+    kc[used] = 0
+    for b, (n, total) in enumerate(lens):
+        x = size * (2 * torch.rand(total, 2, generator=g) - 1) * 0.8
+        top = torch.randint(0, max(1, total - n), (2,), generator=g)
+        x[top] = size * (0.9 + 0.1 * torch.rand(1, 2, generator=g))              # both of the largest alike, seen by every row
+        for j in range(total):
+            kc[int(table[b, j // 16]), j % 16, :, 0] = x[j].to(dtype)
+    q = torch.zeros(T, 8, 64, dtype=dtype)
+    q[..., 0] = (size * (0.5 + 0.5 * torch.rand(T, 8, generator=g))).to(dtype)
+    q, kc, vc, table = (t.cuda() for t in (q, kc, vc, table))
+    out, lse = torch.full_like(q, 7.0), torch.full((T, 8), 7.0, device="cuda")
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), scale=scale, out=out, lse=lse, generic=generic)
+    want, want_lse, _, _, written = attention_reference(q, kc, vc, table, cu, kv, float(np.float32(scale)))
+    assert written.all() and np.isfinite(want).all()
+    u = torch.finfo(dtype).eps / 2
+    tol = np.abs(want) * u + np.abs(vc[torch.isfinite(vc)].double().cpu().numpy()).max() * (u * (1 + u) + 2.0 ** -20) + (2.0 ** -25 if dtype == F16 else 0.0)
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+    with np.errstate(over="ignore", invalid="ignore"):
+        want_lse = want_lse.astype(np.float32).astype(np.float64)                # (beyond float32: infinite)
+        got = lse.double().cpu().numpy()
+        assert ((got == want_lse) | (np.abs(got - want_lse) <= 8 * 2.0 ** -24 * np.abs(want_lse))).all()
+
+
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
 def test_attention_many_small_weights_of_float16(binding, generic):
     """In every 128 keys one that takes nearly all the weight, with value 0, and 127 of 2^-25.2 of its weight, which are all
     that the result consists of.
