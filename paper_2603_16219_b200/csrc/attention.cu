@@ -44,7 +44,9 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
   const T* q = (const T*)p.q;
   const T* kc = (const T*)p.k_cache;
   const T* vc = (const T*)p.v_cache;
-  const float c = p.scale * kLog2e;
+  // A weight is 2^(post (s pre - m)): with a large scale the difference comes first, so that a score times the scale may pass
+  // float32's range; with a small one the product, so that the difference of two scores may.  natural: of a maximum.
+  const float c = p.scale * kLog2e, pre = c < 1.f ? c : 1.f, post = c < 1.f ? 1.f : c, natural = c < 1.f ? kLn2 : p.scale;
 
   if (blockIdx.x == 0 && hk == 0 && p.req_status)
     for (int b = tid; b < p.B; b += kGenThreads)
@@ -150,7 +152,7 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
       for (int i = 0; i < 4; ++i) {
         const int j = k0 + sub + 8 * i;
         seen[i] = j >= lo && j < hi && page_s[sub + 8 * i] >= 0;
-        s[i] *= c;
+        s[i] *= pre;
         if (seen[i]) mt = s[i] > mt || s[i] != s[i] ? s[i] : mt;   // a NaN stays
       }
 #pragma unroll
@@ -160,11 +162,11 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
       }
       const float m_new = mt > m || mt != mt ? mt : m;
       const float ref = m_new == kNegInf ? 0.f : m_new;
-      const float alpha = m == kNegInf ? 0.f : exp2f(m - ref);
+      const float alpha = m == kNegInf ? 0.f : exp2f((m - ref) * post);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float w = exp2f(s[i] - ref);
+        const float w = exp2f((s[i] - ref) * post);
         if (seen[i]) sum += w;
         ps[row][sub + 8 * i] = seen[i] ? w : -1.f;   // -1: not seen, its v is not touched (a NaN there stays away)
       }
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       if (tid < D) from_f32(a0 * inv, o + tid);
       if (tid + kGenThreads < D) from_f32(a1 * inv, o + tid + kGenThreads);
-      if (tid == 0 && p.lse) p.lse[(rq.row0 + rr / G) * p.Hq + hk * G + rr % G] = top == kNegInf ? kNegInf : (top + log2f(sum)) * kLn2;
+      if (tid == 0 && p.lse) p.lse[(rq.row0 + rr / G) * p.Hq + hk * G + rr % G] = top == kNegInf ? kNegInf : fmaf(top, natural, log2f(sum) * kLn2);
     };
     if (n_split == 1) {
 #pragma unroll
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
           top = y > top || y != y ? y : top;
         }
         for (int i = 0; i < n_split; ++i) {
-          const float y = *cluster.map_shared_rank(&m_s[r], i), f = y == kNegInf ? 0.f : exp2f(y - top);
+          const float y = *cluster.map_shared_rank(&m_s[r], i), f = y == kNegInf ? 0.f : exp2f((y - top) * post);
           sum = fmaf(*cluster.map_shared_rank(&l_s[r], i), f, sum);
           if (tid < D) a0 = fmaf(*cluster.map_shared_rank(&qs[r][tid], i), f, a0);
           if (tid + kGenThreads < D) a1 = fmaf(*cluster.map_shared_rank(&qs[r][tid + kGenThreads], i), f, a1);

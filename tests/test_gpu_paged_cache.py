@@ -352,7 +352,7 @@ def test_attention_one_key_far_above_those_before_it(binding, above, generic):
 
 @pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
 @pytest.mark.parametrize("dtype,size,scale", [(F16, 40.0, 1.0), (F16, 4000.0, 0.088), (F16, 8000.0, 1.0), (F16, 60000.0, 1.0), (F16, 60000.0, 1e9), (BF16, 1e5, 1.0), (BF16, 3e6, 0.125),
-                                              (BF16, 1e12, 1.0), (BF16, 1e19, 0.01), (BF16, 1.0, 1e38), (BF16, 1e-3, 1e38)])
+                                              (BF16, 1e12, 1.0), (BF16, 1e19, 0.01), (BF16, 1e19, 30.0), (BF16, 1.0, 1e38), (BF16, 1e-3, 1e38)])
 def test_attention_very_large_scores(binding, dtype, size, scale, generic):
     """Scores of up to 1e38 and scales of up to 1e38: the largest key takes all the weight, keys of the same score share it.
 
