@@ -459,7 +459,7 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.  Pages that end before the first key
  *     that the request's first row sees (behind a window) may be gone: their ids do not matter.
  *   - req_status may be NULL; bits are OR-ed into it (clear it first; specsteer_cache_plan writes it).
- *   - scale >= 0 and finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
+ *   - scale >= 0, scale * log2(e) finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
  *     caches and out.  Strides in elements, innermost axis dense.
  *   - The tensor-core kernel takes D <= 128 in multiples of 8; page_size 8, 16, 32 or a multiple of 64; up to 128 query
  *     heads per kv head (G), of which G * 8 / gcd(G, 8) <= 128; scale >= 1e-30; pointers of q and the caches on 16-byte

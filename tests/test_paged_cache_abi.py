@@ -99,6 +99,13 @@ def test_attention_refuses_wide_heads_and_takes_nothing(binding):
     assert lib.specsteer_cache_append(_append(binding, T=0, k=None), None) == binding.OK
 
 
+def test_attention_refuses_a_scale_that_does_not_fit_powers_of_two(binding):
+    """The kernels weigh with powers of two: scale * log2(e) has to be a float32 too (scale up to 2.35e38)."""
+    lib = binding.load_library()
+    assert lib.specsteer_chunk_attention(_attention(binding, scale=2.4e38), None) == binding.ERR_INVALID_ARG
+    assert lib.specsteer_chunk_attention(_attention(binding, scale=2.3e38, T=0, q=None, out=None), None) == binding.OK
+
+
 def test_binding_checks_tensors(binding):
     import torch
     i32 = torch.int32
