@@ -276,6 +276,24 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const specsteer_cache
   }
 }
 
+constexpr int kPlanIpt = SPECSTEER_PLAN_MAX_B / kPlanThreads;   // of the kernel for more requests than a CTA has threads
+constexpr size_t plan_smem_bytes(int B) { return ((size_t)5 * B + 3) * sizeof(int); }
+
+// Shared memory for the largest plan, allowed once per device.  The limit belongs to the kernel and not to a call: a call that
+// set its own size would take it away under another thread that is about to launch a larger plan.
+bool allow_largest_plan() {
+  static std::atomic<bool> done[64];   // two threads that both find it clear set the same value
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) { cudaGetLastError(); return false; }
+  if (done[dev & 63].load(std::memory_order_acquire)) return true;
+  if (cudaFuncSetAttribute(cache_plan_kernel<kPlanIpt>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_smem_bytes(SPECSTEER_PLAN_MAX_B)) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  done[dev & 63].store(true, std::memory_order_release);
+  return true;
+}
+
 size_t elem_size(int dtype) { return dtype == SPECSTEER_F32 ? 4 : 2; }
 bool mult16(long long elems, size_t es) { return ((unsigned long long)elems * es) % 16 == 0; }
 
@@ -307,8 +325,8 @@ extern "C" specsteer_status specsteer_cache_plan(const specsteer_cache_plan_desc
     return SPECSTEER_ERR_INVALID_ARG;
   if (d->max_tokens > 0 && !d->slot_map) return SPECSTEER_ERR_INVALID_ARG;
   if (d->B > SPECSTEER_PLAN_MAX_B) return SPECSTEER_ERR_UNSUPPORTED;
-  const size_t smem = ((size_t)5 * d->B + 3) * sizeof(int);
-  auto kernel = d->B <= kPlanThreads ? cache_plan_kernel<1> : cache_plan_kernel<SPECSTEER_PLAN_MAX_B / kPlanThreads>;
+  const size_t smem = plan_smem_bytes(d->B);
+  auto kernel = d->B <= kPlanThreads ? cache_plan_kernel<1> : cache_plan_kernel<kPlanIpt>;
   // A plan is bound by its barriers and by the slot map's dependent steps (owner, table entry, slot), never by its bytes.
   // Up to 256 requests and 4096 rows one CTA serves: 32 threads for a handful of requests (one request and 5 rows 3.8 us,
   // with 256 threads 4.7), else 256.  Larger plans get a CTA for every 512 rows up to the cluster (512 requests and 3584
@@ -318,12 +336,7 @@ extern "C" specsteer_status specsteer_cache_plan(const specsteer_cache_plan_desc
   const int threads = !small ? (d->B <= 512 ? 512 : kPlanThreads) : d->B <= 32 && d->max_tokens <= 256 ? 32 : 256;
   const int wanted = d->max_tokens / 512 + (d->max_tokens % 512 != 0);
   const int ctas = small || wanted < 1 ? 1 : wanted < kPlanCluster ? wanted : kPlanCluster;
-  if (smem > 40 * 1024) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-      cudaGetLastError();
-      return SPECSTEER_ERR_CUDA;
-    }
-  }
+  if (smem > 40 * 1024 && !allow_largest_plan()) return SPECSTEER_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(threads);

@@ -141,6 +141,41 @@ def test_plan_without_advance_and_strided_table(binding):
     assert (wide[:, 10:] == -3).all()
 
 
+def test_plans_of_several_host_threads(binding):
+    """Plans of thousands of requests, of different sizes, called from several threads at once: none is refused, and each
+    gives what it gives alone."""
+    import ctypes as C
+    import threading
+    lib, jobs = binding.load_library(), []
+    for B in (8192, 2100, 5000):
+        rng = np.random.default_rng(B)
+        seq, adv, new, held, table, ring, pos, P = _random_state(rng, B, 16, 5, 20000)
+        cap = sum(max(n, 0) for n in new) + 3
+        i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+        t, r = torch.tensor(table, device="cuda"), torch.tensor(ring, device="cuda")
+        args = [i32(seq), i32(new), i32(held), t, r, torch.tensor(pos, device="cuda"), i32(adv)]
+        # (seq_len and the rest go to other arrays, so a call can be made again; what it moves then is not looked at)
+        got = binding.cache_plan(*args[:6], page_size=16, max_tokens=cap, advance=args[6])
+        _check_plan(dict(got, block_table=t, free_ring=r), plan_reference(seq, adv, new, held, table, ring, pos, 16, cap, P))
+        d = binding.CachePlanDesc(B, 16, P, 5, cap, 5, *(x.data_ptr() for x in (args[0], args[6], args[1], args[2], args[5], t, r)),
+                                  *(got[k].data_ptr() for k in ("seq_len", "pages_held", "ring_pos", "cu_new", "kv_len", "slot_map", "positions", "token_req", "status")))
+        jobs.append((d, torch.cuda.Stream(), args, got))
+    torch.cuda.synchronize()
+    codes = [set() for _ in jobs]
+
+    def work(i):
+        d, stream, _, _ = jobs[i]
+        for _ in range(3000):
+            codes[i].add(lib.specsteer_cache_plan(C.byref(d), stream.cuda_stream))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert codes == [{binding.OK}] * len(jobs)
+
+
 # ---- append ---------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("T,Hkv,D,page,dtype,layout", [
     (1, 1, 8, 1, BF16, "nhd"), (5, 8, 128, 16, BF16, "nhd"), (77, 2, 64, 32, F16, "hnd"), (33, 3, 80, 7, BF16, "hnd"), (40, 2, 33, 16, F16, "nhd"),
