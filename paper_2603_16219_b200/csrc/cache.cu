@@ -180,9 +180,10 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const specstee
 
   const i64 head0 = pool_ok ? head % P : 0, tail0 = pool_ok ? tail % P : 0;
   auto ring_at = [&](i64 base, int r) { return base + r < P ? base + r : base + r - P; };   // r < P
-  // pages given back: entry target + i of the request's table to place tail + r of the ring
-  for (int r = first_thread; r < given; r += n_threads) {
-    const int b = owner_of(cum_give, B, r);
+  // pages given back: entry target + i of the request's table to place tail + r of the ring (64-bit counters: a pool may have
+  // 2^31 - 1 pages, and a counter steps past the last)
+  for (i64 i = first_thread; i < given; i += n_threads) {
+    const int r = (int)i, b = owner_of(cum_give, B, r);
     p.free_ring[ring_at(tail0, r)] = p.block_table[(i64)b * p.ld_table + from_s[b] + (r - cum_give[b])];
   }
   if (rank == 0) {
@@ -191,8 +192,8 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const specstee
       if (tid * IPT + k < B) p.req_status[tid * IPT + k] = status[k];
   }
   sync_all();   // the ring is whole; nobody reads the inputs any more, which the outputs may be in place of
-  for (int r = first_thread; r < taken; r += n_threads) {
-    const int b = owner_of(cum_take, B, r);
+  for (i64 i = first_thread; i < taken; i += n_threads) {
+    const int r = (int)i, b = owner_of(cum_take, B, r);
     p.block_table[(i64)b * p.ld_table + from_s[b] + (r - cum_take[b])] = __ldcg(p.free_ring + ring_at(head0, r));
   }
   if (rank == 0) {

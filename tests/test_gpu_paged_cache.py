@@ -141,6 +141,30 @@ def test_plan_without_advance_and_strided_table(binding):
     assert (wide[:, 10:] == -3).all()
 
 
+def test_plan_moves_every_page_of_the_largest_pool(binding):
+    """A pool of 2^31 - 1 pages, all of them taken in one call and given back in the next: the counters of pages pass 2^31."""
+    P, B, W = 2 ** 31 - 1, 8192, 2 ** 18
+    ring = torch.arange(P, dtype=torch.int32, device="cuda")
+    table = torch.full((B, W), -1, dtype=torch.int32, device="cuda")
+    i32 = lambda v: torch.full((B,), v, dtype=torch.int32, device="cuda")  # noqa: E731
+    seq = i32(W)
+    seq[-1] = W - 1
+    head = 12345
+    got = binding.cache_plan(seq, i32(0), i32(0), table, ring, torch.tensor([head, head + P], device="cuda"), page_size=1, max_tokens=4096)
+    assert (got["status"] == 0).all() and got["ring_pos"].tolist() == [head + P, head + P] and torch.equal(got["pages_held"], seq)
+    flat, step = table.view(-1), 1 << 28
+    for at in range(0, P, step):
+        n = min(step, P - at)
+        assert torch.equal(flat[at:at + n].long(), (torch.arange(at, at + n, device="cuda") + head) % P)
+    assert int(flat[P]) == -1
+    ring.fill_(-1)
+    got = binding.cache_plan(got["seq_len"], i32(-1), got["pages_held"], table, ring, got["ring_pos"], page_size=1, max_tokens=4096)
+    assert (got["status"] == 0).all() and got["ring_pos"].tolist() == [head + P, head + 2 * P] and (got["pages_held"] == 0).all()
+    for at in range(0, P, step):       # in request order behind the ring's end, which has come round to place `head`
+        n = min(step, P - at)
+        assert torch.equal(ring[at:at + n].long(), torch.arange(at, at + n, device="cuda"))
+
+
 def test_plans_of_several_host_threads(binding):
     """Plans of thousands of requests, of different sizes, called from several threads at once: none is refused, and each
     gives what it gives alone."""
