@@ -514,6 +514,12 @@ def _launch(fn, name: str, desc, dev: int):
         raise SpecSteerError(code, name)
 
 
+def _fits(largest: int, smallest: int = 0) -> None:
+    """The descriptors hold 32-bit sizes, and ctypes would cut a larger number down without a word."""
+    if largest > 0x7fffffff or smallest < -0x80000000:
+        raise ValueError("sizes must fit 32 bits: %d" % (largest if largest > 0x7fffffff else smallest))
+
+
 def _flat(t: torch.Tensor, dtype, n: int, dev: int) -> int:
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
         raise ValueError("bad tensor: dtype %s, %d elements, device %d (want contiguous %s, %d, %d)" %
@@ -574,11 +580,12 @@ def cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, pages_held: torch.T
             return cache_plan(seq_len, new_len, pages_held, block_table, free_ring, ring_pos, page_size=page_size, max_tokens=max_tokens, advance=advance, out=out)
     dev = block_table.get_device()
     table, B, width, ld = _table(block_table, dev)
-    T, n_pages = int(max_tokens), free_ring.numel()
+    T, n_pages, page_size = int(max_tokens), free_ring.numel(), int(page_size)
+    _fits(max(T, n_pages, page_size, B, width), min(T, page_size))
     if out is None:
         sizes = (B, B, 2, B + 1, B, T, T, T, B)
         out = {name: torch.empty(n, dtype=dt, device=block_table.device) for (name, dt), n in zip(_PLAN_OUT, sizes)}
-    d = CachePlanDesc(B, int(page_size), n_pages, width, T, ld,
+    d = CachePlanDesc(B, page_size, n_pages, width, T, ld,
                       _flat(seq_len, _I32, B, dev), None if advance is None else _flat(advance, _I32, B, dev), _flat(new_len, _I32, B, dev),
                       _flat(pages_held, _I32, B, dev), _flat(ring_pos, _I64, 2, dev), table, _flat(free_ring, _I32, n_pages, dev),
                       _flat(out["seq_len"], _I32, B, dev), _flat(out["pages_held"], _I32, B, dev), _flat(out["ring_pos"], _I64, 2, dev),
@@ -598,6 +605,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     shape, e, f, dev, code = _caches(k_cache, v_cache)
     n_pages, page_size, H, D = shape
     T = slot_map.numel()
+    _fits(max(T, n_pages, page_size, H, D))
     want, dtype = (T, H, D), k_cache.dtype
     a, b = _heads(k, want, dtype, dev), _heads(v, want, dtype, dev)
     d = CacheAppendDesc(T, H, D, page_size, n_pages, code, a[0], a[1], b[0], b[1], e[0], e[1], e[2], f[0], f[1], f[2],
@@ -629,12 +637,14 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     a = _heads(q, want, dtype, dev)
     T, Hq, _ = want
     table, B, width, ld = _table(block_table, dev)
+    window = int(window)
+    _fits(max(T, Hq, Hkv, D, n_pages, page_size, B, width, window), window)
     if out is None:
         out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
     o = _heads(out, want, dtype, dev)
     if lse is None:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-    d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, code, int(window),
+    d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, code, window,
                       1.0 / math.sqrt(D) if scale is None else float(scale), ATTENTION_GENERIC if generic else 0, ld,
                       a[0], a[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
                       q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev),

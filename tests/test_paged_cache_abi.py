@@ -135,3 +135,33 @@ def test_binding_checks_tensors(binding):
             binding.chunk_attention(*bad)
     with pytest.raises(RuntimeError):
         binding.chunk_attention(q, kc, kc, table, cu, kv)
+
+
+def test_binding_refuses_numbers_beyond_32_bits(binding):
+    """A descriptor holds 32-bit sizes: a window of 2^32 + 5 must not become one of 5."""
+    import torch
+    i32, bf = torch.int32, torch.bfloat16
+    seq, ring, pos, table = torch.zeros(2, dtype=i32), torch.zeros(8, dtype=i32), torch.zeros(2, dtype=torch.int64), torch.zeros(2, 4, dtype=i32)
+    args = [seq, seq.clone(), seq.clone(), table, ring, pos]
+    for bad in (dict(page_size=2 ** 32 + 16, max_tokens=4), dict(page_size=-2 ** 32 + 16, max_tokens=4), dict(page_size=16, max_tokens=2 ** 32 + 4),
+                dict(page_size=16, max_tokens=-2 ** 32 + 4)):
+        with pytest.raises(ValueError):
+            binding.cache_plan(*args, **bad)
+    wide = torch.zeros(1, dtype=i32).expand(2 ** 31)                 # (no memory behind it: refused before anything is read)
+    with pytest.raises(ValueError):
+        binding.cache_plan(seq, seq.clone(), seq.clone(), table, wide, pos, page_size=16, max_tokens=4)
+    q, kc, cu, kv = torch.zeros(3, 4, 64, dtype=bf), torch.zeros(8, 16, 2, 64, dtype=bf), torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32)
+    for window in (2 ** 31, 2 ** 32 + 5, -2 ** 32 + 5):
+        with pytest.raises(ValueError):
+            binding.chunk_attention(q, kc, kc, table, cu, kv, window=window)
+    many = torch.zeros(1, 1, 1, 8, dtype=bf).expand(2 ** 32 + 8, 1, 1, 8)
+    with pytest.raises(ValueError):
+        binding.chunk_attention(torch.zeros(3, 1, 8, dtype=bf), many, many, table, cu, kv)
+    k = torch.zeros(3, 1, 8, dtype=bf)
+    with pytest.raises(ValueError):
+        binding.cache_append(k, k, many, many, torch.zeros(3, dtype=torch.int64))
+    rows = torch.zeros(1, 1, 8, dtype=bf).expand(2 ** 32 + 3, 1, 8)
+    with pytest.raises(ValueError):
+        binding.chunk_attention(rows, kc[:, :, :1, :8], kc[:, :, :1, :8], table, cu, kv)
+    with pytest.raises(ValueError):
+        binding.cache_append(rows, rows, kc[:, :, :1, :8], kc[:, :, :1, :8], torch.zeros(1, dtype=torch.int64).expand(2 ** 32 + 3))
