@@ -514,6 +514,13 @@ def _launch(fn, name: str, desc, dev: int):
         raise SpecSteerError(code, name)
 
 
+def _on(stream, t: torch.Tensor):
+    """A context in which `stream` is the current one, for work on t's device."""
+    if stream.device_index != t.get_device():
+        raise ValueError("the stream is on device %s, the tensors on %d" % (stream.device_index, t.get_device()))
+    return torch.cuda.stream(stream)
+
+
 def _fits(largest: int, smallest: int = 0) -> None:
     """The descriptors hold 32-bit sizes, and ctypes would cut a larger number down without a word."""
     if largest > 0x7fffffff or smallest < -0x80000000:
@@ -576,7 +583,7 @@ def cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, pages_held: torch.T
     slot_map / positions / token_req [max_tokens] and status [B].  ``out``: tensors to write those into; its seq_len,
     pages_held and ring_pos may be the inputs themselves.  Formulas and refusals: specsteer_cache_plan."""
     if stream is not None:   # what is allocated on the way belongs to that stream too
-        with torch.cuda.stream(stream):
+        with _on(stream, block_table):
             return cache_plan(seq_len, new_len, pages_held, block_table, free_ring, ring_pos, page_size=page_size, max_tokens=max_tokens, advance=advance, out=out)
     dev = block_table.get_device()
     table, B, width, ld = _table(block_table, dev)
@@ -600,7 +607,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     strides with a contiguous last axis; a cache laid out by heads is passed as a transposed view).  slot_map [T] int64:
     page * page_size + offset; a slot outside the cache (-1) drops its token."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, k_cache):
             return cache_append(k, v, k_cache, v_cache, slot_map)
     shape, e, f, dev, code = _caches(k_cache, v_cache)
     n_pages, page_size, H, D = shape
@@ -626,7 +633,7 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     is allocated from torch's pool when none is given; a call captured into a graph, or overlapping others, keeps its
     own.  Formulas, limits and refusals: specsteer_chunk_attention."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, k_cache):
             return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
                                    workspace=workspace, generic=generic)
     shape, e, f, dev, code = _caches(k_cache, v_cache)

@@ -165,3 +165,19 @@ def test_binding_refuses_numbers_beyond_32_bits(binding):
         binding.chunk_attention(rows, kc[:, :, :1, :8], kc[:, :, :1, :8], table, cu, kv)
     with pytest.raises(ValueError):
         binding.cache_append(rows, rows, kc[:, :, :1, :8], kc[:, :, :1, :8], torch.zeros(1, dtype=torch.int64).expand(2 ** 32 + 3))
+
+
+def test_binding_refuses_a_stream_of_another_device(binding):
+    """The work goes to the tensors' device: a stream of another one could not order it."""
+    import types
+
+    import torch
+    i32, bf = torch.int32, torch.bfloat16
+    seq, ring, pos, table = torch.zeros(2, dtype=i32), torch.zeros(8, dtype=i32), torch.zeros(2, dtype=torch.int64), torch.zeros(2, 4, dtype=i32)
+    q, kc, k = torch.zeros(3, 4, 64, dtype=bf), torch.zeros(8, 16, 2, 64, dtype=bf), torch.zeros(3, 2, 64, dtype=bf)
+    other = types.SimpleNamespace(device_index=1)
+    for call in (lambda: binding.cache_plan(seq, seq, seq, table, ring, pos, page_size=16, max_tokens=4, stream=other),
+                 lambda: binding.cache_append(k, k, kc, kc, torch.zeros(3, dtype=torch.int64), stream=other),
+                 lambda: binding.chunk_attention(q, kc, kc, table, torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32), stream=other)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
