@@ -432,8 +432,8 @@ specsteer_status specsteer_cache_plan(const specsteer_cache_plan_desc *desc, voi
 /* k and v of T tokens into their slots: cache[slot / page_size][slot mod page_size][h][:] = k[t][h][:].  A slot outside
  * [0, n_pages*page_size) (-1: a padded row) names no place and its token is dropped.  Two tokens of one call that name
  * the same slot leave a mixture of the two there (a plan never makes such slots unless tables share a page).  Strides in
- * elements, the innermost axis dense; any strides and alignment are taken, 16-byte multiples are faster.  dtype: F32,
- * BF16 or F16, the same on both sides.  Errors: INVALID_ARG, CUDA. */
+ * elements, the innermost axis dense; any strides (the caches' not zero on axes longer than one) and alignment are taken,
+ * 16-byte multiples are faster.  dtype: F32, BF16 or F16, the same on both sides.  Errors: INVALID_ARG, CUDA. */
 typedef struct {
   int32_t T, Hkv, D, page_size, n_pages, dtype;
   int64_t k_tok, k_head, v_tok, v_head;           /* strides of k and v */
@@ -453,7 +453,7 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  * and -inf.  Keys that a row does not see do not reach it, whatever they hold (NaN included).  Products are formed in
  * float32 from the inputs' type, sums and maxima are float32, and the tensor-core kernel rounds the weights to the
  * inputs' type for the product with v.
- *   - out and lse overlap no input.
+ *   - out and lse overlap no input, and the rows of out no other (o_tok and o_head are not zero on axes longer than one).
  *   - Requests with cu_new outside [0, T] or decreasing, or kv_len outside [0, table_width*page_size] or above 2^31 - 4097:
  *     BAD_LEN, nothing written.  Rows of no request are left as they are.
  *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.  Pages that end before the first key

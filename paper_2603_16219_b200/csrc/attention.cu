@@ -257,6 +257,7 @@ specsteer_status check_attention(const specsteer_attention_desc* d) {
   const long long strides[] = {d->q_tok, d->q_head, d->o_tok, d->o_head, d->kc_page, d->kc_slot, d->kc_head, d->vc_page, d->vc_slot, d->vc_head};
   for (long long x : strides)
     if (x < 0) return SPECSTEER_ERR_INVALID_ARG;
+  if ((d->T > 1 && !d->o_tok) || (d->Hq > 1 && !d->o_head)) return SPECSTEER_ERR_INVALID_ARG;   // rows that overwrite one another
   if (d->B > 0 && d->T > 0 && (!d->q || !d->k_cache || !d->v_cache || !d->block_table || !d->cu_new || !d->kv_len || !d->out))
     return SPECSTEER_ERR_INVALID_ARG;
   return SPECSTEER_OK;

@@ -365,6 +365,9 @@ extern "C" specsteer_status specsteer_cache_append(const specsteer_cache_append_
   const long long strides[] = {d->k_tok, d->k_head, d->v_tok, d->v_head, d->kc_page, d->kc_slot, d->kc_head, d->vc_page, d->vc_slot, d->vc_head};
   for (long long x : strides)
     if (x < 0) return SPECSTEER_ERR_INVALID_ARG;
+  // slots that share memory would overwrite one another
+  if ((d->n_pages > 1 && (!d->kc_page || !d->vc_page)) || (d->page_size > 1 && (!d->kc_slot || !d->vc_slot)) || (d->Hkv > 1 && (!d->kc_head || !d->vc_head)))
+    return SPECSTEER_ERR_INVALID_ARG;
   if ((long long)d->Hkv * d->D > 0x7fffffff) return SPECSTEER_ERR_INVALID_ARG;
   const size_t es = elem_size(d->dtype);
   const int sm = current_sm_count();

@@ -181,3 +181,15 @@ def test_binding_refuses_a_stream_of_another_device(binding):
                  lambda: binding.chunk_attention(q, kc, kc, table, torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32), stream=other)):
         with pytest.raises(ValueError, match="stream"):
             call()
+
+
+def test_outputs_whose_rows_share_memory_are_refused(binding):
+    """A stride of zero on an axis longer than one would let rows of the result, or slots of the cache, overwrite one another."""
+    lib = binding.load_library()
+    for bad in (dict(o_tok=0), dict(o_head=0)):
+        assert lib.specsteer_chunk_attention(_attention(binding, **bad), None) == binding.ERR_INVALID_ARG
+    for bad in (dict(kc_page=0), dict(kc_slot=0), dict(kc_head=0), dict(vc_page=0), dict(vc_slot=0), dict(vc_head=0)):
+        assert lib.specsteer_cache_append(_append(binding, **bad), None) == binding.ERR_INVALID_ARG
+    # the axis of one carries no stride; inputs may be broadcast
+    assert lib.specsteer_chunk_attention(_attention(binding, T=0, o_tok=0, q_tok=0, kc_head=0), None) == binding.OK
+    assert lib.specsteer_cache_append(_append(binding, T=0, k_tok=0), None) == binding.OK
