@@ -856,6 +856,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             bool raise = none;
 #pragma unroll 1
             for (;;) {
+              float up = fmaf(m, -c, kLift<BF>);
               if (raise) {
                 float mx[8] = {m, m, m, m, m, m, m, m};
 #pragma unroll
@@ -884,17 +885,17 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 l *= alpha;
                 m = top;
                 none = __any_sync(kFullMask, live && !(fabsf(m) * c <= kFar));
-              }
-              float up = m == kNegInf ? 0.f : fmaf(m, -c, kLift<BF>);
-              if (none) {   // (the block's last turn: it has just formed the maximum)
-                const float from = m == kNegInf ? 0.f : -m;
+                up = fmaf(m, -c, kLift<BF>);
+                if (none) {
+                  const float from = m == kNegInf ? 0.f : -m;
 #pragma unroll
-                for (int j = 0; j < 64; j += 2) {
-                  const float2 y = add2(make_float2(v[j], v[j + 1]), make_float2(from, from));
-                  v[j] = y.x;
-                  v[j + 1] = y.y;
+                  for (int j = 0; j < 64; j += 2) {
+                    const float2 y = add2(make_float2(v[j], v[j + 1]), make_float2(from, from));
+                    v[j] = y.x;
+                    v[j + 1] = y.y;
+                  }
+                  up = kLift<BF>;
                 }
-                up = kLift<BF>;
               }
               const float2 c2 = make_float2(c, c), ref2 = make_float2(up, up);
               float poly_top = kNegInf;   // ex2_poly takes no more than 127
