@@ -378,6 +378,24 @@ def test_attention_bad_lengths_and_pages(binding, generic):
         assert status.tolist() == want
 
 
+@pytest.mark.parametrize("generic", [False, True], ids=["", "generic"])
+@pytest.mark.parametrize("cu_bad", [[0, 5, 9, 15, 19], [-1, 5, 9, 15, 18], [5, 9, 2, 2, 5], [0, 5, 5, 2 ** 31 - 1, 18], [3, 3, -2 ** 31, 15, 18]])
+def test_attention_offsets_that_make_no_sense(binding, cu_bad, generic):
+    """Requests with offsets past the rows, before them or going down write nothing, and the others are what they are alone.
+    (No row belongs to two of the accepted requests.)"""
+    lens = [(5, 100), (4, 90), (6, 300), (3, 60)]
+    kc, vc, table, cu, kv, T, g = build_cache(lens, 16, 2, 64, BF16, "cuda", 15)
+    assert T == 18
+    q = torch.randn(T, 4, 64, generator=g).to(BF16).cuda()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    out, lse, status = torch.full_like(q, 7.0), torch.full((T, 4), 7.0, device="cuda"), i32([0] * 4)
+    binding.chunk_attention(q, kc, vc, table, i32(cu_bad), i32(kv), out=out, lse=lse, status=status, generic=generic)
+    bad = [a < 0 or b < a or b > T for a, b in zip(cu_bad, cu_bad[1:])]
+    assert any(bad) and not all(bad)
+    assert status.tolist() == [BAD_LEN * x for x in bad]
+    _compare(out, lse, attention_reference(q, kc, vc, table, cu_bad, kv, 1 / 8))
+
+
 def test_attention_strided_q_and_out(binding):
     """q inside a fused projection's output, out a slice of a wider buffer, a stride that is no multiple of 16 bytes."""
     lens = [(5, 100), (130, 200)]
