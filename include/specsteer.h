@@ -474,7 +474,7 @@ typedef struct {
   int32_t Hq, Hkv, D, page_size, n_pages, table_width;
   int32_t dtype, window;
   float scale;
-  uint32_t flags;                                 /* 0, or SPECSTEER_ATTENTION_GENERIC */
+  uint32_t flags;                                 /* 0, or SPECSTEER_ATTENTION_* */
   int64_t ld_table;
   int64_t q_tok, q_head, o_tok, o_head;           /* strides of q and out */
   int64_t kc_page, kc_slot, kc_head;              /* strides of k_cache */
@@ -488,6 +488,9 @@ typedef struct {
   int64_t workspace_bytes;
 } specsteer_attention_desc;
 enum { SPECSTEER_ATTENTION_GENERIC = 1u };        /* run the generic kernel whatever the shape (comparison, tests) */
+/* A test hook, to be OR-ed into flags: every CTA of the tensor-core kernel stops loading keys once `blocks` (0 to 65534) blocks
+ * of 64 have been loaded, so that the waits for the next ones run out. */
+#define SPECSTEER_ATTENTION_STOP(blocks) ((uint32_t)((blocks) + 1) << 16)
 specsteer_status specsteer_chunk_attention(const specsteer_attention_desc *desc, void *cuda_stream);
 /* Bytes of workspace the call needs (0 for a descriptor that specsteer_chunk_attention refuses). */
 size_t specsteer_chunk_attention_workspace(const specsteer_attention_desc *desc);

@@ -623,7 +623,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
 def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
                     kv_len: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
                     lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
-                    generic: bool = False, stream=None):
+                    generic: bool = False, stop_after: Optional[int] = None, stream=None):
     """Causal attention of a packed chunk of new tokens, q [T, Hq, D], over the paged caches [n_pages, page_size, Hkv, D]
     that hold the chunk's own keys and values already.  Rows [cu_new[b], cu_new[b+1]) belong to request b, whose last row
     stands at position kv_len[b] - 1.  One token per request is plain decoding.
@@ -631,11 +631,12 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     scale: default 1/sqrt(D); window: 0, or the number of last keys a row sees; status [B] int32: bits are OR-ed into it.
     Returns (out [T, Hq, D], lse [T, Hq] float32); rows of no request are left as they are in out and lse.  A workspace (uint8)
     is allocated from torch's pool when none is given; a call captured into a graph, or overlapping others, keeps its
-    own.  Formulas, limits and refusals: specsteer_chunk_attention."""
+    own.  generic: the kernel for every shape, with the weights of the softmax in 32 bits; stop_after: a test hook,
+    SPECSTEER_ATTENTION_STOP.  Formulas, limits and refusals: specsteer_chunk_attention."""
     if stream is not None:
         with _on(stream, k_cache):
             return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
-                                   workspace=workspace, generic=generic)
+                                   workspace=workspace, generic=generic, stop_after=stop_after)
     shape, e, f, dev, code = _caches(k_cache, v_cache)
     n_pages, page_size, Hkv, D = shape
     want, dtype = q.shape, k_cache.dtype
@@ -644,6 +645,8 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     a = _heads(q, want, dtype, dev)
     T, Hq, _ = want
     table, B, width, ld = _table(block_table, dev)
+    if stop_after is not None and not 0 <= stop_after < 0xffff:
+        raise ValueError("stop_after must be None or 0 to 65534")
     window = int(window)
     _fits(max(T, Hq, Hkv, D, n_pages, page_size, B, width, window), window)
     if out is None:
@@ -652,7 +655,7 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if lse is None:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
     d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, code, window,
-                      1.0 / math.sqrt(D) if scale is None else float(scale), ATTENTION_GENERIC if generic else 0, ld,
+                      1.0 / math.sqrt(D) if scale is None else float(scale), (ATTENTION_GENERIC if generic else 0) | (0 if stop_after is None else stop_after + 1 << 16), ld,
                       a[0], a[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
                       q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev),
                       out.data_ptr(), _flat(lse, torch.float32, T * Hq, dev), None if status is None else _flat(status, _I32, B, dev), None, 0)

@@ -122,7 +122,9 @@ struct TcParams {
   int out_vec;                         // out rows are 32-byte aligned and a multiple of 32 bytes long
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
   float2* part_ml;                     // [2*gridDim][256] reference (raw score) and sum
-  int* head;                           // [gridDim][8] see write_head
+  int* head;                           // [gridDim][8] 0: slot of the part of a unit that goes on in the next CTA (-1: none), 2..4: that
+                                       // unit; 1: this CTA's part of a unit that began before it (0: none, 1: its end, 2: more)
+  int stop_at;                         // blocks of keys after which a CTA loads no more (see SPECSTEER_ATTENTION_STOP)
 };
 
 // ---- PTX wrappers -------------------------------------------------------------------------------------------------
@@ -324,22 +326,26 @@ __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait of a whole warp (or, WARP false, of a single thread) for a phase of a barrier.  2^21 polls are between
-// a twentieth of a second (if the hardware never parks the thread) and seconds; healthy waits are microseconds.
-constexpr int kPolls = 1 << 21;
-// A warp's waits share a limit: once one has run out, the later ones do not wait any more.  Products and weights then go on
-// over whatever there is, every access in its place, to the end of the piece, where the warp leaves.
-template <bool WARP> __device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, int& limit) {
-  int n = limit;
+// Bounded wait of a whole warp for a phase of a barrier.  The hardware parks a poll that does not succeed for 4 us (measured: 4096
+// of them 16.1 ms), so 2^18 are about a second; healthy waits are microseconds.  A warp's waits share a limit: once one
+// has run out (limit 0) the warp issues and commits nothing more and leaves, every access still in its place.  (The loop is as
+// short as it can be, and the count no parameter of the kernel: with a clock in it the 256-request batch took 3 to 12 %
+// longer, with the count among the parameters the long prompt 1 %.)
+constexpr int kPolls = 1 << 18;
+__device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, int& limit) {
 #pragma unroll 1
-  for (;;) {
-    const bool got = poll(bar, parity);
-    if (WARP ? __all_sync(kFullMask, got) : got) break;
+  for (int n = limit;;) {
+    if (__all_sync(kFullMask, poll(bar, parity))) break;
     if (--n <= 0) { limit = 0; break; }
   }
 }
-__device__ __forceinline__ void gave_up(const TcParams& p) {   // said of request 0 of the call
-  if (p.d.req_status) atomicOr(p.d.req_status, SPECSTEER_REQ_TIMEOUT);
+__device__ __forceinline__ void gave_up(const TcParams& p) {
+  if (p.d.req_status) atomicOr(p.d.req_status, SPECSTEER_REQ_TIMEOUT);   // said of request 0 of the call
+}
+// Before a role ends: copies or products that are on their way, whatever has failed.
+__device__ __forceinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+  for (int n = kPolls; n > 0 && !poll(bar, parity); --n) {}
 }
 
 // ---- units ----------------------------------------------------------------------------------------------------------
@@ -535,6 +541,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     bool any_bad = false;
     int stage = 0, qi = 0, pc = 0, blocks = 0;
     int limit = kPolls;
+    const int stop_at = keys ? p.stop_at : 0x7fffffff;
+    bool lost = false;
     Walk w;
     w.begin(sh);
 #pragma unroll 1
@@ -543,7 +551,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const uint32_t turn = (uint32_t)((pc / kPieces) & 1);
       if (keys) {
         w.load(p);
-        tc_wait<true>(&sh->piece_empty[pc % kPieces], turn ^ 1u, limit);
+        tc_wait(&sh->piece_empty[pc % kPieces], turn ^ 1u, limit);
         if (limit == 0) break;
         if (lane == 0) {
           if (w.take > 0) w.publish(x);
@@ -552,7 +560,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         __syncwarp();
       } else {
-        tc_wait<true>(&sh->piece_full[pc % kPieces], turn, limit);
+        tc_wait(&sh->piece_full[pc % kPieces], turn, limit);
         if (limit == 0) break;
       }
       const int take = x->take, kv = x->kv, hk = x->hk, b = x->b, first = x->first * 2, two = x->two, lo_first = x->lo_first;
@@ -577,7 +585,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           const int slot = qi & 1;
           const uint32_t q_turn = (uint32_t)((qi >> 1) & 1) ^ 1u;
           if (t < L::kStages / 2 && t < take && !__all_sync(kFullMask, mbar_test_nonblocking(&sh->q_empty[slot], q_turn))) break;
-          tc_wait<true>(&sh->q_empty[slot], q_turn, limit);
+          tc_wait(&sh->q_empty[slot], q_turn, limit);
           if (limit == 0) break;
           const int tok = x->tok0 + q_done * p.tile_tok, cnt = min(p.tile_tok, x->tok1 - tok);
           const int nb = (cnt + p.box_tok - 1) / p.box_tok, q_box = lane / chunks;
@@ -589,6 +597,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           ++qi;
           ++q_done;
         }
+        if (blocks >= stop_at && t < take) { limit = 0; lost = true; }
         if (limit == 0 || t == take) break;
         const int blk = first + 2 * t + half;
         const bool outside = page < 0 || page >= p.d.n_pages;
@@ -611,7 +620,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int stage1 = stage + 1 < L::kStages ? stage + 1 : 0, st = half ? stage1 : stage;
         const uint32_t bits = (1u << stage) | (1u << stage1);
         const bool was_two = (last_two >> st) & 1u;
-        tc_wait<true>(&empty[was_two][st], ((was_two ? free_two : free_one) >> st) & 1u, limit);
+        tc_wait(&empty[was_two][st], ((was_two ? free_two : free_one) >> st) & 1u, limit);
         if (limit == 0) break;
         free_two ^= bits & last_two;
         free_one ^= bits & ~last_two;
@@ -635,15 +644,16 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (keys) w.next(p);
       else if (lane == 0) mbar_arrive(&sh->piece_empty[pc % kPieces]);
     }
-    if (limit == 0 && lane == 0) {
-      gave_up(p);
-      limit = kPolls;
-      // copies already issued may still be landing: wait for them (bounded) before the CTA exits
+    if (limit == 0 && !lost && lane == 0) gave_up(p);
+    if (lane == 0) {
+      // The CTA does not exit under a copy: another warp may have given up without looking at those that are on their way.
+#pragma unroll 1
       for (int i = 0; i < min(blocks, L::kStages); ++i) {
         const bool t2 = (last_two >> i) & 1u, t1 = (last_own >> i) & 1u;
-        tc_wait<false>(&full[t2 ? 2 : t1 ? 1 : 0][i], (((t2 ? landed2 : t1 ? landed1 : landed0) >> i) & 1u) ^ 1u, limit);
+        tc_drain(&full[t2 ? 2 : t1 ? 1 : 0][i], (((t2 ? landed2 : t1 ? landed1 : landed0) >> i) & 1u) ^ 1u);
       }
-      for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_wait<false>(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1), limit);
+#pragma unroll 1
+      for (int i = qi > 2 ? qi - 2 : 0; i < qi; ++i) tc_drain(&sh->q_full[i & 1], (uint32_t)((i >> 1) & 1));
     }
   } else if (warp >= kMmaWarp) {
     // ================= tensor-core issuers, one a stream =================
@@ -655,7 +665,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     int qi = 0, pc = 0, blocks0 = 0;
     uint32_t p_phase = 0;
     int limit = kPolls;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { tc_wait<true>(bar, parity, limit); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { tc_wait(bar, parity, limit); };
     uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // parity of each stage's full barriers, a bit a stage
 #pragma unroll 1
     for (;; ++pc) {
@@ -693,6 +703,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             for (int k = 0; k < 4; ++k)
               mma_ts(t_o, t_s + h * 64 + k * 8, b + (uint32_t)(k * (2048 >> 4)), id_pv, h > 0 || k > 0 || t > t_from);
           }
+          if (limit == 0) break;
           if (next) {
             // Scores of block h of tile t + step.  The commit also says that the product with the block's values before it
             // is complete.
@@ -705,6 +716,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             for (int k = 0; k < DP / 16; ++k)
               mma_ss(t_s + h * 64, q_desc + (uint32_t)((k >> 2) * ((128 * 128) >> 4) + (k & 3) * 2), b + (uint32_t)((k >> 2) * ((kBlock * 128) >> 4) + (k & 3) * 2),
                      id_qk, k != 0);
+            if (limit == 0) break;
             mma_commit(&sh->s_full[s][h]);
             mma_commit(&ring->k_empty[two][stage2]);
           } else if (h == 0 && now) {
@@ -712,8 +724,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
           if (now) mma_commit(&ring->v_empty[two][stage]);
         }
+        if (limit == 0) break;
         if (now) p_phase ^= 1u;
       }
+      if (limit == 0) break;
       // (a stream that had no tile says nothing: it could come by twice before anybody looks)
       if (t_from < take) mma_commit(&sh->o_full[s]);
       mma_commit(&sh->q_empty[qs]);
@@ -722,15 +736,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       blocks0 += 2 * take;
       if (two) { k_both = k_par; v_both = v_par; }
       else { k_own = k_par; v_own = v_par; }
-      if (limit == 0) break;
     }
-    if (limit == 0) {   // let everything issued finish before tensor memory is given back
-      if (lane == 0) gave_up(p);
-      __syncwarp();
-      mma_commit(&sh->drain[s]);
-      limit = kPolls;
-      wait(&sh->drain[s], 0);
-    }
+    if (limit == 0 && lane == 0) gave_up(p);
+    // Products end before tensor memory is given back and the CTA exits: a softmax warp that gave up did not wait for them.
+    __syncwarp();
+    mma_commit(&sh->drain[s]);
+    tc_drain(&sh->drain[s], 0);
   } else {
     // ================= softmax: one row a thread =================
     const int s = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
@@ -745,7 +756,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t v_own = 0, v_both = 0;         // as the issuer's
     int limit = kPolls;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      tc_wait<true>(bar, parity, limit);
+      tc_wait(bar, parity, limit);
       fence_after();
     };
     // barriers among the softmax warps: of this stream, of both (bounded like every wait)
@@ -784,7 +795,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       uint32_t v_par = two ? v_both : v_own;
       int v_first = (blocks0 + 2 * t_from) % L::kStages;   // stage of the tile's first block
 #pragma unroll 1
-      for (int t = t_from; t < take; t += step) {
+      for (int t = t_from; t < take && limit; t += step) {
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           const int k0 = (first + t) * kKeys + h * kBlock;
@@ -934,6 +945,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (v_first >= L::kStages) v_first -= L::kStages;
         s_phase ^= 1u;
       }
+      if (limit == 0) break;
       if (t_from < take) half_phase ^= 1u;
       if (two) v_both = v_par;
       else v_own = v_par;
@@ -1256,6 +1268,7 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   p.part = (float*)d->workspace;
   p.part_ml = (float2*)((char*)d->workspace + part_bytes(DP));
   p.head = (int*)((char*)d->workspace + part_bytes(DP) + ml_bytes());
+  p.stop_at = d->flags >> 16 ? (int)(d->flags >> 16) - 1 : 0x7fffffff;
   CUtensorMap tm[3];
   {
     const long long dims[3] = {d->D, d->Hq, d->T}, st[3] = {0, d->q_head, d->q_tok};

@@ -522,6 +522,48 @@ def test_attention_pages_behind_the_window_may_be_gone(binding, page, generic):
     assert status.tolist() == [0] * 4
 
 
+# With the blocks of 64 keys that 148 CTAs load on average: a CTA that has as many or more stops before them.
+STOP_SHAPES = [
+    ("one_tile_parts", [(5, 60001), (0, 9), (3, 700)], 8, 1, 128, 64, BF16, (0, 2, 4)),                     # 938 / 148 = 6.3
+    ("two_tiles", [(2500, 2500), (700, 3900), (1, 5)], 8, 2, 128, 16, BF16, (0, 2, 5, 12)),                 # 64 tokens a unit: 2870 / 148 = 19
+    ("single_tokens", [(1, 1 + 97 * i) for i in range(60)], 8, 4, 64, 32, F16, (0, 2, 5, 12)),              # 10700 / 148 = 72
+    ("windows_of_whole_units", [(300, 2000)] * 3 + [(5, 900)] * 40, 16, 4, 64, 8, F16, (0, 2, 4)),          # 1040 / 148 = 7.0
+]
+
+
+@pytest.mark.parametrize("case", STOP_SHAPES, ids=[c[0] for c in STOP_SHAPES])
+def test_attention_waits_that_run_out_are_reported(binding, case):
+    """CTAs that stop loading keys after some blocks: the waits for the next ones run out (after a second), the kernel ends by
+    itself and says TIMEOUT on request 0, and the call after it is what it was before.  Rows of no request, and those of refused
+    requests, are left as they are."""
+    name, lens, Hq, Hkv, D, page, dtype, stops = case
+    kc, vc, table, cu, kv, T, g = build_cache(lens, page, Hkv, D, dtype, "cuda", 80)
+    q = torch.randn(T + 3, Hq, D, generator=g).to(dtype).cuda()
+    kv[2] = -1
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    args = (q, kc, vc, table, i32(cu), i32(kv))
+    mine = torch.ones(T + 3, dtype=torch.bool, device="cuda")
+    mine[T:] = False
+    mine[cu[2]:cu[3]] = False
+
+    def call(**k):
+        out, lse, status = torch.full_like(q, 7.0), torch.full((T + 3, Hq), 7.0, device="cuda"), i32([0] * len(lens))
+        binding.chunk_attention(*args, out=out, lse=lse, status=status, window=300 if name.startswith("window") else 0, **k)
+        torch.cuda.synchronize()
+        assert (out[~mine] == 7).all() and (lse[~mine] == 7).all()
+        assert int(status[2]) == BAD_LEN and int(status.sum()) - int(status[0]) == BAD_LEN
+        return out, lse, int(status[0])
+    want, want_lse, status = call()
+    assert status == 0
+    for blocks in stops:
+        out, lse, status = call(stop_after=blocks)
+        assert status == binding.REQ_TIMEOUT
+        out, lse, status = call()
+        assert status == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
+    out, lse, status = call(stop_after=65534)             # more than any CTA has
+    assert status == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
 @pytest.mark.parametrize("seed", range(32))
 def test_attention_random_shapes(binding, seed):
     """Shapes, lengths, windows, layouts and bad pages drawn at random over what the tensor-core kernel takes."""

@@ -193,3 +193,17 @@ def test_outputs_whose_rows_share_memory_are_refused(binding):
     # the axis of one carries no stride; inputs may be broadcast
     assert lib.specsteer_chunk_attention(_attention(binding, T=0, o_tok=0, q_tok=0, kc_head=0), None) == binding.OK
     assert lib.specsteer_cache_append(_append(binding, T=0, k_tok=0), None) == binding.OK
+
+
+def test_the_hook_that_stops_loading(binding):
+    """Bits 16 to 31 of flags, and what the binding makes of a number of blocks."""
+    import torch
+    lib = binding.load_library()
+    assert lib.specsteer_chunk_attention(_attention(binding, flags=5 << 16, T=0), None) == binding.OK
+    assert lib.specsteer_chunk_attention(_attention(binding, flags=5 << 16 | 4, T=0), None) == binding.ERR_INVALID_ARG
+    i32, bf = torch.int32, torch.bfloat16
+    args = (torch.zeros(3, 4, 64, dtype=bf), torch.zeros(8, 16, 2, 64, dtype=bf), torch.zeros(8, 16, 2, 64, dtype=bf), torch.zeros(2, 4, dtype=i32),
+            torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32))
+    for blocks in (-1, 65535, 1 << 40):
+        with pytest.raises(ValueError):
+            binding.chunk_attention(*args, stop_after=blocks)
