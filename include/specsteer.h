@@ -381,8 +381,7 @@ enum {
   SPECSTEER_REQ_NO_ROOM = 64,   /* plan: the chunk does not fit max_tokens; the request gets no tokens this time */
   SPECSTEER_REQ_NO_PAGES = 128, /* plan: the pool has too few free pages; no tokens this time, pages as they were */
   SPECSTEER_REQ_BAD_POOL = 256, /* plan: ring_pos does not describe a ring of n_pages entries; nothing is moved */
-  SPECSTEER_REQ_TIMEOUT = 512   /* attention (on request 0): a bounded device-side wait gave up; the call's outputs are
-                                   undefined */
+  SPECSTEER_REQ_TIMEOUT = 512   /* attention (on request 0): a bounded device-side wait gave up; every row of the call is NaN */
 };
 
 /* Block tables and slot maps from request lengths.  Per request b, in this order:
@@ -459,6 +458,9 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *   - Keys on a page whose id lies outside [0, n_pages) count as not seen: BAD_PAGE.  Pages that end before the first key
  *     that the request's first row sees (behind a window) may be gone: their ids do not matter.
  *   - req_status may be NULL; bits are OR-ed into it (clear it first; specsteer_cache_plan writes it).
+ *   - Waits inside the tensor-core kernel are bounded (about a second).  If one runs out, which nothing short of a fault of the
+ *     kernel or the device makes it do, the kernel ends by itself, request 0 gets TIMEOUT, and out and lse are NaN in every row
+ *     of the accepted requests, which a caller without req_status sees too.
  *   - scale >= 0, scale * log2(e) finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
  *     caches and out.  Strides in elements, innermost axis dense.
  *   - The tensor-core kernel takes D <= 128 in multiples of 8; page_size 8, 16, 32 or a multiple of 64; up to 128 query

@@ -124,6 +124,7 @@ struct TcParams {
   float2* part_ml;                     // [2*gridDim][256] reference (raw score) and sum
   int* head;                           // [gridDim][8] 0: slot of the part of a unit that goes on in the next CTA (-1: none), 2..4: that
                                        // unit; 1: this CTA's part of a unit that began before it (0: none, 1: its end, 2: more)
+  int* failed;                         // [gridDim] whether a bounded wait of the CTA has run out
   int stop_at;                         // blocks of keys after which a CTA loads no more (see SPECSTEER_ATTENTION_STOP)
 };
 
@@ -340,6 +341,9 @@ __device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, int& lim
   }
 }
 __device__ __forceinline__ void gave_up(const TcParams& p) {
+  uint32_t cta;
+  asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(cta));   // (read anew: blockIdx.x would be kept in a register throughout)
+  p.failed[cta] = 1;
   if (p.d.req_status) atomicOr(p.d.req_status, SPECSTEER_REQ_TIMEOUT);   // said of request 0 of the call
 }
 // Before a role ends: copies or products that are on their way, whatever has failed.
@@ -483,6 +487,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   if (warp == kMmaWarp) tc_alloc(&sh->tmem_slot);
   pdl_wait();                // so far nothing touched what the kernels before wrote or read
   pdl_launch_dependents();   // attention_join_kernel may come up; it waits for the end of this kernel before it reads
+  if (tid == 0) p.failed[blockIdx.x] = 0;
 
   // ---- this CTA's range of the list of key tiles
   {
@@ -1060,20 +1065,42 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   }
 }
 
+// A call in which a bounded wait ran out leaves no number behind that could be taken for a result: NaN in every row.
+template <bool BF> __device__ __forceinline__ void spoil(const TcParams& p) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  for (int b = 0; b < p.d.B; ++b) {
+    const AttnRequest rq = attn_request(p.d, b);
+    const long long n = (long long)rq.n * p.d.Hq;
+    for (long long i = warp; i < n; i += warps) {
+      const long long row = rq.row0 + i / p.d.Hq, head = i % p.d.Hq;
+      unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head;
+      for (int j = lane; j < p.d.D; j += 32) dst[j] = BF ? 0x7fc0u : 0x7e00u;
+      if (lane == 0 && p.d.lse) p.d.lse[row * p.d.Hq + head] = __int_as_float(0x7fc00000);
+    }
+  }
+}
+
 // Puts the parts of a cut unit together: blocks x take the unit that begins in CTA x and goes on in the CTAs behind it.
 // One warp a row; the parts are added in their order, so the bits do not depend on who came first.
 // It waits on latency (about ten dependent trips to L2): 4 to 8 us behind the main kernel, 15 to 17 us where every CTA's
 // range cuts a unit of 256 rows (35 MB of parts); with 8 blocks a unit instead of 16 long contexts took 3 us
 // more, with 32 the same.
 template <int DP, bool BF>
-__global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
+__global__ void __launch_bounds__(256, 4) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
   pdl_launch_dependents();   // the next call's main kernel may set itself up meanwhile
   pdl_wait();
   const int cta = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // what every row begins with, on its way before anything is known to be needed (the addresses are the workspace's own)
   const int4 h = *reinterpret_cast<const int4*>(p.head + cta * 8);
   const int u = p.head[cta * 8 + 4], first_kind = lane == 0 ? 2 : cta + lane < n_cta ? p.head[(cta + lane) * 8 + 1] : 1;
+  const int failed = threadIdx.x < n_cta ? p.failed[threadIdx.x] : 0;   // (at most kMaxCtas of them, fewer than the threads)
   const int slot0 = h.x;
+  const bool first_block = blockIdx.x == 0 && blockIdx.y == 0;
+  if (slot0 < 0 && !first_block) return;
+  if (__syncthreads_or(failed)) {
+    if (first_block) spoil<BF>(p);
+    return;
+  }
   if (slot0 < 0) return;
   const AttnRequest rq = attn_request(p.d, h.z);
   const Unit x = make_unit(p, rq, u);
@@ -1193,6 +1220,8 @@ constexpr int kMaxCtas = 148;
 size_t part_bytes(int DP) { return (size_t)2 * kMaxCtas * 256 * DP * sizeof(float); }
 size_t ml_bytes() { return (size_t)2 * kMaxCtas * 256 * sizeof(float2); }
 size_t head_bytes() { return (size_t)kMaxCtas * 8 * sizeof(int); }
+size_t failed_bytes() { return (size_t)kMaxCtas * sizeof(int); }
+static_assert(kMaxCtas <= 256, "a thread of attention_join_kernel for every CTA");
 
 template <int DP, bool BF>
 cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStream_t s) {
@@ -1242,7 +1271,7 @@ bool attention_tc_takes(const specsteer_attention_desc* d) {
          ok(d->vc_slot, d->page_size) && ok(d->vc_head, d->Hkv);
 }
 
-size_t attention_tc_workspace(const specsteer_attention_desc* d) { return part_bytes(d->D <= 64 ? 64 : 128) + ml_bytes() + head_bytes(); }
+size_t attention_tc_workspace(const specsteer_attention_desc* d) { return part_bytes(d->D <= 64 ? 64 : 128) + ml_bytes() + head_bytes() + failed_bytes(); }
 
 cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t s) {
   const int sm = current_sm_count();
@@ -1268,6 +1297,7 @@ cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t 
   p.part = (float*)d->workspace;
   p.part_ml = (float2*)((char*)d->workspace + part_bytes(DP));
   p.head = (int*)((char*)d->workspace + part_bytes(DP) + ml_bytes());
+  p.failed = p.head + kMaxCtas * 8;
   p.stop_at = d->flags >> 16 ? (int)(d->flags >> 16) - 1 : 0x7fffffff;
   CUtensorMap tm[3];
   {

@@ -564,6 +564,24 @@ def test_attention_waits_that_run_out_are_reported(binding, case):
     assert status == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
+@pytest.mark.parametrize("case", STOP_SHAPES, ids=[c[0] for c in STOP_SHAPES])
+def test_attention_that_gave_up_leaves_nan(binding, case):
+    """A caller who passes no status sees a wait that ran out too: every row of the accepted requests is NaN, no other row is."""
+    name, lens, Hq, Hkv, D, page, dtype, stops = case
+    kc, vc, table, cu, kv, T, g = build_cache(lens, page, Hkv, D, dtype, "cuda", 81)
+    q = torch.randn(T + 3, Hq, D, generator=g).to(dtype).cuda()
+    kv[2] = -1
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    mine = torch.ones(T + 3, dtype=torch.bool, device="cuda")
+    mine[T:] = False
+    mine[cu[2]:cu[3]] = False
+    wide = torch.full((T + 3, Hq, D + 16), 7.0, dtype=dtype, device="cuda")
+    out, lse = wide[..., 8:8 + D], torch.full((T + 3, Hq), 7.0, device="cuda")
+    binding.chunk_attention(q, kc, vc, table, i32(cu), i32(kv), out=out, lse=lse, stop_after=stops[-1])
+    assert out[mine].isnan().all() and lse[mine].isnan().all()
+    assert (out[~mine] == 7).all() and (lse[~mine] == 7).all() and (wide[..., :8] == 7).all() and (wide[..., 8 + D:] == 7).all()
+
+
 @pytest.mark.parametrize("seed", range(32))
 def test_attention_random_shapes(binding, seed):
     """Shapes, lengths, windows, layouts and bad pages drawn at random over what the tensor-core kernel takes."""
