@@ -463,7 +463,8 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *     of the accepted requests, which a caller without req_status sees too.
  *   - scale >= 0, scale * log2(e) finite; Hq a multiple of Hkv; 1 <= D <= SPECSTEER_ATTENTION_MAX_D; dtype BF16 or F16 for q, both
  *     caches and out.  Strides in elements, innermost axis dense.
- *   - The tensor-core kernel takes D <= 128 in multiples of 8; page_size 8, 16, 32 or a multiple of 64; up to 128 query
+ *   - B <= 2^31 - 4097, Hkv <= 65535 (UNSUPPORTED beyond).
+ *   - The tensor-core kernel takes T <= 2^31 - 4097; D <= 128 in multiples of 8; page_size 8, 16, 32 or a multiple of 64; up to 128 query
  *     heads per kv head (G), of which G * 8 / gcd(G, 8) <= 128; scale >= 1e-30; pointers of q and the caches on 16-byte
  *     boundaries and their strides (of axes longer than one) positive multiples of 16 bytes.  Everything else runs on a
  *     slower generic kernel.

@@ -253,7 +253,7 @@ specsteer_status check_attention(const specsteer_attention_desc* d) {
     return SPECSTEER_ERR_INVALID_ARG;
   if (d->dtype != SPECSTEER_BF16 && d->dtype != SPECSTEER_F16) return SPECSTEER_ERR_INVALID_ARG;
   if (!(d->scale >= 0.f) || !std::isfinite(d->scale * kLog2e) || (d->flags & 0xffffu & ~(uint32_t)SPECSTEER_ATTENTION_GENERIC)) return SPECSTEER_ERR_INVALID_ARG;
-  if (d->D > SPECSTEER_ATTENTION_MAX_D || d->Hkv > 65535) return SPECSTEER_ERR_UNSUPPORTED;
+  if (d->D > SPECSTEER_ATTENTION_MAX_D || d->Hkv > 65535 || d->B > kAttnMaxKv) return SPECSTEER_ERR_UNSUPPORTED;
   const long long strides[] = {d->q_tok, d->q_head, d->o_tok, d->o_head, d->kc_page, d->kc_slot, d->kc_head, d->vc_page, d->vc_slot, d->vc_head};
   for (long long x : strides)
     if (x < 0) return SPECSTEER_ERR_INVALID_ARG;

@@ -7,7 +7,8 @@
 
 namespace specsteer {
 
-// Longest sequence the index arithmetic takes: a tile past the end must not overflow 32 bits.
+// The most that the index arithmetic takes of keys, requests, and (the tensor-core kernel) rows: a step past the end must not
+// overflow 32 bits.
 constexpr int kAttnMaxKv = 0x7fffffff - 4096;
 
 struct AttnRequest {

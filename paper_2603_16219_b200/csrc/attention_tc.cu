@@ -1265,7 +1265,7 @@ bool attention_tc_takes(const specsteer_attention_desc* d) {
   // strides of axes longer than one: positive multiples of 16 bytes below the tensor map's limit
   auto ok = [](long long stride, long long extent) { return extent <= 1 || (stride > 0 && stride % 8 == 0 && stride < (1ll << 38)); };
   const int pr = d->page_size < kBlock ? d->page_size : kBlock;
-  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->D <= 128 && d->D % 8 == 0 && d->scale >= kLeastScale && pr % 8 == 0 && kBlock % pr == 0 && d->page_size % pr == 0 &&
+  return !(d->flags & SPECSTEER_ATTENTION_GENERIC) && d->T <= kAttnMaxKv && d->D <= 128 && d->D % 8 == 0 && d->scale >= kLeastScale && pr % 8 == 0 && kBlock % pr == 0 && d->page_size % pr == 0 &&
          query_box(d->Hq / d->Hkv, &tok, &boxes) && a16(d->q) && a16(d->k_cache) && a16(d->v_cache) && ok(d->q_tok, d->T) && ok(d->q_head, d->Hq) &&
          ok(d->kc_page, d->n_pages) && ok(d->kc_slot, d->page_size) && ok(d->kc_head, d->Hkv) && ok(d->vc_page, d->n_pages) &&
          ok(d->vc_slot, d->page_size) && ok(d->vc_head, d->Hkv);

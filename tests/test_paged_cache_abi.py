@@ -207,3 +207,15 @@ def test_the_hook_that_stops_loading(binding):
     for blocks in (-1, 65535, 1 << 40):
         with pytest.raises(ValueError):
             binding.chunk_attention(*args, stop_after=blocks)
+
+
+def test_attention_sizes_next_to_2_to_the_31(binding):
+    """Loops over requests and over tiles of rows step past the last one: what would leave 32 bits is refused, or is the
+    generic kernel's, which counts rows in 64 bits."""
+    lib, most = binding.load_library(), 2 ** 31 - 1 - 4096
+    for bad in (dict(B=most + 1), dict(B=2 ** 31 - 1)):
+        assert lib.specsteer_chunk_attention(_attention(binding, **bad), None) == binding.ERR_UNSUPPORTED
+        assert lib.specsteer_chunk_attention_workspace(_attention(binding, **bad)) == 0
+    assert lib.specsteer_chunk_attention_workspace(_attention(binding, B=most)) > 0
+    assert lib.specsteer_chunk_attention_workspace(_attention(binding, T=most)) > 0        # the tensor-core kernel's workspace
+    assert lib.specsteer_chunk_attention_workspace(_attention(binding, T=most + 1)) == 0   # the generic kernel needs none
