@@ -451,7 +451,8 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  * One token per request is plain decoding.  A row that sees no key (p < 0), or only keys whose scores are -inf, gets 0
  * and -inf.  Keys that a row does not see do not reach it, whatever they hold (NaN included).  Products are formed in
  * float32 from the inputs' type, sums and maxima are float32, and the tensor-core kernel rounds the weights to the
- * inputs' type for the product with v.
+ * inputs' type for the product with v (the generic kernel, which SPECSTEER_ATTENTION_GENERIC asks for, keeps 32 bits).  The
+ * sums of v are formed before they are divided: they stay finite while |v| times the keys seen is below 2^117.
  *   - out and lse overlap no input, and the rows of out no other (o_tok and o_head are not zero on axes longer than one).
  *   - Requests with cu_new outside [0, T] or decreasing, or kv_len outside [0, table_width*page_size] or above 2^31 - 4097:
  *     BAD_LEN, nothing written.  Rows of no request are left as they are.
@@ -469,7 +470,8 @@ specsteer_status specsteer_cache_append(const specsteer_cache_append_desc *desc,
  *     boundaries and their strides (of axes longer than one) positive multiples of 16 bytes.  Everything else runs on a
  *     slower generic kernel.
  *   - workspace: 32-byte aligned device memory of at least specsteer_chunk_attention_workspace(desc) bytes, whose content
- *     before and after the call means nothing; calls that may overlap (two streams, two graphs) need one each.
+ *     before and after the call means nothing; calls that may overlap (two streams, two graphs) need one each.  It is the
+ *     same for every shape the tensor-core kernel takes (20 MB for D <= 64, else 39 MB).
  * Same inputs give the same bits.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE (too small), CUDA. */
 #define SPECSTEER_ATTENTION_MAX_D 256
 typedef struct {

@@ -3,8 +3,8 @@
 // The generic kernel computes the definition in float32 on the CUDA cores, one block per 16 rows (a row is a token and
 // a query head of one kv head) with the running maximum and sum of a softmax over tiles of 32 keys.  When that gives few
 // blocks, a cluster of 8 shares each: its CTAs take the key tiles in turn and put their sums together through
-// distributed shared memory.  Measured on shapes the tensor-core kernel takes: five rows of one request 43 us (16 there), 64
-// single tokens 1.0 ms (0.08), four prompt chunks 23 ms (0.28).  It is bound by the shared-memory reads of its two inner
+// distributed shared memory.  Measured on shapes the tensor-core kernel takes: five rows of one request 39 us (15 there), 64
+// single tokens 0.99 ms (0.08), four prompt chunks 23 ms (0.31).  It is bound by the shared-memory reads of its two inner
 // loops (five for four products of a score, one for two of a result), which only a tile per warp would change; it is
 // there for the shapes that the tensor-core kernel leaves, not for speed.
 #include <cooperative_groups.h>
@@ -291,7 +291,7 @@ extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_
   const int sm = current_sm_count();
   if (sm <= 0) return SPECSTEER_ERR_CUDA;
   // A cluster of 8 a block while the blocks do not fill the SMs (four CTAs each) four times over: 5 rows over 720 keys of
-  // width 256 take 54 us (one CTA a block: 250 us), a batch of 64 single tokens of width 256 1.5 ms (2.4 ms).
+  // width 256 take 51 us (one CTA a block: 250 us), a batch of 64 single tokens of width 256 1.6 ms (2.4 ms).
   const int split = blocks * d->Hkv <= (long long)sm * 16 ? kGenSplit : 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)) * split, d->Hkv);

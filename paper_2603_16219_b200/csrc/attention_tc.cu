@@ -27,14 +27,15 @@
 // long as it leaves the weights in range.  From |c m| = 2^24 on (half a step: 1) it is c (s - m) + lift instead, with m the
 // maximum so far, formed for every block: rare, and a branch of the warp that the other rows do not pay for.
 //
-// Measured (bfloat16 and D = 128 unless said, the whole call):
-//   3 requests of 30 to 120 thousand keys, 9 tokens of 64 heads        158 to 165 us, 5.6 to 5.8 TB/s: bound by HBM
-//   256 requests of up to 4000 keys, 5 tokens of 64 heads              373 to 395 us, 5.6 to 5.9 TB/s: bound by HBM
-//   a prompt of 8192 tokens of 32 heads                                0.55 to 0.61 ms, 0.90 to 1.0 PFLOP/s: bound by the issue of
-//     the softmax warps and by the clock that the power limit leaves (tensor pipe busy for 45 % of the cycles)
-//   64 single tokens, up to 4000 keys, 32 heads of 64, float16         77 us, 3.4 TB/s: the few rows of a request sit in one warp
-//     of each stream, whose 2000 clocks a block of 64 keys (1500 of arithmetic and tensor-memory latency, 500 of
-//     handshakes) bound it
+// Measured (bfloat16 and D = 128 unless said; a call among others on inputs that change, on several machines; in brackets a
+// pass among others of a captured graph, whose inputs stay the same):
+//   3 requests of 30 to 120 thousand keys, 9 tokens of 64 heads        166 to 185 us, 5.0 to 5.6 TB/s (163 to 170): bound by HBM
+//   256 requests of up to 4000 keys, 5 tokens of 64 heads              415 to 458 us, 4.8 to 5.3 TB/s (405 to 417): bound by HBM
+//   a prompt of 8192 tokens of 32 heads                                0.61 to 0.63 ms, 0.88 to 0.90 PFLOP/s (0.59 to 0.60): bound by
+//     the issue of the softmax warps and by the clock that the power limit leaves (tensor pipe busy for 45 % of the cycles)
+//   64 single tokens, up to 4000 keys, 32 heads of 64, float16         81 to 87 us, 3.0 to 3.2 TB/s (78): the few rows of a request
+//     sit in one warp of each stream, whose 2000 clocks a block of 64 keys (1500 of arithmetic and tensor-memory latency,
+//     500 of handshakes) bound it
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -916,7 +917,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               const float2 c2 = make_float2(c, c), ref2 = make_float2(up, up);
               float poly_top = kNegInf;   // ex2_poly takes no more than 127
               float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-              // The weights go to the second product in the inputs' type, rounded to nearest; the sums keep 32 bits.
+              // The weights go to the second product in the inputs' type, rounded to nearest; the sums keep 32 bits.  The operand
+              // of the product has 16 bits: weights of 32 would mean two products.  It is most of what the result is further off
+              // than with weights of 32 bits (relative error 0.0023 instead of 0.0017 for the 256 requests, bfloat16).
 #pragma unroll
               for (int i = 0; i < 64; i += 32) {
                 uint32_t w16[16];
@@ -1216,6 +1219,7 @@ bool query_box(int G, int* box_tok, int* boxes) {
   return true;
 }
 
+// One CTA per SM, up to the 148 of a B200; the workspace is laid out for that many whatever the shape.
 constexpr int kMaxCtas = 148;
 size_t part_bytes(int DP) { return (size_t)2 * kMaxCtas * 256 * DP * sizeof(float); }
 size_t ml_bytes() { return (size_t)2 * kMaxCtas * 256 * sizeof(float2); }
