@@ -500,6 +500,145 @@ specsteer_status specsteer_chunk_attention(const specsteer_attention_desc *desc,
 /* Bytes of workspace the call needs (0 for a descriptor that specsteer_chunk_attention refuses). */
 size_t specsteer_chunk_attention_workspace(const specsteer_attention_desc *desc);
 
+/* ---- A round over trees of drafts ----------------------------------------------------------------------------------
+ * A request may draft a tree of tokens instead of a chain.  Row 0 of its chunk is the last emitted token (the root) and
+ * every other row names its parent, a row before it; siblings are alternatives for the same place.  specsteer_cache_plan
+ * makes room for the chunk as for any other (row i of the request has the slot of position kv_len - n + i, whatever its
+ * depth), and these operators take the place of, or stand beside, those for chains:
+ *   specsteer_tree_plan       parents -> the ancestors of every row as bits, and its position
+ *   specsteer_rotate_append   norm by head and rotation by position, keys and values into their slots (chains too)
+ *   specsteer_tree_attention  the rows over the cache and over their ancestors
+ *   specsteer_token_logprobs  log probabilities of tokens, entropy, the likeliest tokens (of any rows of logits)
+ *   specsteer_tree_keep       the path that the tokens chosen behind the rows confirm, its keys and values moved together
+ * Written for serving: forward only.  The conventions are those of the paged cache's operators above. */
+
+/* further bits of req_status[b] */
+enum { SPECSTEER_REQ_BAD_PARENT = 1024 /* a row's parent is not a row before it (nor -1): taken for -1 */ };
+#define SPECSTEER_TREE_MAX_ROWS 1024  /* rows of one request's tree */
+
+/* Ancestors and positions from parents.  parent[cu_new[b] + i] is the number (in the request) of the parent of row i, below i, or -1
+ * for a row that hangs on the cached tokens alone.  With A(i) = the rows from i up to its root, i among them, depth(i) =
+ * |A(i)| - 1 and past = kv_len - n:
+ *   mask[row] bit j (word j/32, bit j mod 32) = j in A(i), and with window > 0 only if depth(i) - depth(j) < window
+ *   positions[row] = past + depth(i)
+ * Rows behind the last request's (cu_new[B] <= row < T) get no bits and -1.  A request with more rows than 32 * mask_words or
+ * SPECSTEER_TREE_MAX_ROWS gets BAD_LEN and the same; one whose offsets or lengths make no sense (cu_new outside [0, T] or decreasing,
+ * kv_len < n) BAD_LEN, and nothing of it is written.  positions may be NULL; req_status may be NULL, bits are OR-ed into it.
+ * 1 <= mask_words <= SPECSTEER_TREE_MAX_ROWS / 32; ld_mask >= mask_words, in words.  Errors: INVALID_ARG, CUDA. */
+typedef struct {
+  int32_t B, T, mask_words, window;
+  int64_t ld_mask;
+  const int32_t *parent;       /* [T] */
+  const int32_t *cu_new;       /* [B+1] */
+  const int32_t *kv_len;       /* [B] */
+  uint32_t *mask;              /* [T][ld_mask] */
+  int32_t *positions;          /* [T] or NULL */
+  int32_t *req_status;         /* [B] or NULL */
+} specsteer_tree_plan_desc;
+specsteer_status specsteer_tree_plan(const specsteer_tree_plan_desc *desc, void *cuda_stream);
+
+/* What stands between a layer's projections and its attention, in one pass over T rows of Hq query heads and Hkv key and
+ * value heads of width D.  For every head x of q and of k:
+ *   norm     with eps >= 0:  x <- x / sqrt(mean(x^2) + eps) * weight     (weight NULL: 1; eps < 0: no norm)
+ *   turn     for i < rot/2, with p = positions[axis_of[i]][t] and the angle a = p * inv_freq[i]:
+ *            (x_i, x_j) <- factor * (x_i cos a - x_j sin a, x_j cos a + x_i sin a), where (i, j) = (i, i + rot/2), or
+ *            (2i, 2i+1) with neighbours != 0.  Elements from rot on are not turned (nor multiplied by factor).
+ * q goes to q_out (which may be q itself), k and v to their slots as in specsteer_cache_append: rows whose slot lies outside
+ * [0, n_pages*page_size) leave no key and no value, their queries are written all the same.  Computed in float32, angles in
+ * float64 (positions up to 2^31), each result rounded once.  Several axes of positions (time, height, width of images
+ * and video): positions is [n_axes][T] and axis_of [rot/2] says which axis turns pair i; NULL: axis 0.  A value of axis_of
+ * outside [0, n_axes) leaves its pair unturned (angle 0).
+ * T, Hq, Hkv >= 0 (any may be 0: nothing to do for those), 1 <= D <= SPECSTEER_ROTATE_MAX_D, 0 <= rot <= D, even.  Strides in
+ * elements, the innermost axis dense; any strides (q_out's and the caches' not zero on axes longer than one) and alignment
+ * are taken, 16-byte multiples with rot a multiple of 16 (with neighbours: of 8) are faster.  dtype (of q, k, v, q_out and the caches) and weight_dtype:
+ * F32, BF16 or F16.  Errors: INVALID_ARG, UNSUPPORTED (D), CUDA. */
+#define SPECSTEER_ROTATE_MAX_D 256
+typedef struct {
+  int32_t T, Hq, Hkv, D, rot, n_axes, neighbours, page_size, n_pages, dtype, weight_dtype;
+  float eps, factor;
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;   /* strides of q, k, v and q_out */
+  int64_t kc_page, kc_slot, kc_head;              /* strides of k_cache */
+  int64_t vc_page, vc_slot, vc_head;              /* strides of v_cache */
+  const void *q, *k, *v;                          /* [T][Hq][D], [T][Hkv][D] twice */
+  void *q_out;                                    /* [T][Hq][D] */
+  const void *q_weight, *k_weight;                /* [D] or NULL */
+  const int32_t *positions;                       /* [n_axes][T] */
+  const float *inv_freq;                          /* [rot/2] */
+  const int32_t *axis_of;                         /* [rot/2] or NULL */
+  const int64_t *slot_map;                        /* [T] */
+  void *k_cache, *v_cache;                        /* [n_pages][page_size][Hkv][D] */
+} specsteer_rotate_append_desc;
+specsteer_status specsteer_rotate_append(const specsteer_rotate_append_desc *desc, void *cuda_stream);
+
+/* specsteer_chunk_attention for trees: row i of a request with n rows sees
+ *   of the past = kv_len - n cached tokens before the chunk those j < past, and with window > 0 only j > positions[row] - window
+ *   (positions taken into [past, past + i]; needed with a window only);
+ *   of the chunk's own keys exactly those whose bit is set in mask[row] (bits from n on count for nothing; a row may be
+ *   without its own).
+ * Everything else is as there: `a` is that call's descriptor, with its types, layouts, limits, refusals, workspace and status bits.  A
+ * request with kv_len < n, or with more rows than 32 * mask_words, is refused with BAD_LEN as well.  Masks of chains (bit j of row i for j <= i)
+ * give what specsteer_chunk_attention gives, up to the order of sums.  mask_words >= 1, ld_mask >= mask_words, in words.
+ * The workspace is that of specsteer_chunk_attention for `a`.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+typedef struct {
+  specsteer_attention_desc a;
+  int32_t mask_words;
+  int64_t ld_mask;
+  const uint32_t *mask;        /* [T][ld_mask] */
+  const int32_t *positions;    /* [T] or NULL (window = 0) */
+} specsteer_tree_attention_desc;
+specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc *desc, void *cuda_stream);
+
+/* For R rows of V logits, with l = x / temperature (NULL: 1) and Z = sum exp l:
+ *   lse = log Z,   logprob[r][i] = l[token[r][i]] - lse,   entropy = lse - sum p l   (nats; entries of -inf have no share),
+ *   top_id[r][0..n_top): the tokens of largest x, in that order, the lowest id among equals; top_logprob theirs.
+ * A token outside [0, V) has logprob -inf, and BAD_TOKEN is set unless it is -1 (no token).  A row that holds NaN or +inf, or nothing
+ * but -inf, or whose l passes float32, gets NaN everywhere, ids of -1, and NONFINITE; so does one whose temperature is not
+ * positive and finite, with BAD_PARAM.  lse and entropy may be NULL; so may row_status,
+ * into which bits are OR-ed.  Sums in float32, one read of the logits.  Equal inputs give equal bits.
+ * R, n_tokens >= 0; 1 <= V; 0 <= n_top <= min(V, SPECSTEER_TOP_MAX); ld_row >= V.  dtype F32, BF16 or F16.  Any alignment is taken,
+ * rows of 16-byte multiples are faster.  Errors: INVALID_ARG, CUDA. */
+#define SPECSTEER_TOP_MAX 32
+typedef struct {
+  int32_t R, V, n_tokens, n_top, dtype;
+  int64_t ld_row, ld_tok;      /* elements between rows of logits, and of token and logprob */
+  const void *logits;          /* [R][ld_row] */
+  const float *temperature;    /* [R] or NULL */
+  const int32_t *token;        /* [R][ld_tok] or NULL (n_tokens = 0) */
+  float *logprob;              /* [R][ld_tok] */
+  float *lse, *entropy;        /* [R] */
+  int32_t *top_id;             /* [R][n_top] */
+  float *top_logprob;          /* [R][n_top] */
+  int32_t *row_status;         /* [R] */
+} specsteer_token_logprobs_desc;
+specsteer_status specsteer_token_logprobs(const specsteer_token_logprobs_desc *desc, void *cuda_stream);
+
+/* The end of a round over trees.  token[row] is a row's token, choice[row] the one that the model emits behind it (its likeliest,
+ * or one sampled from its probabilities: then the emitted tokens follow the model's law).  Per request:
+ *   path[0] = 0;   path[i+1] = the lowest row whose parent is path[i] and whose token is choice[path[i]], while there is one
+ *   and i + 1 < max_out;   n_out = the length of the path (0 when the request has no rows)
+ *   out_tokens[i] = choice[path[i]]: what the round emits; the last of them is the next root
+ * and behind them path and out_tokens hold -1.  The keys and values of row path[i] go to the place of row i, in each of n_layers
+ * caches: the cache then holds past + n_out tokens of the request, and n_out is the next specsteer_cache_plan's advance.
+ * A token whose old or new page lies outside [0, n_pages) is not moved: BAD_PAGE.  Parents that are not before their row: the row is nobody's
+ * child.  Requests with cu_new outside [0, T] or decreasing, kv_len < n or beyond table_width*page_size, or more than
+ * SPECSTEER_TREE_MAX_ROWS rows: BAD_LEN, n_out 0, nothing moved.  Caches of layers that are separate tensors take a call each (with the
+ * same path); n_layers = 0 moves nothing and looks at no table.  dtype F32, BF16 or F16; strides in elements, the innermost axis
+ * dense, not zero on axes longer than one.  req_status may be NULL, bits are OR-ed into it; path and out_tokens may be NULL.
+ * B, T, n_layers >= 0, max_out >= 1.  Errors: INVALID_ARG, CUDA. */
+typedef struct {
+  int32_t B, T, max_out, n_layers, Hkv, D, page_size, n_pages, table_width, dtype;
+  int64_t ld_table;
+  int64_t kc_layer, kc_page, kc_slot, kc_head;    /* strides of k_cache */
+  int64_t vc_layer, vc_page, vc_slot, vc_head;    /* strides of v_cache */
+  const int32_t *parent, *token, *choice;         /* [T] */
+  const int32_t *cu_new, *kv_len, *block_table;   /* [B+1], [B], [B][ld_table] */
+  void *k_cache, *v_cache;                        /* [n_layers][n_pages][page_size][Hkv][D] */
+  int32_t *n_out;                                 /* [B] */
+  int32_t *path, *out_tokens;                     /* [B][max_out] */
+  int32_t *req_status;                            /* [B] or NULL */
+} specsteer_tree_keep_desc;
+specsteer_status specsteer_tree_keep(const specsteer_tree_keep_desc *desc, void *cuda_stream);
+
 /* Bytes of device workspace owned by the context. */
 size_t specsteer_ctx_workspace_bytes(const specsteer_ctx *ctx);
 

@@ -27,7 +27,9 @@ FLAG_ONE_LAUNCH = 8
 REQ_BAD_TOKEN, REQ_BAD_LEN, REQ_NONFINITE, REQ_RESIDUAL_EMPTY, REQ_BAD_PARAM = 1, 2, 4, 8, 16
 REQ_BAD_PAGE, REQ_NO_ROOM, REQ_NO_PAGES, REQ_BAD_POOL, REQ_TIMEOUT = 32, 64, 128, 256, 512
 ATTENTION_GENERIC = 1
+REQ_BAD_PARENT = 1024
 PLAN_MAX_B, ATTENTION_MAX_D = 8192, 256
+TREE_MAX_ROWS, ROTATE_MAX_D, TOP_MAX = 1024, 256, 32
 
 EXPORTS = (
     "specsteer_ctx_create", "specsteer_ctx_destroy", "specsteer_verify_round", "specsteer_recover_sample",
@@ -41,6 +43,7 @@ EXPORTS = (
     "specsteer_shard_greedy_local", "specsteer_lmhead_shard_greedy_local", "specsteer_shard_greedy_finish",
     "specsteer_probe_ex2", "specsteer_ctx_set_wait_limit",
     "specsteer_cache_plan", "specsteer_cache_append", "specsteer_chunk_attention", "specsteer_chunk_attention_workspace",
+    "specsteer_tree_plan", "specsteer_rotate_append", "specsteer_tree_attention", "specsteer_token_logprobs", "specsteer_tree_keep",
 )
 SHARD_PARTIAL_BYTES = 64
 MAX_SHARDS = 32
@@ -116,6 +119,54 @@ class AttentionDesc(C.Structure):
     ]
 
 
+class TreePlanDesc(C.Structure):
+    """Mirror of ``specsteer_tree_plan_desc``."""
+    _fields_ = [
+        ("B", C.c_int32), ("T", C.c_int32), ("mask_words", C.c_int32), ("window", C.c_int32), ("ld_mask", C.c_int64),
+        ("parent", C.c_void_p), ("cu_new", C.c_void_p), ("kv_len", C.c_void_p), ("mask", C.c_void_p), ("positions", C.c_void_p), ("req_status", C.c_void_p),
+    ]
+
+
+class RotateAppendDesc(C.Structure):
+    """Mirror of ``specsteer_rotate_append_desc``."""
+    _fields_ = [
+        ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("rot", C.c_int32), ("n_axes", C.c_int32), ("neighbours", C.c_int32),
+        ("page_size", C.c_int32), ("n_pages", C.c_int32), ("dtype", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float), ("factor", C.c_float),
+        ("q_tok", C.c_int64), ("q_head", C.c_int64), ("k_tok", C.c_int64), ("k_head", C.c_int64), ("v_tok", C.c_int64), ("v_head", C.c_int64),
+        ("o_tok", C.c_int64), ("o_head", C.c_int64),
+        ("kc_page", C.c_int64), ("kc_slot", C.c_int64), ("kc_head", C.c_int64),
+        ("vc_page", C.c_int64), ("vc_slot", C.c_int64), ("vc_head", C.c_int64),
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+        ("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("axis_of", C.c_void_p), ("slot_map", C.c_void_p), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
+    ]
+
+
+class TreeAttentionDesc(C.Structure):
+    """Mirror of ``specsteer_tree_attention_desc``."""
+    _fields_ = [("a", AttentionDesc), ("mask_words", C.c_int32), ("ld_mask", C.c_int64), ("mask", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class TokenLogprobsDesc(C.Structure):
+    """Mirror of ``specsteer_token_logprobs_desc``."""
+    _fields_ = [
+        ("R", C.c_int32), ("V", C.c_int32), ("n_tokens", C.c_int32), ("n_top", C.c_int32), ("dtype", C.c_int32), ("ld_row", C.c_int64), ("ld_tok", C.c_int64),
+        ("logits", C.c_void_p), ("temperature", C.c_void_p), ("token", C.c_void_p), ("logprob", C.c_void_p), ("lse", C.c_void_p), ("entropy", C.c_void_p),
+        ("top_id", C.c_void_p), ("top_logprob", C.c_void_p), ("row_status", C.c_void_p),
+    ]
+
+
+class TreeKeepDesc(C.Structure):
+    """Mirror of ``specsteer_tree_keep_desc``."""
+    _fields_ = [
+        ("B", C.c_int32), ("T", C.c_int32), ("max_out", C.c_int32), ("n_layers", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32),
+        ("n_pages", C.c_int32), ("table_width", C.c_int32), ("dtype", C.c_int32), ("ld_table", C.c_int64),
+        ("kc_layer", C.c_int64), ("kc_page", C.c_int64), ("kc_slot", C.c_int64), ("kc_head", C.c_int64),
+        ("vc_layer", C.c_int64), ("vc_page", C.c_int64), ("vc_slot", C.c_int64), ("vc_head", C.c_int64),
+        ("parent", C.c_void_p), ("token", C.c_void_p), ("choice", C.c_void_p), ("cu_new", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p),
+        ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("n_out", C.c_void_p), ("path", C.c_void_p), ("out_tokens", C.c_void_p), ("req_status", C.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -178,6 +229,11 @@ def load_library(path: Optional[str] = None):
     for name, desc in (("specsteer_cache_plan", CachePlanDesc), ("specsteer_cache_append", CacheAppendDesc),
                        ("specsteer_chunk_attention", AttentionDesc)):
         fn = getattr(lib, name)
+        fn.argtypes = [C.POINTER(desc), C.c_void_p]
+        fn.restype = C.c_int
+    for name, desc in (("tree_plan", TreePlanDesc), ("rotate_append", RotateAppendDesc), ("tree_attention", TreeAttentionDesc), ("token_logprobs", TokenLogprobsDesc),
+                       ("tree_keep", TreeKeepDesc)):
+        fn = getattr(lib, "specsteer_" + name)
         fn.argtypes = [C.POINTER(desc), C.c_void_p]
         fn.restype = C.c_int
     lib.specsteer_chunk_attention_workspace.argtypes = [C.POINTER(AttentionDesc)]
@@ -620,23 +676,8 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     _launch((_lib or load_library()).specsteer_cache_append, "specsteer_cache_append", d, dev)
 
 
-def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
-                    kv_len: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
-                    lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
-                    generic: bool = False, stop_after: Optional[int] = None, stream=None):
-    """Causal attention of a packed chunk of new tokens, q [T, Hq, D], over the paged caches [n_pages, page_size, Hkv, D]
-    that hold the chunk's own keys and values already.  Rows [cu_new[b], cu_new[b+1]) belong to request b, whose last row
-    stands at position kv_len[b] - 1.  One token per request is plain decoding.
-
-    scale: default 1/sqrt(D); window: 0, or the number of last keys a row sees; status [B] int32: bits are OR-ed into it.
-    Returns (out [T, Hq, D], lse [T, Hq] float32); rows of no request are left as they are in out and lse.  A workspace (uint8)
-    is allocated from torch's pool when none is given; a call captured into a graph, or overlapping others, keeps its
-    own.  generic: the kernel for every shape, with the weights of the softmax in 32 bits; stop_after: a test hook,
-    SPECSTEER_ATTENTION_STOP.  Formulas, limits and refusals: specsteer_chunk_attention."""
-    if stream is not None:
-        with _on(stream, k_cache):
-            return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
-                                   workspace=workspace, generic=generic, stop_after=stop_after)
+def _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after):
+    """(descriptor without a workspace, out, lse, device) of an attention call; the outputs are allocated where there are none."""
     shape, e, f, dev, code = _caches(k_cache, v_cache)
     n_pages, page_size, Hkv, D = shape
     want, dtype = q.shape, k_cache.dtype
@@ -659,7 +700,11 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                       a[0], a[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
                       q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev),
                       out.data_ptr(), _flat(lse, torch.float32, T * Hq, dev), None if status is None else _flat(status, _I32, B, dev), None, 0)
-    lib = _lib or load_library()
+    return d, out, lse, dev
+
+
+def _workspace(lib, d: AttentionDesc, workspace: Optional[torch.Tensor], q: torch.Tensor, dev: int):
+    """Put the caller's workspace into the descriptor, or one from torch's pool, which is returned."""
     if workspace is None:
         need = lib.specsteer_chunk_attention_workspace(d)
         if need and dev >= 0:
@@ -668,5 +713,217 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     else:
         d.workspace_bytes = workspace.numel()
         d.workspace = _flat(workspace, torch.uint8, d.workspace_bytes, dev)
+    return workspace
+
+
+def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
+                    kv_len: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    generic: bool = False, stop_after: Optional[int] = None, stream=None):
+    """Causal attention of a packed chunk of new tokens, q [T, Hq, D], over the paged caches [n_pages, page_size, Hkv, D]
+    that hold the chunk's own keys and values already.  Rows [cu_new[b], cu_new[b+1]) belong to request b, whose last row
+    stands at position kv_len[b] - 1.  One token per request is plain decoding.
+
+    scale: default 1/sqrt(D); window: 0, or the number of last keys a row sees; status [B] int32: bits are OR-ed into it.
+    Returns (out [T, Hq, D], lse [T, Hq] float32); rows of no request are left as they are in out and lse.  A workspace (uint8)
+    is allocated from torch's pool when none is given; a call captured into a graph, or overlapping others, keeps its
+    own.  generic: the kernel for every shape, with the weights of the softmax in 32 bits; stop_after: a test hook,
+    SPECSTEER_ATTENTION_STOP.  Formulas, limits and refusals: specsteer_chunk_attention."""
+    if stream is not None:
+        with _on(stream, k_cache):
+            return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
+                                   workspace=workspace, generic=generic, stop_after=stop_after)
+    d, out, lse, dev = _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
+    lib = _lib or load_library()
+    keep = _workspace(lib, d, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
     _launch(lib.specsteer_chunk_attention, "specsteer_chunk_attention", d, dev)
     return out, lse
+
+
+# ---- a round over trees of drafts --------------------------------------------------------------------------------------
+def tree_plan(parent: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, *, words: int, window: int = 0, out: Optional[Dict[str, torch.Tensor]] = None,
+              status: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Ancestors and positions of the rows of trees: parent [T] int32 names each row's parent by its number within the
+    request (-1: none), cu_new [B+1] and kv_len [B] are the plan's.  Returns mask [T, words] int32, whose bit j of row i
+    says that j is i or an ancestor of i (with window > 0: fewer than window steps above it), and positions [T] int32.  ``out``:
+    tensors to write those into; status [B] int32: bits are OR-ed into it.  Definition and refusals: specsteer_tree_plan."""
+    if stream is not None:
+        with _on(stream, parent):
+            return tree_plan(parent, cu_new, kv_len, words=words, window=window, out=out, status=status)
+    dev, T, B, words, window = parent.get_device(), parent.numel(), kv_len.numel(), int(words), int(window)
+    _fits(max(T, B, words, window), min(words, window))
+    if out is None:
+        if words < 1:
+            raise ValueError("words must be at least 1")
+        out = {"mask": torch.empty((T, words), dtype=_I32, device=parent.device), "positions": torch.empty(T, dtype=_I32, device=parent.device)}
+    mask, ld = _mask(out["mask"], T, dev)
+    if out["mask"].shape[1] != words:
+        raise ValueError("mask must be [T, words]")
+    d = TreePlanDesc(B, T, words, window, ld, _flat(parent, _I32, T, dev), _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev), mask,
+                     _flat(out["positions"], _I32, T, dev), None if status is None else _flat(status, _I32, B, dev))
+    _launch((_lib or load_library()).specsteer_tree_plan, "specsteer_tree_plan", d, dev)
+    return out
+
+
+def _mask(mask: torch.Tensor, T: int, dev: int):
+    """(pointer, words between rows) of a mask [T, words]."""
+    shape = mask.shape
+    if len(shape) != 2 or shape[0] != T or shape[1] < 1 or mask.dtype is not _I32 or mask.get_device() != dev:
+        raise ValueError("mask must be an int32 tensor [T, words] on the device of the others")
+    ld, one = mask.stride()
+    if (one != 1 and shape[1] > 1) or (T > 1 and ld < shape[1]):
+        raise ValueError("mask needs dense rows, one behind another")
+    return mask.data_ptr(), (ld if T > 1 else shape[1])
+
+
+def rotate_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                  slot_map: torch.Tensor, *, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None,
+                  axis_of: Optional[torch.Tensor] = None, neighbours: bool = False, factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """Norm the heads of q [T, Hq, D] and k [T, Hkv, D] (eps given: root mean square, times q_weight / k_weight [D]), turn them by
+    positions, and store k and v in their slots of the caches [n_pages, page_size, Hkv, D], all in one pass.
+
+    positions [T] or [n_axes, T] int32; inv_freq [rot/2] float32 turns the first rot elements of a head: pairs (i, i + rot/2),
+    or neighbours (2i, 2i+1); axis_of [rot/2] int32: the axis of positions that turns each pair.  slot_map [T] int64 as in
+    cache_append.  The slices of one projection's output serve as q, k and v.  Returns q_out (default: a new tensor; may be
+    q).  Definition and refusals: specsteer_rotate_append."""
+    if stream is not None:
+        with _on(stream, k_cache):
+            return rotate_append(q, k, v, positions, inv_freq, k_cache, v_cache, slot_map, q_weight=q_weight, k_weight=k_weight, eps=eps, axis_of=axis_of,
+                                 neighbours=neighbours, factor=factor, q_out=q_out)
+    shape, e, f, dev, code = _caches(k_cache, v_cache)
+    n_pages, page_size, H, D = shape
+    T, dtype, want = slot_map.numel(), k_cache.dtype, q.shape
+    if len(want) != 3 or want[0] != T or want[2] != D:
+        raise ValueError("q must be [T, Hq, D] with the caches' D and as many rows as slot_map")
+    Hq, half = want[1], inv_freq.numel()
+    _fits(max(T, n_pages, page_size, H, Hq, D, 2 * half))
+    a, b, c = _heads(q, want, dtype, dev), _heads(k, (T, H, D), dtype, dev), _heads(v, (T, H, D), dtype, dev)
+    if q_out is None:
+        q_out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
+    o = _heads(q_out, want, dtype, dev)
+    n_axes = 1 if positions.dim() == 1 else positions.shape[0]
+    if eps is None:
+        if q_weight is not None or k_weight is not None:
+            raise ValueError("weights belong to a norm: give eps")
+        eps = -1.0
+    elif not eps >= 0:
+        raise ValueError("eps must not be negative")
+    weight = q_weight if q_weight is not None else k_weight
+    w_dtype = torch.float32 if weight is None else weight.dtype
+    w_code = _CACHE_DTYPES.get(w_dtype)
+    if w_code is None:
+        raise ValueError("weights must be float32, bfloat16 or float16")
+    d = RotateAppendDesc(T, Hq, H, D, 2 * half, n_axes, 1 if neighbours else 0, page_size, n_pages, code, w_code, eps, factor,
+                         a[0], a[1], b[0], b[1], c[0], c[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
+                         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(),
+                         None if q_weight is None else _flat(q_weight, w_dtype, D, dev), None if k_weight is None else _flat(k_weight, w_dtype, D, dev),
+                         _flat(positions, _I32, n_axes * T, dev), _flat(inv_freq, torch.float32, half, dev), None if axis_of is None else _flat(axis_of, _I32, half, dev),
+                         _flat(slot_map, _I64, T, dev), k_cache.data_ptr(), v_cache.data_ptr())
+    _launch((_lib or load_library()).specsteer_rotate_append, "specsteer_rotate_append", d, dev)
+    return q_out
+
+
+def tree_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor,
+                   mask: torch.Tensor, *, positions: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0,
+                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, generic: bool = False, stop_after: Optional[int] = None, stream=None):
+    """chunk_attention for trees of drafts: a row sees the cached tokens before its request's chunk (with a window: those after
+    positions[row] - window) and, of the chunk's own, those whose bit is set in mask [T, words] int32 (tree_plan's, or any other).
+    Everything else is as there.  Definition and refusals: specsteer_tree_attention."""
+    if stream is not None:
+        with _on(stream, k_cache):
+            return tree_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, mask, positions=positions, scale=scale, window=window, out=out, lse=lse, status=status,
+                                  workspace=workspace, generic=generic, stop_after=stop_after)
+    a, out, lse, dev = _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
+    bits, ld = _mask(mask, a.T, dev)
+    words = mask.shape[1]
+    _fits(words)
+    if a.window and positions is None:
+        raise ValueError("a window needs the rows' positions")
+    lib = _lib or load_library()
+    keep = _workspace(lib, a, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
+    d = TreeAttentionDesc(a, words, ld, bits, None if positions is None else _flat(positions, _I32, a.T, dev))
+    _launch(lib.specsteer_tree_attention, "specsteer_tree_attention", d, dev)
+    return out, lse
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, temperature: Optional[torch.Tensor] = None, top: int = 0,
+                   out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """What softmax(logits / temperature) says of every row of logits [R, V]: a dict with lse and entropy [R], with tokens
+    ([R] or [R, M] int32; -1: none) their logprob in the same shape, and with top > 0 top_id and top_logprob [R, top], the likeliest
+    tokens in order, the lowest id among equals.  temperature [R] float32; ``out``: tensors to write into; status [R] int32: bits
+    are OR-ed into it.  Definition and refusals: specsteer_token_logprobs."""
+    if stream is not None:
+        with _on(stream, logits):
+            return token_logprobs(logits, tokens, temperature=temperature, top=top, out=out, status=status)
+    dev, code, top = logits.get_device(), _CACHE_DTYPES.get(logits.dtype), int(top)
+    if logits.dim() != 2 or code is None or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [R, V] float32, bfloat16 or float16 with a contiguous last axis")
+    R, V = logits.shape
+    M = 0 if tokens is None else 1 if tokens.dim() == 1 else tokens.shape[1]
+    _fits(max(R, V, M, top), top)
+    if not 0 <= top <= min(V, TOP_MAX):
+        raise ValueError("top must be 0 to %d, and at most V" % TOP_MAX)
+    if out is None:
+        e = lambda *n, dt=torch.float32: torch.empty(n, dtype=dt, device=logits.device)  # noqa: E731
+        out = {"lse": e(R), "entropy": e(R)}
+        if tokens is not None:
+            out["logprob"] = e(*tokens.shape)
+        if top:
+            out["top_id"], out["top_logprob"] = e(R, top, dt=_I32), e(R, top)
+    d = TokenLogprobsDesc(R, V, M, top, code, logits.stride(0) if R > 1 else V, M, logits.data_ptr(), None if temperature is None else _flat(temperature, torch.float32, R, dev),
+                          None if tokens is None else _flat(tokens, _I32, R * M, dev), None if tokens is None else _flat(out["logprob"], torch.float32, R * M, dev),
+                          _flat(out["lse"], torch.float32, R, dev), _flat(out["entropy"], torch.float32, R, dev),
+                          _flat(out["top_id"], _I32, R * top, dev) if top else None, _flat(out["top_logprob"], torch.float32, R * top, dev) if top else None,
+                          None if status is None else _flat(status, _I32, R, dev))
+    _launch((_lib or load_library()).specsteer_token_logprobs, "specsteer_token_logprobs", d, dev)
+    return out
+
+
+def tree_keep(parent: torch.Tensor, token: torch.Tensor, choice: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor,
+              block_table: Optional[torch.Tensor] = None, k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None, *, max_out: int,
+              out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """End a round over trees: from the root on, follow the row whose token is the one chosen behind its parent (choice [T]: the
+    likeliest, or a sample), up to max_out rows, and move the path's keys and values together in the caches, [n_pages,
+    page_size, Hkv, D] or [layers, n_pages, page_size, Hkv, D] (None: only the path).  Returns n_out [B] (the next plan's
+    advance), path and out_tokens [B, max_out] (what the round emits, -1 behind it), all int32.  Definition and refusals:
+    specsteer_tree_keep."""
+    if stream is not None:
+        with _on(stream, parent):
+            return tree_keep(parent, token, choice, cu_new, kv_len, block_table, k_cache, v_cache, max_out=max_out, out=out, status=status)
+    dev, T, B, max_out = parent.get_device(), parent.numel(), kv_len.numel(), int(max_out)
+    _fits(max(T, B, max_out), max_out)
+    if max_out < 1:
+        raise ValueError("max_out must be at least 1")
+    if out is None:
+        out = {"n_out": torch.empty(B, dtype=_I32, device=parent.device)}
+        for name in ("path", "out_tokens"):
+            out[name] = torch.empty((B, max_out), dtype=_I32, device=parent.device)
+    d = TreeKeepDesc(B, T, max_out)
+    if k_cache is not None:
+        if v_cache is None or block_table is None:
+            raise ValueError("the caches come together, with the block table")
+        shape, dtype, e, f = k_cache.shape, k_cache.dtype, k_cache.stride(), v_cache.stride()
+        if len(shape) not in (4, 5) or shape != v_cache.shape or dtype is not v_cache.dtype or k_cache.get_device() != dev or v_cache.get_device() != dev:
+            raise ValueError("k_cache and v_cache must share shape [(layers,) n_pages, page_size, Hkv, D] and dtype, on the device of the others")
+        code = _CACHE_DTYPES.get(dtype)
+        if code is None or (shape[-1] > 1 and (e[-1] != 1 or f[-1] != 1)):
+            raise ValueError("the caches must be float32, bfloat16 or float16 with a contiguous last axis")
+        table, rows, width, ld = _table(block_table, dev)
+        if rows != B:
+            raise ValueError("block_table must have a row a request")
+        _fits(max(max(shape), width))
+        if len(shape) == 4:
+            shape, e, f = (1, *shape), (0, *e), (0, *f)
+        d = TreeKeepDesc(B, T, max_out, shape[0], shape[3], shape[4], shape[2], shape[1], width, code, ld, e[0], e[1], e[2], e[3], f[0], f[1], f[2], f[3],
+                         block_table=table, k_cache=k_cache.data_ptr(), v_cache=v_cache.data_ptr())
+    elif v_cache is not None or block_table is not None:
+        raise ValueError("the caches come together, with the block table")
+    d.parent, d.token, d.choice = _flat(parent, _I32, T, dev), _flat(token, _I32, T, dev), _flat(choice, _I32, T, dev)
+    d.cu_new, d.kv_len, d.n_out = _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev), _flat(out["n_out"], _I32, B, dev)
+    d.path, d.out_tokens = _flat(out["path"], _I32, B * max_out, dev), _flat(out["out_tokens"], _I32, B * max_out, dev)
+    if status is not None:
+        d.req_status = _flat(status, _I32, B, dev)
+    _launch((_lib or load_library()).specsteer_tree_keep, "specsteer_tree_keep", d, dev)
+    return out

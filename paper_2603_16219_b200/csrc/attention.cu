@@ -27,8 +27,8 @@ __device__ __forceinline__ void from_f32(float x, __nv_bfloat16* y) { *y = __flo
 __device__ __forceinline__ void from_f32(float x, __half* y) { *y = __float2half_rn(x); }
 
 // Blocks of kGenRows rows are numbered request by request; a block finds its request from the lengths (device data).
-template <typename T>
-__global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const specsteer_attention_desc p) {
+template <typename T, bool TREE>
+__global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const specsteer_attention_desc p, const TreeMask tree) {
   __shared__ float qs[kGenRows][kGenMaxD];   // the queries; at the end of a split block its sums
   __shared__ T ks[kGenKeys][kGenMaxD + 2];   // an odd number of words a row: 8 keys in 8 banks
   __shared__ float ps[kGenRows][kGenKeys];
@@ -48,9 +48,10 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
   // float32's range; with a small one the product, so that the difference of two scores may.  natural: of a maximum.
   const float c = p.scale * kLog2e, pre = c < 1.f ? c : 1.f, post = c < 1.f ? 1.f : c, natural = c < 1.f ? kLn2 : p.scale;
 
+  auto request = [&](int b) { return TREE ? attn_request_tree(p, tree, b) : attn_request(p, b); };
   if (blockIdx.x == 0 && hk == 0 && p.req_status)
     for (int b = tid; b < p.B; b += kGenThreads)
-      if (attn_request(p, b).bad) atomicOr(p.req_status + b, SPECSTEER_REQ_BAD_LEN);
+      if (request(b).bad) atomicOr(p.req_status + b, SPECSTEER_REQ_BAD_LEN);
 
   // blk runs over this block's share of all blocks; `before` = blocks of the requests ahead of request `b0`
   long long before = 0;
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
     while (b0 < p.B) {
       const int b = b0 + tid;
       long long mine = 0;
-      if (b < p.B) mine = ((long long)attn_request(p, b).n * G + kGenRows - 1) / kGenRows;
+      if (b < p.B) mine = ((long long)request(b).n * G + kGenRows - 1) / kGenRows;
       long long x = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -85,7 +86,8 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
     }
     if (found_b < 0) return;
     const int b = found_b;
-    const AttnRequest rq = attn_request(p, b);
+    const AttnRequest rq = request(b);
+    const int past = rq.kv - rq.n;                         // keys before the chunk
     const long long r0 = (blk - found_at) * kGenRows;      // first row of the block within the request and kv head
     const long long n_rows = (long long)rq.n * G;
     if (tid == 0) bad_page = 0;
@@ -100,11 +102,15 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
     const int row = tid >> 3, sub = tid & 7;
     const long long my_row = r0 + row;
     int lo = 0, hi = 0;
-    if (my_row < n_rows) attn_span(p, rq, (int)(my_row / G), lo, hi);
+    if (my_row < n_rows) {
+      attn_span(p, rq, (int)(my_row / G), lo, hi);
+      if (TREE) { lo = tree_row_lo(p, tree, rq, (int)(my_row / G)); hi = rq.kv; }
+    }
     const int last_row = (int)((r0 + kGenRows < n_rows ? r0 + kGenRows : n_rows) - 1 - r0);
     int blo, bhi, tmp;
     attn_span(p, rq, (int)(r0 / G), blo, tmp);
     attn_span(p, rq, (int)((r0 + last_row) / G), tmp, bhi);
+    if (TREE) { blo = tree_lo(p, past); bhi = rq.kv; }
     float m = kNegInf, l = 0.f;
     float acc[kGenRows][2];
 #pragma unroll
@@ -152,6 +158,7 @@ __global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const sp
       for (int i = 0; i < 4; ++i) {
         const int j = k0 + sub + 8 * i;
         seen[i] = j >= lo && j < hi && page_s[sub + 8 * i] >= 0;
+        if (TREE && j >= past) seen[i] = j < hi && page_s[sub + 8 * i] >= 0 && (tree_bits(tree, rq.row0 + my_row / G, rq.n, j - past) & 1u);
         s[i] *= pre;
         if (seen[i]) mt = s[i] > mt || s[i] != s[i] ? s[i] : mt;   // a NaN stays
       }
@@ -268,20 +275,14 @@ specsteer_status check_attention(const specsteer_attention_desc* d) {
 
 using namespace specsteer;
 
-extern "C" size_t specsteer_chunk_attention_workspace(const specsteer_attention_desc* d) {
-  if (check_attention(d) != SPECSTEER_OK || d->B == 0 || d->T == 0) return 0;
-  return attention_tc_takes(d) ? attention_tc_workspace(d) : 0;
-}
+namespace {
 
-extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_desc* d, void* cuda_stream) {
-  const specsteer_status st = check_attention(d);
-  if (st != SPECSTEER_OK) return st;
+specsteer_status run_attention(const specsteer_attention_desc* d, const TreeMask& tree, cudaStream_t s) {
   if (d->B == 0 || d->T == 0) return SPECSTEER_OK;
   const size_t need = specsteer_chunk_attention_workspace(d);
   if (need > 0 && (!d->workspace || d->workspace_bytes < (long long)need || ((uintptr_t)d->workspace & 31u))) return SPECSTEER_ERR_WORKSPACE;
-  cudaStream_t s = (cudaStream_t)cuda_stream;
   if (attention_tc_takes(d)) {
-    if (launch_attention_tc(d, s) != cudaSuccess) {
+    if (launch_attention_tc(d, tree, s) != cudaSuccess) {
       cudaGetLastError();
       return SPECSTEER_ERR_CUDA;
     }
@@ -303,11 +304,34 @@ extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = d->dtype == SPECSTEER_BF16 ? cudaLaunchKernelEx(&cfg, attention_generic_kernel<__nv_bfloat16>, *d)
-                                                   : cudaLaunchKernelEx(&cfg, attention_generic_kernel<__half>, *d);
+  const bool bf16 = d->dtype == SPECSTEER_BF16;
+  const cudaError_t e = tree.bits ? (bf16 ? cudaLaunchKernelEx(&cfg, attention_generic_kernel<__nv_bfloat16, true>, *d, tree)
+                                          : cudaLaunchKernelEx(&cfg, attention_generic_kernel<__half, true>, *d, tree))
+                                  : (bf16 ? cudaLaunchKernelEx(&cfg, attention_generic_kernel<__nv_bfloat16, false>, *d, tree)
+                                          : cudaLaunchKernelEx(&cfg, attention_generic_kernel<__half, false>, *d, tree));
   if (e != cudaSuccess) {
     cudaGetLastError();
     return SPECSTEER_ERR_CUDA;
   }
   return SPECSTEER_OK;
+}
+
+}  // namespace
+
+extern "C" size_t specsteer_chunk_attention_workspace(const specsteer_attention_desc* d) {
+  if (check_attention(d) != SPECSTEER_OK || d->B == 0 || d->T == 0) return 0;
+  return attention_tc_takes(d) ? attention_tc_workspace(d) : 0;
+}
+
+extern "C" specsteer_status specsteer_chunk_attention(const specsteer_attention_desc* d, void* cuda_stream) {
+  const specsteer_status st = check_attention(d);
+  return st != SPECSTEER_OK ? st : run_attention(d, TreeMask{}, (cudaStream_t)cuda_stream);
+}
+
+extern "C" specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc* d, void* cuda_stream) {
+  const specsteer_status st = d ? check_attention(&d->a) : SPECSTEER_ERR_INVALID_ARG;
+  if (st != SPECSTEER_OK) return st;
+  if (d->mask_words < 1 || d->ld_mask < d->mask_words) return SPECSTEER_ERR_INVALID_ARG;
+  if (d->a.B > 0 && d->a.T > 0 && (!d->mask || (d->a.window > 0 && !d->positions))) return SPECSTEER_ERR_INVALID_ARG;
+  return run_attention(&d->a, TreeMask{d->mask, d->ld_mask, d->mask_words, d->positions}, (cudaStream_t)cuda_stream);
 }

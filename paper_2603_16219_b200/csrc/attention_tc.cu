@@ -116,6 +116,7 @@ static_assert(sizeof(TcShared) % 8 == 0 && tc_smem_bytes<128>() <= 232448 && tc_
 
 struct TcParams {
   specsteer_attention_desc d;
+  TreeMask tree;
   int G, box_tok, box_rows, tile_tok;  // query box: tokens and rows; tokens of a query tile
   int page_rows, boxes, page_shift;    // key box: keys, boxes per block, log2 of its keys
   int page_blocks, pb_shift;           // blocks per page (1 when a block has several pages), log2 of them or -1
@@ -359,6 +360,13 @@ __device__ __forceinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
 // batch of 64 single tokens takes 121 / 85 / 93 us instead of 80, four prompt chunks with 4 in place of 6 309 us instead of 287.
 __device__ __forceinline__ int unit_base(bool two) { return two ? 6 : 4; }
 
+// TREE here and below: rows of trees of drafts, which see the cached keys before the chunk and, of the chunk's own, those of their
+// mask.  What depends on it are the spans of a unit, taken as wide as any row's, and the keys that a row keeps in a block at the edge.
+template <bool TREE> __device__ __forceinline__ AttnRequest request_of(const TcParams& p, int b) {
+  if constexpr (TREE) return attn_request_tree(p.d, p.tree, b);
+  else return attn_request(p.d, b);
+}
+
 struct Unit {
   int tok0, tok1;          // tokens of the request
   bool two;                // two query tiles
@@ -366,13 +374,21 @@ struct Unit {
   int lo_first, lo_last;   // and begin here
   int t0, nt;              // first key tile, key tiles (at least one, so that a unit that sees nothing is written too)
 };
-__device__ __forceinline__ Unit make_unit(const TcParams& p, const AttnRequest& rq, int u) {
+template <bool TREE> __device__ __forceinline__ Unit make_unit(const TcParams& p, const AttnRequest& rq, int u) {
   Unit x;
   x.tok0 = u * 2 * p.tile_tok;
   x.tok1 = min(rq.n, x.tok0 + 2 * p.tile_tok);
   x.two = x.tok1 - x.tok0 > p.tile_tok;
-  attn_span(p.d, rq, x.tok0, x.lo_first, x.hi_first);
-  attn_span(p.d, rq, x.tok1 - 1, x.lo_last, x.hi_last);
+  if constexpr (TREE) {
+    const int past = rq.kv - rq.n;
+    x.lo_first = tree_lo(p.d, past);                  // of a row as near as the root
+    x.lo_last = tree_lo(p.d, past + x.tok1 - 1);      // of one as far as its own place
+    x.hi_first = past;                                // every row sees the keys up to here
+    x.hi_last = rq.kv;
+  } else {
+    attn_span(p.d, rq, x.tok0, x.lo_first, x.hi_first);
+    attn_span(p.d, rq, x.tok1 - 1, x.lo_last, x.hi_last);
+  }
   x.t0 = x.lo_first / kKeys;
   x.nt = max(1, (max(x.hi_last, 0) + kKeys - 1) / kKeys - x.t0);
   return x;
@@ -384,15 +400,15 @@ __device__ __forceinline__ int cut_tile(const Unit& x, long long pos) {
   return pos <= base ? 0 : (int)min((long long)x.nt, (pos - base) >> (x.two ? 1 : 0));
 }
 __device__ __forceinline__ int n_units(const TcParams& p, const AttnRequest& rq) { return (rq.n + 2 * p.tile_tok - 1) / (2 * p.tile_tok); }
-__device__ __forceinline__ long long head_cost(const TcParams& p, const AttnRequest& rq) {
+template <bool TREE> __device__ __forceinline__ long long head_cost(const TcParams& p, const AttnRequest& rq) {
   long long c = 0;
 #pragma unroll 1
-  for (int u = 0, nu = n_units(p, rq); u < nu; ++u) c += unit_cost(make_unit(p, rq, u));
+  for (int u = 0, nu = n_units(p, rq); u < nu; ++u) c += unit_cost(make_unit<TREE>(p, rq, u));
   return c;
 }
 
 // Walks this CTA's share: the pieces [off, off + take) of consecutive units.
-struct Walk {
+template <bool TREE> struct Walk {
   int b, hk, u, off, take, index;
   long long end;     // where the range ends, from the beginning of the unit
   AttnRequest rq;
@@ -406,8 +422,8 @@ struct Walk {
   __device__ __forceinline__ void load(const TcParams& p) {
     take = 0;
     if (end <= 0) return;
-    rq = attn_request(p.d, b);
-    x = make_unit(p, rq, u);
+    rq = request_of<TREE>(p, b);
+    x = make_unit<TREE>(p, rq, u);
     take = (end >= unit_cost(x) ? x.nt : cut_tile(x, end)) - off;
   }
   __device__ __forceinline__ void next(const TcParams& p) {
@@ -419,7 +435,7 @@ struct Walk {
       u = 0;
       if (++hk == p.d.Hkv) {
         hk = 0;
-        do { ++b; } while (b + 1 < p.d.B && attn_request(p.d, b).n == 0);   // end > 0: a request with rows follows
+        do { ++b; } while (b + 1 < p.d.B && request_of<TREE>(p, b).n == 0);   // end > 0: a request with rows follows
       }
     }
   }
@@ -455,7 +471,7 @@ __device__ __forceinline__ long long block_sum(long long v, TcShared* sh, long l
   return before + x - v;
 }
 
-template <int DP, bool BF>
+template <int DP, bool BF, bool TREE>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                     const __grid_constant__ TcParams p) {
@@ -496,9 +512,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     long long mine = 0, total;
 #pragma unroll 1
     for (int b = b_lo; b < b_hi; ++b) {
-      const AttnRequest rq = attn_request(p.d, b);
+      const AttnRequest rq = request_of<TREE>(p, b);
       if (rq.bad && blockIdx.x == 0 && p.d.req_status) atomicOr(p.d.req_status + b, SPECSTEER_REQ_BAD_LEN);
-      if (rq.n > 0) mine += head_cost(p, rq) * p.d.Hkv;
+      if (rq.n > 0) mine += head_cost<TREE>(p, rq) * p.d.Hkv;
     }
     const long long before = block_sum(mine, sh, &total);   // (its barrier also publishes the set-up above)
     const long long s0 = total * blockIdx.x / gridDim.x, s1 = total * (blockIdx.x + 1) / gridDim.x;
@@ -506,15 +522,15 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       long long rem = s0 - before;
 #pragma unroll 1
       for (int b = b_lo; b < b_hi; ++b) {
-        const AttnRequest rq = attn_request(p.d, b);
+        const AttnRequest rq = request_of<TREE>(p, b);
         if (rq.n == 0) continue;
-        const long long per_head = head_cost(p, rq);
+        const long long per_head = head_cost<TREE>(p, rq);
         if (rem >= per_head * p.d.Hkv) { rem -= per_head * p.d.Hkv; continue; }
         const int hk = (int)(rem / per_head);
         rem -= hk * per_head;
 #pragma unroll 1
         for (int u = 0;; ++u) {
-          const Unit x = make_unit(p, rq, u);
+          const Unit x = make_unit<TREE>(p, rq, u);
           if (rem >= unit_cost(x)) { rem -= unit_cost(x); continue; }
           sh->start_b = b; sh->start_hk = hk; sh->start_u = u; sh->start_off = cut_tile(x, rem);
           sh->end = rem + s1 - s0;
@@ -549,7 +565,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     int limit = kPolls;
     const int stop_at = keys ? p.stop_at : 0x7fffffff;
     bool lost = false;
-    Walk w;
+    Walk<TREE> w;
     w.begin(sh);
 #pragma unroll 1
     for (;; ++pc) {
@@ -793,6 +809,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (live) {
         hi = x.kv - x.n + tok + 1;
         lo = p.d.window > 0 && hi > p.d.window ? hi - p.d.window : 0;
+        if constexpr (TREE) {   // the cached keys before the chunk; its own are looked up at the edge
+          hi = x.kv - x.n;
+          lo = tree_row_lo(p.d, p.tree, AttnRequest{x.row0, x.n, x.kv, false}, tok);
+        }
       }
       const int hi_first = x.hi_first, lo_last = x.lo_last;
       float m = live ? kNegInf : 0.f, l = 0.f;       // reference (raw score; none yet: -inf), sum
@@ -861,6 +881,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // the columns of 32 that the row sees, as bits
                 const int from = max(lo - k0 - i, 0), to = min(hi - k0 - i, 32);
                 uint32_t keep = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
+                if constexpr (TREE) {
+                  if (live) keep |= tree_bits(p.tree, (long long)x.row0 + tok, x.n, k0 + i - hi);
+                }
                 if (bad) {
 #pragma unroll 1
                   for (int j = 0; j < 32; j += 8)   // boxes hold 8 keys or more
@@ -1004,10 +1027,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             for (int j = 0; j < 32; ++j) o[j] *= f0;
           }
           if (poisoned && live) {
-            const int k_lo = max(lo, first * kKeys), k_hi = min(hi, (first + take) * kKeys);
+            const int k_lo = TREE ? first * kKeys : max(lo, first * kKeys), k_hi = min(TREE ? x.kv : hi, (first + take) * kKeys);
 #pragma unroll 1
             for (int key = k_lo; key < k_hi; ++key) {
               if (key < hi_first && key >= lo_last) continue;   // only those that were taken out
+              if constexpr (TREE) {
+                if (key < hi ? key < lo : !(tree_bits(p.tree, row, x.n, key - hi) & 1u)) continue;
+              }
               const int page = p.d.block_table[(long long)x.b * p.d.ld_table + key / p.d.page_size];
               if (page < 0 || page >= p.d.n_pages) continue;
               const unsigned short* v = reinterpret_cast<const unsigned short*>(p.d.v_cache) + page * p.d.vc_page + (key % p.d.page_size) * p.d.vc_slot + x.hk * p.d.vc_head + j0;
@@ -1069,10 +1095,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 }
 
 // A call in which a bounded wait ran out leaves no number behind that could be taken for a result: NaN in every row.
-template <bool BF> __device__ __forceinline__ void spoil(const TcParams& p) {
+template <bool BF, bool TREE> __device__ __forceinline__ void spoil(const TcParams& p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   for (int b = 0; b < p.d.B; ++b) {
-    const AttnRequest rq = attn_request(p.d, b);
+    const AttnRequest rq = request_of<TREE>(p, b);
     const long long n = (long long)rq.n * p.d.Hq;
     for (long long i = warp; i < n; i += warps) {
       const long long row = rq.row0 + i / p.d.Hq, head = i % p.d.Hq;
@@ -1088,7 +1114,7 @@ template <bool BF> __device__ __forceinline__ void spoil(const TcParams& p) {
 // It waits on latency (about ten dependent trips to L2): 4 to 8 us behind the main kernel, 15 to 17 us where every CTA's
 // range cuts a unit of 256 rows (35 MB of parts); with 8 blocks a unit instead of 16 long contexts took 3 us
 // more, with 32 the same.
-template <int DP, bool BF>
+template <int DP, bool BF, bool TREE>
 __global__ void __launch_bounds__(256, 4) attention_join_kernel(const __grid_constant__ TcParams p, int n_cta) {
   pdl_launch_dependents();   // the next call's main kernel may set itself up meanwhile
   pdl_wait();
@@ -1101,12 +1127,12 @@ __global__ void __launch_bounds__(256, 4) attention_join_kernel(const __grid_con
   const bool first_block = blockIdx.x == 0 && blockIdx.y == 0;
   if (slot0 < 0 && !first_block) return;
   if (__syncthreads_or(failed)) {
-    if (first_block) spoil<BF>(p);
+    if (first_block) spoil<BF, TREE>(p);
     return;
   }
   if (slot0 < 0) return;
-  const AttnRequest rq = attn_request(p.d, h.z);
-  const Unit x = make_unit(p, rq, u);
+  const AttnRequest rq = request_of<TREE>(p, h.z);
+  const Unit x = make_unit<TREE>(p, rq, u);
   const int rows = (x.tok1 - x.tok0) * p.G, tile_rows = p.tile_tok * p.G;
   for (int q = blockIdx.y * 8 + warp; q < rows; q += gridDim.y * 8) {
     const int part_row = q < tile_rows ? q : 128 + q - tile_rows;
@@ -1227,14 +1253,14 @@ size_t head_bytes() { return (size_t)kMaxCtas * 8 * sizeof(int); }
 size_t failed_bytes() { return (size_t)kMaxCtas * sizeof(int); }
 static_assert(kMaxCtas <= 256, "a thread of attention_join_kernel for every CTA");
 
-template <int DP, bool BF>
-cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStream_t s) {
+template <int DP, bool BF, bool TREE>
+cudaError_t launch_as(const CUtensorMap* tm, const TcParams& p, int grid, cudaStream_t s) {
   static std::atomic<bool> attr_set[64];   // per device; two host threads that both find it clear set the same value
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!attr_set[dev & 63].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(attention_tc_kernel<DP, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem_bytes<DP>());
+    e = cudaFuncSetAttribute(attention_tc_kernel<DP, BF, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem_bytes<DP>());
     if (e != cudaSuccess) return e;
     attr_set[dev & 63].store(true, std::memory_order_release);
   }
@@ -1250,12 +1276,16 @@ cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStrea
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, attention_tc_kernel<DP, BF>, tm[0], tm[1], tm[2], p);
+  e = cudaLaunchKernelEx(&cfg, attention_tc_kernel<DP, BF, TREE>, tm[0], tm[1], tm[2], p);
   if (e != cudaSuccess) return e;
   cfg.gridDim = dim3(grid, 16);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, attention_join_kernel<DP, BF>, p, grid);
+  return cudaLaunchKernelEx(&cfg, attention_join_kernel<DP, BF, TREE>, p, grid);
+}
+template <int DP, bool BF>
+cudaError_t launch(const CUtensorMap* tm, const TcParams& p, int grid, cudaStream_t s) {
+  return p.tree.bits ? launch_as<DP, BF, true>(tm, p, grid, s) : launch_as<DP, BF, false>(tm, p, grid, s);
 }
 
 }  // namespace
@@ -1277,13 +1307,14 @@ bool attention_tc_takes(const specsteer_attention_desc* d) {
 
 size_t attention_tc_workspace(const specsteer_attention_desc* d) { return part_bytes(d->D <= 64 ? 64 : 128) + ml_bytes() + head_bytes() + failed_bytes(); }
 
-cudaError_t launch_attention_tc(const specsteer_attention_desc* d, cudaStream_t s) {
+cudaError_t launch_attention_tc(const specsteer_attention_desc* d, const TreeMask& tree, cudaStream_t s) {
   const int sm = current_sm_count();
   if (sm <= 0) return cudaErrorInvalidDevice;
   const bool bf16 = d->dtype == SPECSTEER_BF16;
   const int DP = d->D <= 64 ? 64 : 128;
   TcParams p;
   p.d = *d;
+  p.tree = tree;
   p.G = d->Hq / d->Hkv;
   int boxes = 0;
   query_box(p.G, &p.box_tok, &boxes);
