@@ -592,7 +592,7 @@ specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc *d
  *   lse = log Z,   logprob[r][i] = l[token[r][i]] - lse,   entropy = lse - sum p l   (nats; entries of -inf have no share),
  *   top_id[r][0..n_top): the tokens of largest x, in that order, the lowest id among equals; top_logprob theirs.
  * A token outside [0, V) has logprob -inf, and BAD_TOKEN is set unless it is -1 (no token).  A row that holds NaN or +inf, or nothing
- * but -inf, or whose l passes float32, gets NaN everywhere, ids of -1, and NONFINITE; so does one whose temperature is not
+ * but -inf, or whose lse is no finite float32, gets NaN everywhere, ids of -1, and NONFINITE; so does one whose temperature is not
  * positive and finite, with BAD_PARAM.  lse and entropy may be NULL; so may row_status,
  * into which bits are OR-ed.  Sums in float32, one read of the logits.  Equal inputs give equal bits.
  * R, n_tokens >= 0; 1 <= V; 0 <= n_top <= min(V, SPECSTEER_TOP_MAX); ld_row >= V.  dtype F32, BF16 or F16.  Any alignment is taken,

@@ -11,7 +11,7 @@ _CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libspecsteer.so")
 SOURCES = ["api.cu", "verify.cu", "recover.cu", "topk.cu", "lmhead.cu", "static_scratch.cu", "probe.cu", "cache.cu", "attention.cu", "attention_tc.cu",
            "tree.cu", "rotate.cu", "logprobs.cu"]
-HEADERS = ["common.cuh", "internal.h", "records.cuh", "recover_steer.cuh", "attention.cuh", "paged.h"]
+HEADERS = ["common.cuh", "internal.h", "records.cuh", "recover_steer.cuh", "attention.cuh", "paged.h", "f32x2.cuh"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v", "--threads", "8"]
 
