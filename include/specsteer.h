@@ -596,7 +596,8 @@ specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc *d
  * positive and finite, with BAD_PARAM.  lse and entropy may be NULL; so may row_status,
  * into which bits are OR-ed.  Sums in float32, one read of the logits.  Equal inputs give equal bits.
  * R, n_tokens >= 0; 1 <= V; 0 <= n_top <= min(V, SPECSTEER_TOP_MAX); ld_row >= V.  dtype F32, BF16 or F16.  Any alignment is taken,
- * rows of 16-byte multiples are faster.  Errors: INVALID_ARG, CUDA. */
+ * and rows of any length.  workspace: 32-byte aligned device memory of at least specsteer_token_logprobs_workspace(desc) bytes, whose content
+ * before and after the call means nothing; calls that may overlap need one each.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
 #define SPECSTEER_TOP_MAX 32
 typedef struct {
   int32_t R, V, n_tokens, n_top, dtype;
@@ -609,8 +610,12 @@ typedef struct {
   int32_t *top_id;             /* [R][n_top] */
   float *top_logprob;          /* [R][n_top] */
   int32_t *row_status;         /* [R] */
+  void *workspace;
+  int64_t workspace_bytes;
 } specsteer_token_logprobs_desc;
 specsteer_status specsteer_token_logprobs(const specsteer_token_logprobs_desc *desc, void *cuda_stream);
+/* Bytes of workspace the call needs (0 for a descriptor that specsteer_token_logprobs refuses). */
+size_t specsteer_token_logprobs_workspace(const specsteer_token_logprobs_desc *desc);
 
 /* The end of a round over trees.  token[row] is a row's token, choice[row] the one that the model emits behind it (its likeliest,
  * or one sampled from its probabilities: then the emitted tokens follow the model's law).  Per request:

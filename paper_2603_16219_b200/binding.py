@@ -43,7 +43,8 @@ EXPORTS = (
     "specsteer_shard_greedy_local", "specsteer_lmhead_shard_greedy_local", "specsteer_shard_greedy_finish",
     "specsteer_probe_ex2", "specsteer_ctx_set_wait_limit",
     "specsteer_cache_plan", "specsteer_cache_append", "specsteer_chunk_attention", "specsteer_chunk_attention_workspace",
-    "specsteer_tree_plan", "specsteer_rotate_append", "specsteer_tree_attention", "specsteer_token_logprobs", "specsteer_tree_keep",
+    "specsteer_tree_plan", "specsteer_rotate_append", "specsteer_tree_attention", "specsteer_token_logprobs", "specsteer_token_logprobs_workspace",
+    "specsteer_tree_keep",
 )
 SHARD_PARTIAL_BYTES = 64
 MAX_SHARDS = 32
@@ -151,7 +152,7 @@ class TokenLogprobsDesc(C.Structure):
     _fields_ = [
         ("R", C.c_int32), ("V", C.c_int32), ("n_tokens", C.c_int32), ("n_top", C.c_int32), ("dtype", C.c_int32), ("ld_row", C.c_int64), ("ld_tok", C.c_int64),
         ("logits", C.c_void_p), ("temperature", C.c_void_p), ("token", C.c_void_p), ("logprob", C.c_void_p), ("lse", C.c_void_p), ("entropy", C.c_void_p),
-        ("top_id", C.c_void_p), ("top_logprob", C.c_void_p), ("row_status", C.c_void_p),
+        ("top_id", C.c_void_p), ("top_logprob", C.c_void_p), ("row_status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
     ]
 
 
@@ -231,6 +232,8 @@ def load_library(path: Optional[str] = None):
         fn = getattr(lib, name)
         fn.argtypes = [C.POINTER(desc), C.c_void_p]
         fn.restype = C.c_int
+    lib.specsteer_token_logprobs_workspace.argtypes = [C.POINTER(TokenLogprobsDesc)]
+    lib.specsteer_token_logprobs_workspace.restype = C.c_size_t
     for name, desc in (("tree_plan", TreePlanDesc), ("rotate_append", RotateAppendDesc), ("tree_attention", TreeAttentionDesc), ("token_logprobs", TokenLogprobsDesc),
                        ("tree_keep", TreeKeepDesc)):
         fn = getattr(lib, "specsteer_" + name)
@@ -703,12 +706,12 @@ def _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, win
     return d, out, lse, dev
 
 
-def _workspace(lib, d: AttentionDesc, workspace: Optional[torch.Tensor], q: torch.Tensor, dev: int):
+def _workspace(size, d, workspace: Optional[torch.Tensor], x: torch.Tensor, dev: int):
     """Put the caller's workspace into the descriptor, or one from torch's pool, which is returned."""
     if workspace is None:
-        need = lib.specsteer_chunk_attention_workspace(d)
+        need = size(d)
         if need and dev >= 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
             d.workspace, d.workspace_bytes = workspace.data_ptr(), need
     else:
         d.workspace_bytes = workspace.numel()
@@ -735,7 +738,7 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                                    workspace=workspace, generic=generic, stop_after=stop_after)
     d, out, lse, dev = _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
     lib = _lib or load_library()
-    keep = _workspace(lib, d, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
+    keep = _workspace(lib.specsteer_chunk_attention_workspace, d, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
     _launch(lib.specsteer_chunk_attention, "specsteer_chunk_attention", d, dev)
     return out, lse
 
@@ -842,21 +845,22 @@ def tree_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
     if a.window and positions is None:
         raise ValueError("a window needs the rows' positions")
     lib = _lib or load_library()
-    keep = _workspace(lib, a, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
+    keep = _workspace(lib.specsteer_chunk_attention_workspace, a, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
     d = TreeAttentionDesc(a, words, ld, bits, None if positions is None else _flat(positions, _I32, a.T, dev))
     _launch(lib.specsteer_tree_attention, "specsteer_tree_attention", d, dev)
     return out, lse
 
 
 def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, temperature: Optional[torch.Tensor] = None, top: int = 0,
-                   out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+                   out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> Dict[str, torch.Tensor]:
     """What softmax(logits / temperature) says of every row of logits [R, V]: a dict with lse and entropy [R], with tokens
     ([R] or [R, M] int32; -1: none) their logprob in the same shape, and with top > 0 top_id and top_logprob [R, top], the likeliest
     tokens in order, the lowest id among equals.  temperature [R] float32; ``out``: tensors to write into; status [R] int32: bits
-    are OR-ed into it.  Definition and refusals: specsteer_token_logprobs."""
+    are OR-ed into it; workspace as for chunk_attention.  Definition and refusals: specsteer_token_logprobs."""
     if stream is not None:
         with _on(stream, logits):
-            return token_logprobs(logits, tokens, temperature=temperature, top=top, out=out, status=status)
+            return token_logprobs(logits, tokens, temperature=temperature, top=top, out=out, status=status, workspace=workspace)
     dev, code, top = logits.get_device(), _CACHE_DTYPES.get(logits.dtype), int(top)
     if logits.dim() != 2 or code is None or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [R, V] float32, bfloat16 or float16 with a contiguous last axis")
@@ -877,7 +881,9 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
                           _flat(out["lse"], torch.float32, R, dev), _flat(out["entropy"], torch.float32, R, dev),
                           _flat(out["top_id"], _I32, R * top, dev) if top else None, _flat(out["top_logprob"], torch.float32, R * top, dev) if top else None,
                           None if status is None else _flat(status, _I32, R, dev))
-    _launch((_lib or load_library()).specsteer_token_logprobs, "specsteer_token_logprobs", d, dev)
+    lib = _lib or load_library()
+    keep = _workspace(lib.specsteer_token_logprobs_workspace, d, workspace, logits, dev)   # noqa: F841
+    _launch(lib.specsteer_token_logprobs, "specsteer_token_logprobs", d, dev)
     return out
 
 

@@ -1,19 +1,19 @@
 // Log probabilities of given tokens, entropy and the likeliest tokens of rows of logits, in one read of the logits.
 //
-// Sums.  A thread walks its share of a row in chunks of 64 bytes.  With l = c x, c = log2(e)/temperature, it keeps
+// logprobs_stream_kernel reads.  All rows' tiles of 4 KB form one list, which is cut into equal ranges, a warp each, so that few
+// long rows and many short ones load the SMs alike and no warp waits for another.  With l = c x, c = log2(e)/temperature, a lane
+// keeps of a row
 //   S = sum 2^(l - ref),   W = sum 2^(l - ref) (l - ref)
-// for a reference that follows its largest l at a distance of at most 8, so that S and W are rescaled for hardly any chunk; brought
-// together at M = max l they give  lse = M + log2 S  and  entropy = log2 S - W/S, in units of log 2.  The difference of logits is
-// formed before it is scaled, so that entries of the type's lowest value, and rows of nothing else, stay in float32's range.
+// for a reference that follows its largest l at a distance of at most 8, so that S and W are rescaled for hardly any tile; at a row's
+// or a range's end the warp brings them together and leaves a record.  The difference of logits is formed before it is
+// scaled, so that entries of the type's lowest value, and rows of nothing else, stay in float32's range.  For the likeliest tokens a lane
+// leaves the largest entry of its part of a tile (a slot: 128 bytes), and the stream carries no selection at all.
 //
-// The likeliest tokens.  Besides the sums a thread leaves nothing behind but the maximum of each of its slots (one or several
-// chunks) in shared memory.  The n_top-th largest of the threads' maxima is a value that at least n_top entries reach, and only
-// the slots that reach it, hardly more than n_top of them, are read again, from L2, by warps that keep their best entries as
-// a list of one 64-bit key a lane (larger value first, then lower id).  So the stream carries no selection at all.  A slot whose best
-// possible key does not beat the list's is not read: rows with many equal entries (a masked vocabulary) cost little more.
-//
-// Few rows are split over clusters of up to 8 CTAs, whose parts the first one joins through distributed shared memory.
-#include <cooperative_groups.h>
+// logprobs_end_kernel, a CTA a row, joins the records at M = max l:  lse = M + log2 S,  entropy = log2 S - W/S  (in units of log 2).
+// From the slots' maxima it takes a bound that at least n_top entries reach (the least of the best few lanes' maxima of each
+// warp), reads the slots that reach it again, hardly more than n_top, and ranks their entries that do by counting.  Where too
+// many do (a masked vocabulary, equal entries) warps keep lists of one 64-bit key a lane instead (larger value first, then lower id)
+// and pass over slots whose best possible key does not beat the list's.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -26,14 +26,18 @@ namespace specsteer {
 namespace {
 
 typedef long long i64;
-constexpr int kLogThreads = 256, kLogWarps = kLogThreads / 32;
-constexpr int kVecs = 4;             // vectors of 16 bytes a thread has in a chunk
-constexpr int kSlots = 16;           // of a thread at most
+constexpr int kThreads = 256, kCtas = 2;   // of the streaming kernel, on an SM
+constexpr int kVecs = 8;                   // vectors of 16 bytes that a lane has of a tile
+constexpr int kTileVecs = 32 * kVecs;      // of a tile: 4 KB, a warp's step
+constexpr int kEndThreads = 128, kEndWarps = kEndThreads / 32;
+constexpr int kPicked = 512;               // slots and entries that the quick selection takes
+constexpr int kMaxSms = 148;                // the workspace is laid out for as many
 constexpr float kSlack = 8.f;        // how far l may be above the reference
 constexpr float kLeast = 1024.f;     // and below: there a weight is zero, and its product with the distance too
 
 // The types of logits: elements of a vector, the pair in a 32-bit word (16-bit types), -inf in every element, the largest of a vector.
 template <int DT> struct Logit;
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i < 2 ? (i ? v.y : v.x) : (i == 2 ? v.z : v.w); }
 template <> struct Logit<SPECSTEER_F32> {
   typedef float type;
   static constexpr int N = 4;
@@ -42,15 +46,21 @@ template <> struct Logit<SPECSTEER_F32> {
   static __device__ __forceinline__ float2 pair(const uint4& v, int i) {
     return i == 0 ? make_float2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
   }
+  // the entries that reach tau, a bit each; the entry of a bit, and its value
+  static __device__ __forceinline__ uint32_t reach(const uint4& v, float tau) {
+    return (__uint_as_float(v.x) >= tau) | (__uint_as_float(v.y) >= tau) << 1 | (__uint_as_float(v.z) >= tau) << 2 | (__uint_as_float(v.w) >= tau) << 3;
+  }
+  static __device__ __forceinline__ int entry(int bit) { return bit; }
+  static __device__ __forceinline__ float value(const uint4& v, int bit) { return __uint_as_float(word_of(v, bit)); }
   static __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
   }
-  static __device__ __forceinline__ float largest(const uint4 (&v)[kVecs]) {
+  template <int NV> static __device__ __forceinline__ float largest(const uint4 (&v)[NV]) {
     float m = __uint_as_float(v[0].x);
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) m = max3_nan(max3_nan(m, __uint_as_float(v[u].x), __uint_as_float(v[u].y)), __uint_as_float(v[u].z), __uint_as_float(v[u].w));
+    for (int u = 0; u < NV; ++u) m = max3_nan(max3_nan(m, __uint_as_float(v[u].x), __uint_as_float(v[u].y)), __uint_as_float(v[u].z), __uint_as_float(v[u].w));
     return m;
   }
 };
@@ -63,15 +73,31 @@ template <> struct Logit<SPECSTEER_BF16> {
     const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
     return make_float2(bf16lo(w), bf16hi(w));
   }
+  static __device__ __forceinline__ uint32_t reach(const uint4& v, float tau) {   // bit i: low half of word i, bit 16 + i: the high one
+    uint32_t got = 0;
+    const uint32_t t2 = __float_as_uint(tau) | __float_as_uint(tau) >> 16;          // (tau is a number of this type)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t m;
+      asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(word_of(v, i)), "r"(t2));
+      got |= (m & 0x10001u) << i;
+    }
+    return got;
+  }
+  static __device__ __forceinline__ int entry(int bit) { return 2 * (bit & 15) + (bit >> 4); }
+  static __device__ __forceinline__ float value(const uint4& v, int bit) {
+    const uint32_t w = word_of(v, bit & 15);
+    return bit >> 4 ? bf16hi(w) : bf16lo(w);
+  }
   static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
-  static __device__ __forceinline__ float largest(const uint4 (&v)[kVecs]) {
+  template <int NV> static __device__ __forceinline__ float largest(const uint4 (&v)[NV]) {
     uint32_t m = v[0].x;
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) m = max2(max2(m, v[u].x), max2(v[u].y, max2(v[u].z, v[u].w)));
+    for (int u = 0; u < NV; ++u) m = max2(max2(m, v[u].x), max2(v[u].y, max2(v[u].z, v[u].w)));
     m = max2(m, (m >> 16) | (m << 16));
     return bf16lo(m);
   }
@@ -85,15 +111,30 @@ template <> struct Logit<SPECSTEER_F16> {
     const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
   }
+  static __device__ __forceinline__ uint32_t reach(const uint4& v, float tau) {
+    uint32_t got = 0;
+    const uint32_t t1 = __half_as_ushort(__float2half_rn(tau)), t2 = t1 | t1 << 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t m;
+      asm("set.ge.u32.f16x2 %0, %1, %2;" : "=r"(m) : "r"(word_of(v, i)), "r"(t2));
+      got |= (m & 0x10001u) << i;
+    }
+    return got;
+  }
+  static __device__ __forceinline__ int entry(int bit) { return 2 * (bit & 15) + (bit >> 4); }
+  static __device__ __forceinline__ float value(const uint4& v, int bit) {
+    return __half2float(__ushort_as_half((unsigned short)(word_of(v, bit & 15) >> (bit & 16))));
+  }
   static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
-  static __device__ __forceinline__ float largest(const uint4 (&v)[kVecs]) {
+  template <int NV> static __device__ __forceinline__ float largest(const uint4 (&v)[NV]) {
     uint32_t m = v[0].x;
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) m = max2(max2(m, v[u].x), max2(v[u].y, max2(v[u].z, v[u].w)));
+    for (int u = 0; u < NV; ++u) m = max2(max2(m, v[u].x), max2(v[u].y, max2(v[u].z, v[u].w)));
     m = max2(m, (m >> 16) | (m << 16));
     return __half2float(__ushort_as_half((unsigned short)m));
   }
@@ -143,6 +184,12 @@ template <int DT> __device__ __forceinline__ float take(Sums& a, const uint4 (&v
   return mx;
 }
 
+__device__ __forceinline__ float warp_min_redux(float v) {
+  float r;
+  asm volatile("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
 // ---- lists of the best entries: one descending key a lane, 0 = empty ------------------------------------------------
 __device__ __forceinline__ void list_insert(u64& mine, u64 key, int lane) {
   const int pos = __popc(__ballot_sync(kFullMask, mine > key));
@@ -160,236 +207,418 @@ __device__ __forceinline__ u64 list_merge(u64 mine, u64 other, int lane) {
   }
   return x;
 }
-// 32 floats of a warp in descending order.
-__device__ __forceinline__ float sort_desc(float x, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-    for (int o = size >> 1; o > 0; o >>= 1) {
-      const float y = __shfl_xor_sync(kFullMask, x, o);
-      const bool low = ((lane & o) != 0) != ((lane & size) != 0 && size < 32);
-      x = low ? fminf(x, y) : fmaxf(x, y);
-    }
-  }
-  return x;
-}
-__device__ __forceinline__ float sorted_merge(float mine, float other, int lane) {
-  float x = fmaxf(mine, other);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float y = __shfl_xor_sync(kFullMask, x, o);
-    x = (lane & o) ? fminf(x, y) : fmaxf(x, y);
-  }
-  return x;
-}
 
-struct LogShared {
-  float slot[kSlots][kLogThreads];   // largest entry of each slot
-  float sorted[kLogWarps][32];
-  u64 list[kLogWarps][32];           // [0]: the CTA's
-  float red[3][kLogWarps];
-  Sums sums;                         // the CTA's, at its largest entry
-  float all[2];                      // the row's M, log2 S
-  int bad;
+struct LogParams {
+  specsteer_token_logprobs_desc d;
+  int tiles;                 // of a row (one of 16-byte aligned start has as many vectors as any)
+  long long warps;           // that share the tiles
+  double tile_inv, total_inv, warp_inv;   // 1/tiles, 1/(R tiles), 1/warps
+  float4* record;            // [R + warps]: that of warp w for row r at r + w
+  uint16_t* slot_max;        // [R][tiles][32], or nullptr: rounded down to bfloat16, of float16 logits as they are
 };
 
-template <int DT>
-__global__ void __launch_bounds__(kLogThreads, 3) logprobs_kernel(const specsteer_token_logprobs_desc p) {
-  typedef Logit<DT> L;
-  typedef typename L::type T;
-  __shared__ LogShared sh;
-  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
-  const int n_part = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const float nan = __int_as_float(0x7fc00000);
-  for (i64 r = blockIdx.x / n_part; r < p.R; r += gridDim.x / n_part) {
-    const T* x = (const T*)p.logits + r * p.ld_row;
-    const float temp = p.temperature ? p.temperature[r] : 1.f;
-    const float c = kLog2e / temp;
-    // the first of the given tokens, on their way early
-    float given = 0.f;
-    int token = -1;
-    if (part == 0 && tid < p.n_tokens) {
-      token = p.token[r * p.ld_tok + tid];
-      if (token >= 0 && token < p.V) given = L::one(x + token);
-    }
-    // [0, head): entries before the first 16-byte boundary; then whole vectors; the rest behind them
+// A row: entries before the first 16-byte boundary, whole vectors, entries behind them.
+template <int DT> struct Row {
+  typedef typename Logit<DT>::type T;
+  static constexpr int N = Logit<DT>::N;
+  const T* x;
+  int head, n_vec;
+  __device__ __forceinline__ Row(const specsteer_token_logprobs_desc& d, i64 r) {
+    x = (const T*)d.logits + r * d.ld_row;
     const int off = (int)(((uintptr_t)x & 15u) / sizeof(T));
-    const int head = min(p.V, off ? L::N - off : 0), n_vec = (p.V - head) / L::N, rest = p.V - head - n_vec * L::N;
-    const int v0 = (int)((i64)n_vec * part / n_part), v1 = (int)((i64)n_vec * (part + 1) / n_part);
-    const uint4* vec = reinterpret_cast<const uint4*>(x + head) + v0;
-    const int n = v1 - v0, iters = (n + kVecs * kLogThreads - 1) / (kVecs * kLogThreads);
-    const int per_slot = max(1, (iters + kSlots - 1) / kSlots), slots = (iters + per_slot - 1) / per_slot;
-    Sums a{kNegInf, 0.f, 0.f};
-    const uint4 none = make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
-    auto load = [&](int it, uint4 (&v)[kVecs]) {
+    head = min(d.V, off ? N - off : 0);
+    n_vec = (d.V - head) / N;
+  }
+};
+// a / b with 1/b at hand: a division of 64 bits is a hundred instructions, of a kernel that takes a few microseconds.
+__device__ __forceinline__ i64 divide(i64 a, i64 b, double inv) {
+  i64 q = (i64)((double)a * inv);   // off by one at most (a below 2^52: the rows lie in memory)
+  if (q * b > a) --q;
+  else if ((q + 1) * b <= a) ++q;
+  return q;
+}
+// The warp whose range holds a tile: ranges are [n w / W, n (w+1) / W).
+__device__ __forceinline__ i64 warp_of(const LogParams& p, i64 tile) { return divide((tile + 1) * p.warps - 1, (i64)p.d.R * p.tiles, p.total_inv); }
+
+// A slot's maximum has 16 bits.  Rounded down it serves both ends: entries reach a bound formed from such numbers, and a slot holds
+// an entry that reaches a bound of that kind just when its own number does.  Only -inf itself becomes -inf: finite numbers
+// below bfloat16's lowest become that one, which as a bound stands for float32's lowest (see tau).
+constexpr uint32_t kLowest = 0xff7f0000u;
+template <int DT> __device__ __forceinline__ uint16_t slot_bits(float x) {
+  if (DT == SPECSTEER_F16) return __half_as_ushort(__float2half_rn(x));   // (exact)
+  uint32_t b = __float_as_uint(x);                                        // (NaN may become anything: its row has no result)
+  if (DT == SPECSTEER_F32 && (b >> 31)) b = b >= kLowest && b < 0xff800000u ? kLowest : b + 0xffffu;
+  return (uint16_t)(b >> 16);
+}
+// streaming loads of what is read once, which do not push what is read again out of L2
+__device__ __forceinline__ uint4 load_once(const uint4* at, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(at), "l"(policy));
+  return v;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads, kCtas) logprobs_stream_kernel(const LogParams p) {
+  typedef Logit<DT> L;
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const i64 w = (i64)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), total = (i64)p.d.R * p.tiles;
+  if (w >= p.warps) return;
+  const i64 first = divide(total * w, p.warps, p.warp_inv), end = divide(total * (w + 1), p.warps, p.warp_inv);
+  if (first >= end) return;
+  const uint4 none = make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
+  const uint64_t policy = l2_policy_evict_first();
+  i64 r = divide(first, p.tiles, p.tile_inv);
+  int tile = (int)(first - r * p.tiles);
+  // the row and tile of the loads, one tile ahead of those of the sums
+  i64 next_r = r;
+  int next_tile = tile;
+  Row<DT> row(p.d, r);
+  float c = 0.f, next_c = kLog2e / (p.d.temperature ? p.d.temperature[r] : 1.f);
+  uint4 v[kVecs], next[kVecs];
+  auto load = [&](uint4 (&to)[kVecs]) {
+    const uint4* at = reinterpret_cast<const uint4*>(row.x + row.head) + (i64)next_tile * kTileVecs + lane;
+    const int left = row.n_vec - next_tile * kTileVecs - lane;
+    if (left > 32 * (kVecs - 1)) {
 #pragma unroll
-      for (int u = 0; u < kVecs; ++u) {
-        const i64 i = ((i64)it * kVecs + u) * kLogThreads + tid;
-        v[u] = i < n ? __ldg(vec + i) : none;
-      }
-    };
-    // entries outside the vectors: the first part's, one a thread
-    float single = kNegInf;
-    int single_at = 0x7fffffff;
-    if (part == 0 && tid < head + rest) {
-      single_at = tid < head ? tid : p.V - rest + (tid - head);
-      single = L::one(x + single_at);
-    }
-    float top = kNegInf, slot_top = kNegInf;
-    {
-      uint4 v[kVecs], next[kVecs];
-      load(0, v);
-      int left = per_slot, slot = 0;
-      for (int it = 0; it < iters; ++it) {
-        if (it + 1 < iters) load(it + 1, next);
-        slot_top = fmaxf(slot_top, take<DT>(a, v, c));
-        if (--left == 0 || it + 1 == iters) {
-          sh.slot[slot++][tid] = slot_top;
-          top = fmaxf(top, slot_top);
-          slot_top = kNegInf;
-          left = per_slot;
-        }
+      for (int u = 0; u < kVecs; ++u) to[u] = load_once(at + 32 * u, policy);
+    } else {
 #pragma unroll
-        for (int u = 0; u < kVecs; ++u) v[u] = next[u];
-      }
+      for (int u = 0; u < kVecs; ++u) to[u] = 32 * u < left ? load_once(at + 32 * u, policy) : none;
     }
-    // the threads' maxima, sorted, before the single entries join them: those are offered to the list in any case
-    if (p.n_top > 0) sh.sorted[warp][lane] = sort_desc(top, lane);
-    if (single_at != 0x7fffffff) {
-      if (single > kNegInf && single < -kNegInf) {
-        if (a.ref == kNegInf || (single - a.ref) * c > kSlack) rescale(a, single, c);
-        const float t = fmaxf((single - a.ref) * c, -kLeast), e = ex2(t);
-        a.s += e;
-        a.w = fmaf(e, t, a.w);
-        top = fmaxf(top, single);
-      } else if (single != kNegInf) {
-        a.s = nan;
+  };
+  load(v);
+  Sums a{kNegInf, 0.f, 0.f};
+  float top = kNegInf;
+  c = next_c;
+#pragma unroll 1
+  for (i64 i = first; i < end; ++i) {
+    const bool more = i + 1 < end;
+    if (more) {
+      if (++next_tile == p.tiles) {
+        next_tile = 0;
+        row = Row<DT>(p.d, ++next_r);
+        next_c = kLog2e / (p.d.temperature ? p.d.temperature[next_r] : 1.f);
       }
+      load(next);
     }
-    // the CTA's largest entry, and the sums there
-    const float m = warp_max(top);
-    if (lane == 0) sh.red[0][warp] = m;
-    __syncthreads();
-    float most = sh.red[0][0];
+    const float mx = take<DT>(a, v, c);
+    top = fmaxf(top, mx);
+    if (p.slot_max) p.slot_max[(r * p.tiles + tile) * 32 + lane] = slot_bits<DT>(mx);
+    if (!more || next_r != r) {
+      const float M = warp_max(top);
+      rescale(a, M == kNegInf ? 0.f : M, c);
+      const float s = warp_sum(a.s), ww = warp_sum(a.w);
+      if (lane == 0) p.record[r + w] = make_float4(M, s, ww, 0.f);
+      a = Sums{kNegInf, 0.f, 0.f};
+      top = kNegInf;
+      c = next_c;
+    }
+    r = next_r;
+    tile = next_tile;
 #pragma unroll
-    for (int w = 1; w < kLogWarps; ++w) most = fmaxf(most, sh.red[0][w]);
-    rescale(a, most == kNegInf ? 0.f : most, c);
-    const float ws = warp_sum(a.s), ww = warp_sum(a.w);
-    if (lane == 0) { sh.red[1][warp] = ws; sh.red[2][warp] = ww; }
-    if (p.n_top > 0) {
-      // the n_top-th largest of the threads' maxima
-      float best = sh.sorted[0][lane];
-#pragma unroll
-      for (int w = 1; w < kLogWarps; ++w) best = sorted_merge(best, sh.sorted[w][31 - lane], lane);
-      const float tau = __shfl_sync(kFullMask, best, p.n_top - 1);
-      // the slots that reach it, of this warp's own threads
-      u64 mine = 0, last = 0;
-      auto offer = [&](float value, int at, bool there) {
-        const u64 key = entry_key(value + 0.f, at);
-        uint32_t todo = __ballot_sync(kFullMask, there && key > last);
-        while (todo) {
-          const int src = __ffs(todo) - 1;
-          todo &= todo - 1;
-          list_insert(mine, __shfl_sync(kFullMask, key, src), lane);
-        }
-        last = __shfl_sync(kFullMask, mine, p.n_top - 1);
-      };
-      if (warp == 0) offer(single, single_at, single_at != 0x7fffffff);
-      for (int s = 0; s < slots; ++s) {
-        const float value = sh.slot[s][tid];
-        const i64 from = (i64)s * per_slot * kVecs * kLogThreads;   // of the slot's vectors; this lane's first is tid behind
-        uint32_t todo = __ballot_sync(kFullMask, value >= tau);
-        while (todo) {
-          const int src = __ffs(todo) - 1;
-          todo &= todo - 1;
-          const int first_vec = (int)(from + warp * 32 + src);
-          const u64 bound = entry_key(__shfl_sync(kFullMask, value, src) + 0.f, head + (v0 + first_vec) * L::N);
-          if (bound <= last) continue;
-          const int entries = per_slot * kVecs * L::N;
-          for (int e0 = 0; e0 < entries; e0 += 32) {
-            const int e = e0 + lane;
-            const i64 i = first_vec + (i64)(e / L::N) * kLogThreads;
-            const bool there = e < entries && i < n;
-            const int at = there ? head + (v0 + (int)i) * L::N + e % L::N : 0;
-            offer(there ? L::one(x + at) : 0.f, at, there);
-          }
-        }
-      }
-      sh.list[warp][lane] = mine;
-    }
-    __syncthreads();
-    if (warp == 0) {
-      if (p.n_top > 0) {
-        u64 best = sh.list[0][lane];
-#pragma unroll
-        for (int w = 1; w < kLogWarps; ++w) best = list_merge(best, sh.list[w][31 - lane], lane);
-        sh.list[0][lane] = best;
-      }
-      if (lane == 0) {
-        float s = 0.f, w = 0.f;
-#pragma unroll
-        for (int i = 0; i < kLogWarps; ++i) { s += sh.red[1][i]; w += sh.red[2][i]; }
-        sh.sums = Sums{most, s, w};
-      }
-    }
-    if (n_part > 1) cluster.sync();
-    else __syncthreads();
-    if (part == 0) {
-      if (warp == 0) {
-        u64 best = p.n_top > 0 ? sh.list[0][lane] : 0;
-        if (n_part > 1 && p.n_top > 0)
-          for (int i = 1; i < n_part; ++i) best = list_merge(best, cluster.map_shared_rank(&sh.list[0][0], i)[31 - lane], lane);
-        // the parts' sums, a lane each
-        Sums b{kNegInf, 0.f, 0.f};
-        if (lane < n_part) b = *cluster.map_shared_rank(&sh.sums, lane);
-        const float M = warp_max(b.ref);
-        rescale(b, M, c);
-        const float s = warp_sum(b.s), w = warp_sum(b.w), l2s = log2f(s), lse = fmaf(l2s, kLn2, M / temp);
-        const bool bad_temp = !(temp > 0.f && temp < -kNegInf);
-        const bool bad = bad_temp || !(s > 0.f && s < -kNegInf) || !(fabsf(lse) < -kNegInf);
-        if (lane == 0) {
-          if (p.lse) p.lse[r] = bad ? nan : lse;
-          if (p.entropy) p.entropy[r] = bad ? nan : (l2s - w / s) * kLn2;
-          if (bad && p.row_status) atomicOr(p.row_status + r, bad_temp ? SPECSTEER_REQ_BAD_PARAM : SPECSTEER_REQ_NONFINITE);
-          sh.all[0] = M;
-          sh.all[1] = l2s;
-          sh.bad = bad;
-        }
-        if (lane < p.n_top) {
-          p.top_id[r * p.n_top + lane] = bad ? -1 : (int)(0xffffffffu - (uint32_t)best);
-          p.top_logprob[r * p.n_top + lane] = bad ? nan : ((order_val((uint32_t)(best >> 32)) - M) * c - l2s) * kLn2;
-        }
-      }
-      __syncthreads();
-      const float M = sh.all[0], l2s = sh.all[1];
-      for (int i = tid; i < p.n_tokens; i += kLogThreads) {
-        if (i != tid) {
-          token = p.token[r * p.ld_tok + i];
-          if (token >= 0 && token < p.V) given = L::one(x + token);
-        }
-        const bool outside = token < 0 || token >= p.V;
-        if (outside && token != -1 && p.row_status) atomicOr(p.row_status + r, SPECSTEER_REQ_BAD_TOKEN);
-        p.logprob[r * p.ld_tok + i] = sh.bad ? nan : outside ? kNegInf : ((given - M) * c - l2s) * kLn2;
-      }
-    }
-    if (n_part > 1) cluster.sync();   // nobody overwrites its part, or leaves, before the first has read it
-    else __syncthreads();
+    for (int u = 0; u < kVecs; ++u) v[u] = next[u];
   }
 }
 
-template <int DT> cudaError_t launch(const specsteer_token_logprobs_desc* d, int split, int grid, cudaStream_t s) {
+// What no entry of a slot with (rounded) maximum x exceeds: of float32 logits the next number of bfloat16.
+template <int DT> __device__ __forceinline__ float slot_bound(float x) {
+  if (DT != SPECSTEER_F32 || x == kNegInf || x == -kNegInf) return x;
+  const int b = __float_as_int(x);
+  return x == 0.f ? __int_as_float(0x10000) : __int_as_float(b > 0 ? b + 0x10000 : b - 0x10000);
+}
+
+struct EndShared {
+  float red[3][kEndWarps];
+  float best[32];                  // the best few lanes' maxima of each warp
+  int n_slots, n_keys;
+  int slot[kPicked];
+  u64 key[kPicked];
+  u64 out[32];                     // the likeliest, in order
+};
+
+// Executed once a row, so it is its latency that counts, and that of fetching its instructions: what can be is a short loop.
+template <int DT>
+__global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogParams p) {
+  typedef Logit<DT> L;
+  typedef Logit<DT == SPECSTEER_F16 ? SPECSTEER_F16 : SPECSTEER_BF16> S;   // of the slots' maxima
+  typedef typename L::type T;
+  __shared__ EndShared sh;
+  const specsteer_token_logprobs_desc& d = p.d;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const float nan = __int_as_float(0x7fc00000);
+  const i64 r = blockIdx.x;
+  const Row<DT> row(d, r);
+  const T* x = row.x;
+  const float temp = d.temperature ? d.temperature[r] : 1.f, c = kLog2e / temp;
+  // the entries outside the vectors, one a thread
+  const int rest = d.V - row.head - row.n_vec * L::N;
+  float single = kNegInf;
+  int single_at = -1;
+  if (tid < row.head + rest) {
+    single_at = tid < row.head ? tid : d.V - rest + (tid - row.head);
+    single = L::one(x + single_at);
+  }
+  const i64 w0 = p.tiles > 0 ? warp_of(p, r * p.tiles) : 0, w1 = p.tiles > 0 ? warp_of(p, (r + 1) * p.tiles - 1) : -1;
+  if (tid == 0) sh.n_slots = sh.n_keys = 0;
+  pdl_wait();
+  // ---- the slots' maxima: vectors, kHeld a thread at a time; the last ones stay in registers
+  const int n_slot = p.tiles * 32, n_max = d.n_top > 0 ? n_slot / S::N : 0;
+  const typename S::type* slots = (const typename S::type*)p.slot_max + r * n_slot;
+  const uint4* maxima = reinterpret_cast<const uint4*>(slots);
+  constexpr int kHeld = 4;
+  const uint4 none = make_uint4(S::kNone, S::kNone, S::kNone, S::kNone);
+  const int mine = lane * kEndWarps + warp;   // in turn to the warps, which then share few of them
+  uint4 held[kHeld];
+  auto hold = [&](int base) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      const int j = base + mine + k * kEndThreads;
+      held[k] = j < n_max ? __ldcg(maxima + j) : none;
+    }
+  };
+  hold(0);
+  // ---- the row's records
+  Sums a{kNegInf, 0.f, 0.f};
+#pragma unroll 1
+  for (i64 w = w0 + tid; w <= w1; w += kEndThreads) {
+    const float4 q = __ldcg(p.record + r + w);
+    const float M = fmaxf(a.ref, q.x);
+    rescale(a, M, c);
+    Sums b{q.x, q.y, q.z};
+    rescale(b, M, c);
+    a.s += b.s;
+    a.w += b.w;
+  }
+  float top = S::largest(held);
+#pragma unroll 1
+  for (int base = kHeld * kEndThreads; base < n_max; base += kHeld * kEndThreads) {
+    hold(base);
+    top = fmaxf(top, S::largest(held));
+  }
+  if (single > kNegInf && single < -kNegInf) {
+    const float M = fmaxf(a.ref, single);
+    rescale(a, M, c);
+    const float t = fmaxf((single - M) * c, -kLeast), e = ex2(t);
+    a.s += e;
+    a.w = fmaf(e, t, a.w);
+  } else if (single != kNegInf) {
+    a.s = nan;
+  }
+  const float warp_top = warp_max_redux(a.ref);
+  if (lane == 0) sh.red[0][warp] = warp_top;
+  if (d.n_top > 0) {
+    const int few = (d.n_top + kEndWarps - 1) / kEndWarps;   // as many of each warp, of different lanes
+    float t = top;
+    if (n_slot <= kHeld * kEndThreads) {   // few vectors, which would leave lanes without a maximum: single ones
+      t = kNegInf;
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const int j = mine + k * kEndThreads;
+        if (j < n_slot) t = fmaxf(t, S::one(slots + j));
+      }
+    }
+#pragma unroll 1
+    for (int i = 0; i < few; ++i) {
+      const float b = warp_max_redux(t);
+      const uint32_t who = __ballot_sync(kFullMask, t == b);
+      if (who && lane == __ffs(who) - 1) t = kNegInf;
+      if (lane == 0) sh.best[i * kEndWarps + warp] = b;
+    }
+  }
+  __syncthreads();
+  float M = sh.red[0][0];
+#pragma unroll
+  for (int w = 1; w < kEndWarps; ++w) M = fmaxf(M, sh.red[0][w]);
+  rescale(a, M == kNegInf ? 0.f : M, c);
+  const float ws = warp_sum(a.s), ww = warp_sum(a.w);
+  if (lane == 0) { sh.red[1][warp] = ws; sh.red[2][warp] = ww; }
+  // ---- the bound, and the slots and single entries that reach it
+  float tau = kNegInf, slot_tau = kNegInf;
+  if (d.n_top > 0) {
+    const int bests = (d.n_top + kEndWarps - 1) / kEndWarps * kEndWarps;
+    tau = warp_min_redux(lane < bests ? sh.best[lane] : -kNegInf);
+    auto pick = [&](int base) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const int j = base + mine + k * kEndThreads;
+        uint32_t hits = j < n_max ? S::reach(held[k], tau) : 0u;
+        if (!hits) continue;
+        int at = atomicAdd(&sh.n_slots, __popc(hits));
+#pragma unroll 1
+        for (; hits && at < kPicked; hits &= hits - 1) sh.slot[at++] = j * S::N + S::entry(__ffs(hits) - 1);
+      }
+    };
+    if (top >= tau) {
+      int base = n_max > 0 ? (n_max - 1) / (kHeld * kEndThreads) * (kHeld * kEndThreads) : 0;   // what is held
+#pragma unroll 1
+      for (;;) {
+        pick(base);
+        if ((base -= kHeld * kEndThreads) < 0) break;
+        hold(base);
+      }
+    }
+    slot_tau = tau;
+    if (DT == SPECSTEER_F32 && __float_as_uint(tau) == kLowest) tau = -3.402823466e38f;   // of entries; slots have been picked
+    if (single_at >= 0 && single >= tau) {
+      const int at = atomicAdd(&sh.n_keys, 1);
+      if (at < kPicked) sh.key[at] = entry_key(single + 0.f, single_at);
+    }
+  }
+  __syncthreads();
+  float s = 0.f, w = 0.f;
+#pragma unroll
+  for (int i = 0; i < kEndWarps; ++i) { s += sh.red[1][i]; w += sh.red[2][i]; }
+  const float l2s = log2f(s), lse = fmaf(l2s, kLn2, M / temp);
+  const bool bad_temp = !(temp > 0.f && temp < -kNegInf);
+  const bool bad = bad_temp || !(s > 0.f && s < -kNegInf) || !(fabsf(lse) < -kNegInf);
+  // vector u of slot j, counted from the row's first; n_vec or more: there is none
+  auto vec_of = [&](int j, int u) { return (i64)(j >> 5) * kTileVecs + (j & 31) + 32 * u; };
+  const int picked = sh.n_slots;
+  if (picked <= kPicked && !bad) {
+    const uint4* vec = reinterpret_cast<const uint4*>(x + row.head);
+    constexpr int kBatch = 3;   // vectors a thread has on the way
+#pragma unroll 1
+    for (int e0 = tid; e0 < picked * kVecs; e0 += kBatch * kEndThreads) {
+      uint4 v[kBatch];
+      int at[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int e = e0 + k * kEndThreads;
+        const i64 i = e < picked * kVecs ? vec_of(sh.slot[e / kVecs], e % kVecs) : row.n_vec;
+        at[k] = row.head + (int)i * L::N;
+        v[k] = i < row.n_vec ? __ldg(vec + i) : make_uint4(0u, 0u, 0u, 0u);
+        if (i >= row.n_vec) at[k] = -1;
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        uint32_t hits = at[k] >= 0 ? L::reach(v[k], tau) : 0u;
+        if (!hits) continue;
+        int n = atomicAdd(&sh.n_keys, __popc(hits));
+#pragma unroll 1
+        for (; hits && n < kPicked; hits &= hits - 1) {
+          const int bit = __ffs(hits) - 1;
+          sh.key[n++] = entry_key(L::value(v[k], bit) + 0.f, at[k] + L::entry(bit));
+        }
+      }
+    }
+  }
+  if (tid == 0) {
+    if (d.lse) d.lse[r] = bad ? nan : lse;
+    if (d.entropy) d.entropy[r] = bad ? nan : (l2s - w / s) * kLn2;
+    if (bad && d.row_status) atomicOr(d.row_status + r, bad_temp ? SPECSTEER_REQ_BAD_PARAM : SPECSTEER_REQ_NONFINITE);
+  }
+#pragma unroll 1
+  for (int i = tid; i < d.n_tokens; i += kEndThreads) {
+    const int token = d.token[r * d.ld_tok + i];
+    const bool outside = token < 0 || token >= d.V;
+    if (outside && token != -1 && d.row_status) atomicOr(d.row_status + r, SPECSTEER_REQ_BAD_TOKEN);
+    d.logprob[r * d.ld_tok + i] = bad ? nan : outside ? kNegInf : ((L::one(x + token) - M) * c - l2s) * kLn2;
+  }
+  if (d.n_top == 0) return;
+  __syncthreads();
+  const int keys = sh.n_keys;
+  if (!bad && picked <= kPicked && keys <= kPicked) {
+#pragma unroll 1
+    for (int i = tid; i < keys; i += kEndThreads) {
+      const u64 key = sh.key[i];
+      int rank = 0;
+#pragma unroll 4
+      for (int j = 0; j < keys; ++j) rank += sh.key[j] > key;
+      if (rank < d.n_top) sh.out[rank] = key;
+    }
+  } else if (!bad) {
+    // ---- too many: lists, a warp every kEndWarps-th tile, read again where some slot may still beat the list's last
+    u64 list = 0, last = 0;
+    auto offer = [&](float value, int at, bool there) {   // by the whole warp
+      const u64 key = entry_key(value + 0.f, at);
+      uint32_t todo = __ballot_sync(kFullMask, there && key > last);
+#pragma unroll 1
+      while (todo) {
+        const int src = __ffs(todo) - 1;
+        todo &= todo - 1;
+        list_insert(list, __shfl_sync(kFullMask, key, src), lane);
+      }
+      last = __shfl_sync(kFullMask, list, d.n_top - 1);
+    };
+    if (warp == 0) offer(single, single_at, single_at >= 0);
+    const uint4* vec = reinterpret_cast<const uint4*>(x + row.head);
+#pragma unroll 1
+    for (int tile = warp; tile < p.tiles; tile += kEndWarps) {
+      const i64 from = (i64)tile * kTileVecs + lane;
+      const float most = S::one(slots + tile * 32 + lane);
+      const u64 bound = entry_key(slot_bound<DT>(most) + 0.f, row.head + (int)from * L::N);
+      if (!__any_sync(kFullMask, from < row.n_vec && most >= slot_tau && bound > last)) continue;
+      uint4 v[kVecs];
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) v[u] = from + 32 * u < row.n_vec ? __ldg(vec + from + 32 * u) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) {
+        const bool there = from + 32 * u < row.n_vec;
+#pragma unroll 1
+        for (int i = 0; i < L::N; ++i) {
+          const int bit = L::N == 8 ? (i >> 1) + 16 * (i & 1) : i;   // entry i
+          const float y = L::value(v[u], bit);
+          offer(y, row.head + (int)(from + 32 * u) * L::N + i, there && y >= tau);
+        }
+      }
+    }
+    __syncthreads();   // (the keys are read no more)
+    sh.key[tid] = list;
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll 1
+      for (int i = 1; i < kEndWarps; ++i) list = list_merge(list, sh.key[i * 32 + 31 - lane], lane);
+      sh.out[lane] = list;
+    }
+  }
+  __syncthreads();
+  if (tid < d.n_top) {
+    const u64 key = sh.out[tid];
+    d.top_id[r * d.n_top + tid] = bad ? -1 : (int)(0xffffffffu - (uint32_t)key);
+    d.top_logprob[r * d.n_top + tid] = bad ? nan : ((order_val((uint32_t)(key >> 32)) - M) * c - l2s) * kLn2;
+  }
+}
+
+struct LogPlan { int tiles, grid; long long warps; size_t record_bytes, max_bytes; };
+LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
+  LogPlan q;
+  const int es = d->dtype == SPECSTEER_F32 ? 4 : 2;
+  q.tiles = (int)(((long long)d->V * es / 16 + kTileVecs - 1) / kTileVecs);
+  const long long total = (long long)d->R * q.tiles, most = (long long)sm * kCtas * (kThreads / 32);
+  q.warps = total < most ? total : most;
+  q.grid = (int)((q.warps + kThreads / 32 - 1) / (kThreads / 32));
+  q.record_bytes = ((size_t)(d->R + q.warps) * sizeof(float4) + 31) & ~(size_t)31;
+  q.max_bytes = d->n_top > 0 ? (size_t)total * 32 * sizeof(uint16_t) : 0;
+  return q;
+}
+
+template <int DT> cudaError_t launch(const LogParams& p, const LogPlan& q, cudaStream_t s) {
+  if (q.grid > 0) {
+    logprobs_stream_kernel<DT><<<q.grid, kThreads, 0, s>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid * split);
-  cfg.blockDim = dim3(kLogThreads);
+  cfg.gridDim = dim3(p.d.R);
+  cfg.blockDim = dim3(kEndThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = split;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, logprobs_kernel<DT>, *d);
+  cfg.numAttrs = q.grid > 0 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, logprobs_end_kernel<DT>, p);
+}
+
+specsteer_status check_logprobs(const specsteer_token_logprobs_desc* d) {
+  if (!d || d->R < 0 || d->V < 1 || d->n_tokens < 0 || d->n_top < 0 || d->n_top > SPECSTEER_TOP_MAX || d->n_top > d->V || d->ld_row < d->V) return SPECSTEER_ERR_INVALID_ARG;
+  if (d->dtype != SPECSTEER_F32 && d->dtype != SPECSTEER_BF16 && d->dtype != SPECSTEER_F16) return SPECSTEER_ERR_INVALID_ARG;
+  if (d->n_tokens > 0 && d->ld_tok < d->n_tokens) return SPECSTEER_ERR_INVALID_ARG;
+  if (d->R > 0 && (!d->logits || (d->n_tokens > 0 && (!d->token || !d->logprob)) || (d->n_top > 0 && (!d->top_id || !d->top_logprob)))) return SPECSTEER_ERR_INVALID_ARG;
+  return SPECSTEER_OK;
 }
 
 }  // namespace
@@ -397,22 +626,31 @@ template <int DT> cudaError_t launch(const specsteer_token_logprobs_desc* d, int
 
 using namespace specsteer;
 
+extern "C" size_t specsteer_token_logprobs_workspace(const specsteer_token_logprobs_desc* d) {
+  if (check_logprobs(d) != SPECSTEER_OK || d->R == 0) return 0;
+  const LogPlan q = plan_of(d, kMaxSms);
+  return q.record_bytes + q.max_bytes;
+}
+
 extern "C" specsteer_status specsteer_token_logprobs(const specsteer_token_logprobs_desc* d, void* cuda_stream) {
-  if (!d || d->R < 0 || d->V < 1 || d->n_tokens < 0 || d->n_top < 0 || d->n_top > SPECSTEER_TOP_MAX || d->n_top > d->V || d->ld_row < d->V) return SPECSTEER_ERR_INVALID_ARG;
-  if (d->dtype != SPECSTEER_F32 && d->dtype != SPECSTEER_BF16 && d->dtype != SPECSTEER_F16) return SPECSTEER_ERR_INVALID_ARG;
-  if (d->n_tokens > 0 && d->ld_tok < d->n_tokens) return SPECSTEER_ERR_INVALID_ARG;
-  if (d->R == 0) return SPECSTEER_OK;
-  if (!d->logits || (d->n_tokens > 0 && (!d->token || !d->logprob)) || (d->n_top > 0 && (!d->top_id || !d->top_logprob))) return SPECSTEER_ERR_INVALID_ARG;
+  const specsteer_status st = check_logprobs(d);
+  if (st != SPECSTEER_OK || d->R == 0) return st;
+  if (!d->workspace || ((uintptr_t)d->workspace & 31u) || d->workspace_bytes < (long long)specsteer_token_logprobs_workspace(d)) return SPECSTEER_ERR_WORKSPACE;
   const int sm = current_sm_count();
   if (sm <= 0) return SPECSTEER_ERR_CUDA;
-  // Parts of a row: while the rows do not fill the SMs eight times over and a part keeps a chunk a thread.
-  const long long chunks = (long long)d->V * (d->dtype == SPECSTEER_F32 ? 4 : 2) / (16 * kVecs * kLogThreads);
-  int split = 1;
-  while (split < 8 && (long long)d->R * split < 8ll * sm && chunks >= 2 * split) split *= 2;
-  const int grid = d->R < (1 << 20) ? d->R : (1 << 20);
+  const LogPlan q = plan_of(d, sm < kMaxSms ? sm : kMaxSms);
+  LogParams p;
+  p.d = *d;
+  p.tiles = q.tiles;
+  p.warps = q.warps;
+  p.tile_inv = 1. / (q.tiles ? q.tiles : 1);
+  p.total_inv = 1. / (q.tiles ? (double)d->R * q.tiles : 1.);
+  p.warp_inv = 1. / (q.warps ? (double)q.warps : 1.);
+  p.record = (float4*)d->workspace;
+  p.slot_max = q.max_bytes ? (uint16_t*)((char*)d->workspace + q.record_bytes) : nullptr;
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  const cudaError_t e = d->dtype == SPECSTEER_F32 ? launch<SPECSTEER_F32>(d, split, grid, s)
-                        : d->dtype == SPECSTEER_BF16 ? launch<SPECSTEER_BF16>(d, split, grid, s) : launch<SPECSTEER_F16>(d, split, grid, s);
+  const cudaError_t e = d->dtype == SPECSTEER_F32 ? launch<SPECSTEER_F32>(p, q, s)
+                        : d->dtype == SPECSTEER_BF16 ? launch<SPECSTEER_BF16>(p, q, s) : launch<SPECSTEER_F16>(p, q, s);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return SPECSTEER_ERR_CUDA;
