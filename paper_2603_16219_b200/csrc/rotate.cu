@@ -2,11 +2,20 @@
 // and its attention, in one pass.
 //
 // A block takes a row (token).  Its angles are formed once, in float64, where the product of a position of 2^31 and a frequency keeps 22
-// bits behind the point of a turn, and reduced to a turn before the sine; all heads of the row share them.  A warp takes a head.
+// bits behind the point of a turn, and reduced to a turn before the sine; all heads of the row share them.
+//
+//   rotate_kernel      a warp a row, or several that share its heads where rows are few; no warp waits for another.  A lane has a piece
+//                      (16 bytes; 8 where the widths or alignments want it) of each half of a head, or two neighbouring pieces, so
+//                      that the elements of a pair meet in it, and with weights w, the norm r and an element's partner x' an
+//                      element becomes r (x A + x' B), A = w cos and B = -+w' sin, formed once a row for the queries and once
+//                      for the keys.  The words come through shared
+//                      memory, by asynchronous copies several steps ahead, which takes no registers.
+//   rotate_any_kernel  every shape, alignment and width: a warp a head, an element a lane.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "f32x2.cuh"
 #include "paged.h"
 #include "specsteer.h"
 
@@ -16,6 +25,7 @@ namespace {
 typedef long long i64;
 constexpr int kRotMaxD = SPECSTEER_ROTATE_MAX_D;
 constexpr int kRotThreads = 256;
+constexpr int kRotWarps = 16;      // on an SM
 
 __device__ __forceinline__ float load_f32(const float* x) { return *x; }
 __device__ __forceinline__ float load_f32(const __nv_bfloat16* x) { return __bfloat162float(*x); }
@@ -39,6 +49,238 @@ __device__ __forceinline__ float2 turn_of(const specsteer_rotate_append_desc& p,
   float s, c;
   sincospif(2.f * (float)turns, &s, &c);
   return make_float2(c * p.factor, s * p.factor);
+}
+
+// A word of elements as float32 (one, or a pair of 16-bit ones).
+template <int DT> struct Elem;
+template <> struct Elem<SPECSTEER_F32> { static constexpr int ES = 4; };
+template <> struct Elem<SPECSTEER_BF16> {
+  static constexpr int ES = 2;
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(bf16lo(w), bf16hi(w)); }
+  static __device__ __forceinline__ uint32_t pack(float2 x) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(x.y), "f"(x.x));
+    return r;
+  }
+};
+template <> struct Elem<SPECSTEER_F16> {
+  static constexpr int ES = 2;
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+  static __device__ __forceinline__ uint32_t pack(float2 x) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(x.y), "f"(x.x));
+    return r;
+  }
+};
+// WORDS words of a head, moved at once.
+template <int WORDS> struct Piece;
+template <> struct Piece<2> {
+  uint32_t w[2];
+  __device__ __forceinline__ void get(const void* at) { const uint2 v = *(const uint2*)at; w[0] = v.x; w[1] = v.y; }
+  __device__ __forceinline__ void put(void* at) const { *(uint2*)at = make_uint2(w[0], w[1]); }
+  static __device__ __forceinline__ void fetch(void* to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(from) : "memory"); }
+};
+template <> struct Piece<4> {
+  uint32_t w[4];
+  __device__ __forceinline__ void get(const void* at) { const uint4 v = *(const uint4*)at; w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+  __device__ __forceinline__ void put(void* at) const { *(uint4*)at = make_uint4(w[0], w[1], w[2], w[3]); }
+  static __device__ __forceinline__ void fetch(void* to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory"); }
+};
+template <int DT, int WORDS> __device__ __forceinline__ void unpack(const Piece<WORDS>& v, float2 (&x)[WORDS * 2 / Elem<DT>::ES]) {
+  if constexpr (DT == SPECSTEER_F32) {
+#pragma unroll
+    for (int i = 0; i < WORDS / 2; ++i) x[i] = make_float2(__uint_as_float(v.w[2 * i]), __uint_as_float(v.w[2 * i + 1]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) x[i] = Elem<DT>::unpack(v.w[i]);
+  }
+}
+template <int DT, int WORDS> __device__ __forceinline__ void pack(const float2 (&x)[WORDS * 2 / Elem<DT>::ES], Piece<WORDS>& v) {
+  if constexpr (DT == SPECSTEER_F32) {
+#pragma unroll
+    for (int i = 0; i < WORDS / 2; ++i) { v.w[2 * i] = __float_as_uint(x[i].x); v.w[2 * i + 1] = __float_as_uint(x[i].y); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v.w[i] = Elem<DT>::pack(x[i]);
+  }
+}
+
+constexpr int kAhead = 6;   // steps whose copies a warp has on the way
+// A lane has two pieces of WORDS words.  G: lanes of a head, a power of two that covers it.  2^parts_log warps share a row; page_log:
+// log2 of the page size, or -1.
+template <int DT, int WORDS, int G, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kRotThreads, kRotWarps * 32 / kRotThreads)
+rotate_kernel(const specsteer_rotate_append_desc p, const int parts_log, const int page_log) {
+  __shared__ __align__(16) uint32_t ring[kRotThreads / 32][kAhead][2][32][WORDS];   // a lane's places are its own: nobody waits for anybody
+  constexpr int ES = Elem<DT>::ES, H = WORDS * 4 / ES, P = H / 2, kAtOnce = 32 / G;   // elements of a piece, their pairs; heads of a warp's step
+  const int lane = threadIdx.x & 31, l = lane & (G - 1), group = lane / G;
+  const i64 warp = (i64)blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5);
+  const i64 t = warp >> parts_log;
+  const int parts = 1 << parts_log, part = (int)warp & (parts - 1);
+  if (t >= p.T) return;
+  const int half = p.rot / 2;
+  const bool mine = l * 2 * H < p.D;
+  // the lane's two pieces: elements e0.. and e1..; their first pair, and whether they are turned
+  const bool turned = NEIGHBOURS ? l * 2 * H < p.rot : l < half / H;
+  const int e0 = NEIGHBOURS ? l * 2 * H : turned ? l * H : p.rot + (l - half / H) * 2 * H;
+  const int e1 = !NEIGHBOURS && turned ? half + l * H : e0 + H;
+  const int pair0 = l * H;
+  // Steps of kAtOnce heads: of the queries, then of the keys, then of the values, in turn to the row's warps.
+  const int q_steps = (p.Hq + kAtOnce - 1) / kAtOnce, k_steps = (p.Hkv + kAtOnce - 1) / kAtOnce;
+  const int from_k = (part - q_steps) & (parts - 1), from_v = (from_k - k_steps) & (parts - 1);
+  // A lane's way along the heads of one tensor: its two pieces of every step's head.
+  struct Way {
+    char *at0, *at1;
+    int left;      // heads to go, this one among them (none: 0 or less)
+    i64 step;
+    __device__ __forceinline__ void next(int heads) { at0 += step; at1 += step; left -= heads; }
+    __device__ __forceinline__ void put(const Piece<WORDS>& a, const Piece<WORDS>& b) const {
+      if (left > 0) { a.put(at0); b.put(at1); }
+    }
+  };
+  const int heads = parts * kAtOnce;   // from step to step of a warp
+  auto way = [&](const void* base, i64 offset, i64 stride, int from, int n) {
+    const int h = from * kAtOnce + group;
+    char* at = (char*)base + (offset + h * stride) * ES;
+    return Way{at + e0 * ES, at + e1 * ES, mine ? n - h : 0, heads * stride * ES};
+  };
+  // The warp's steps: first nq of the queries, then of the keys, then of the values; step i is fetched kAhead steps before its turn.
+  const int nq = (q_steps - part + parts - 1) >> parts_log, nk = (k_steps - from_k + parts - 1) >> parts_log, nv = (k_steps - from_v + parts - 1) >> parts_log;
+  const int n = nq + nk + nv;
+  uint32_t (*mine_s)[2][32][WORDS] = ring[threadIdx.x >> 5];
+  Way src = way(p.q, t * p.q_tok, p.q_head, part, p.Hq);
+  auto fetch = [&](int i, int at) {
+    if (i == nq) src = way(p.k, t * p.k_tok, p.k_head, from_k, p.Hkv);
+    if (i == nq + nk) src = way(p.v, t * p.v_tok, p.v_head, from_v, p.Hkv);
+    if (i < n) {
+      if (src.left > 0) {
+        Piece<WORDS>::fetch(mine_s[at][0][lane], src.at0);
+        Piece<WORDS>::fetch(mine_s[at][1][lane], src.at1);
+      }
+      src.next(heads);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (!mine) {   // lanes beside a head that does not fill its group add nothing to its norm
+    Piece<WORDS> zero;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) zero.w[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) { zero.put(mine_s[i][0][lane]); zero.put(mine_s[i][1][lane]); }
+  }
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(i, i);
+  const i64 slot = p.Hkv > 0 ? p.slot_map[t] : -1;
+  float w0[H], w1[H];
+  auto weights = [&](const void* weight) {
+#pragma unroll
+    for (int i = 0; i < H; ++i) w0[i] = w1[i] = 1.f;
+    if (weight && mine) {
+      if (p.weight_dtype == SPECSTEER_F32) {
+#pragma unroll
+        for (int i = 0; i < H; ++i) { w0[i] = ((const float*)weight)[e0 + i]; w1[i] = ((const float*)weight)[e1 + i]; }
+      } else {
+#pragma unroll
+        for (int i = 0; i < H; ++i) { w0[i] = weight_at(weight, p.weight_dtype, e0 + i); w1[i] = weight_at(weight, p.weight_dtype, e1 + i); }
+      }
+    }
+  };
+  weights(p.q_weight);
+  // ---- the angles of the lane's H pairs: the warp's groups have the same ones, so each forms its share
+  float2 cs[H];
+#pragma unroll
+  for (int i = 0; i < H; ++i) cs[i] = make_float2(1.f, 0.f);
+  if (p.rot > 0) {
+#pragma unroll
+    for (int i = 0; i < H; i += kAtOnce) {
+      float2 one = make_float2(1.f, 0.f);
+      const int my = i + (kAtOnce > 1 ? group % (H < kAtOnce ? H : kAtOnce) : 0);
+      if (turned) one = turn_of(p, (int)t, pair0 + my);
+#pragma unroll
+      for (int j = 0; j < kAtOnce && i + j < H; ++j) {
+        const int from = j * G + l;
+        cs[i + j] = make_float2(__shfl_sync(kFullMask, one.x, from), __shfl_sync(kFullMask, one.y, from));
+      }
+    }
+  }
+  // ---- a lane's element x with partner x' becomes r (x A + x' B)
+  float2 A0[P], B0[P], A1[P], B1[P];
+  auto coefficients = [&]() {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int x = 2 * i, y = x + 1;
+      if (NEIGHBOURS) {
+        const float2 a = cs[i], b = cs[P + i];
+        A0[i] = make_float2(w0[x] * a.x, w0[y] * a.x);
+        A1[i] = make_float2(w1[x] * b.x, w1[y] * b.x);
+        B0[i] = make_float2(w0[y] * -a.y, w0[x] * a.y);
+        B1[i] = make_float2(w1[y] * -b.y, w1[x] * b.y);
+      } else {
+        const float2 a = cs[x], b = cs[y];
+        A0[i] = make_float2(w0[x] * a.x, w0[y] * b.x);
+        A1[i] = make_float2(w1[x] * a.x, w1[y] * b.x);
+        B0[i] = make_float2(w1[x] * -a.y, w1[y] * -b.y);
+        B1[i] = make_float2(w0[x] * a.y, w0[y] * b.y);
+      }
+    }
+  };
+  const float inv_d = 1.f / (float)p.D;
+  // one step's heads (the whole warp comes here together)
+  auto turn = [&](Piece<WORDS>& v0, Piece<WORDS>& v1) {
+    float2 a0[P], a1[P], b0[P], b1[P];
+    unpack<DT>(v0, a0);
+    unpack<DT>(v1, a1);
+    float2 r2 = make_float2(1.f, 1.f);
+    if (p.eps >= 0.f) {
+      float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum = fma2(a1[i], a1[i], fma2(a0[i], a0[i], sum));
+      float s = sum.x + sum.y, r;
+#pragma unroll
+      for (int o = G / 2; o > 0; o >>= 1) s += __shfl_xor_sync(kFullMask, s, o);
+      asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(fmaf(s, inv_d, p.eps)));
+      r2 = make_float2(r, r);
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      b0[i] = NEIGHBOURS ? make_float2(a0[i].y, a0[i].x) : a1[i];
+      b1[i] = NEIGHBOURS ? make_float2(a1[i].y, a1[i].x) : a0[i];
+    }
+    if (p.rot < p.D && !turned) {   // (an infinity would meet a zero)
+#pragma unroll
+      for (int i = 0; i < P; ++i) b0[i] = b1[i] = make_float2(0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      b0[i] = mul2(fma2(a0[i], A0[i], mul2(b0[i], B0[i])), r2);
+      b1[i] = mul2(fma2(a1[i], A1[i], mul2(b1[i], B1[i])), r2);
+    }
+    pack<DT>(b0, v0);
+    pack<DT>(b1, v1);
+  };
+  coefficients();
+  const bool stored = slot >= 0 && slot < (i64)p.n_pages * p.page_size;
+  const i64 page = !stored ? 0 : page_log >= 0 ? slot >> page_log : slot / p.page_size, off = stored ? slot - page * p.page_size : 0;
+  const int last = stored ? n : nq;   // (the others are dropped)
+  Way dst = way(p.q_out, t * p.o_tok, p.o_head, part, p.Hq);
+#pragma unroll 1
+  for (int i = 0, at = 0; i < last; ++i, at = at + 1 < kAhead ? at + 1 : 0) {
+    if (i == nq) {
+      weights(p.k_weight);
+      coefficients();
+      dst = way(p.k_cache, page * p.kc_page + off * p.kc_slot, p.kc_head, from_k, p.Hkv);
+    }
+    if (i == nq + nk) dst = way(p.v_cache, page * p.vc_page + off * p.vc_slot, p.vc_head, from_v, p.Hkv);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+    Piece<WORDS> a, b;
+    a.get(mine_s[at][0][lane]);
+    b.get(mine_s[at][1][lane]);
+    fetch(i + kAhead, at);
+    if (i < nq + nk) turn(a, b);
+    dst.put(a, b);
+    dst.next(heads);
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Every shape: a warp a head, lane l takes elements l, l + 32, ...
@@ -101,6 +343,43 @@ __global__ void __launch_bounds__(kRotThreads) rotate_any_kernel(const specsteer
   }
 }
 
+// Whether rotate_kernel takes a (checked) descriptor in pieces of `bytes`: whole ones everywhere, two a lane, of a pair's halves too, and
+// a head in a warp.
+bool takes_pieces(const specsteer_rotate_append_desc* d, int bytes) {
+  const int n = bytes / (d->dtype == SPECSTEER_F32 ? 4 : 2);
+  if (d->D % (2 * n) || d->D > 64 * n || d->rot % (2 * n)) return false;
+  auto ok = [&](long long stride, long long extent) { return extent <= 1 || stride % n == 0; };
+  auto at = [&](const void* x) { return (uintptr_t)x % bytes == 0; };
+  if (d->Hq > 0 && !(at(d->q) && at(d->q_out) && ok(d->q_tok, d->T) && ok(d->q_head, d->Hq) && ok(d->o_tok, d->T) && ok(d->o_head, d->Hq))) return false;
+  return d->Hkv == 0 || (at(d->k) && at(d->v) && at(d->k_cache) && at(d->v_cache) && ok(d->k_tok, d->T) && ok(d->k_head, d->Hkv) && ok(d->v_tok, d->T) && ok(d->v_head, d->Hkv) &&
+                         ok(d->kc_page, d->n_pages) && ok(d->kc_slot, d->page_size) && ok(d->kc_head, d->Hkv) && ok(d->vc_page, d->n_pages) && ok(d->vc_slot, d->page_size) &&
+                         ok(d->vc_head, d->Hkv));
+}
+
+template <int DT, int WORDS, int G> void launch_as(const specsteer_rotate_append_desc& d, int sm, cudaStream_t s) {
+  // Warps a row: while the rows' warps do not fill the SMs (kRotWarps each) and a warp keeps kAhead steps.
+  const long long steps = ((long long)d.Hq + 2 * d.Hkv) * G / 32;
+  int parts_log = 0, page_log = -1;
+  while (parts_log < 3 && ((long long)d.T << parts_log) < (long long)sm * kRotWarps && steps >= (2 * kAhead) << parts_log) ++parts_log;
+  for (int i = 0; i < 31; ++i)
+    if (d.page_size == 1 << i) page_log = i;
+  const unsigned grid = (unsigned)((((long long)d.T << parts_log) + kRotThreads / 32 - 1) / (kRotThreads / 32));
+  if (d.neighbours) rotate_kernel<DT, WORDS, G, true><<<grid, kRotThreads, 0, s>>>(d, parts_log, page_log);
+  else rotate_kernel<DT, WORDS, G, false><<<grid, kRotThreads, 0, s>>>(d, parts_log, page_log);
+}
+template <int DT, int WORDS> void launch_type(const specsteer_rotate_append_desc& d, int sm, cudaStream_t s) {
+  const int lanes = d.D * Elem<DT>::ES / (8 * WORDS);
+  if (lanes <= 4) launch_as<DT, WORDS, 4>(d, sm, s);
+  else if (lanes <= 8) launch_as<DT, WORDS, 8>(d, sm, s);
+  else if (lanes <= 16) launch_as<DT, WORDS, 16>(d, sm, s);
+  else launch_as<DT, WORDS, 32>(d, sm, s);
+}
+template <int WORDS> void launch_rotate(const specsteer_rotate_append_desc& d, int sm, cudaStream_t s) {
+  if (d.dtype == SPECSTEER_F32) launch_type<SPECSTEER_F32, WORDS>(d, sm, s);
+  else if (d.dtype == SPECSTEER_BF16) launch_type<SPECSTEER_BF16, WORDS>(d, sm, s);
+  else launch_type<SPECSTEER_F16, WORDS>(d, sm, s);
+}
+
 }  // namespace
 }  // namespace specsteer
 
@@ -132,6 +411,12 @@ extern "C" specsteer_status specsteer_rotate_append(const specsteer_rotate_appen
   const int sm = current_sm_count();
   if (sm <= 0) return SPECSTEER_ERR_CUDA;
   cudaStream_t s = (cudaStream_t)cuda_stream;
+  const bool by16 = takes_pieces(d, 16);
+  if (by16 || takes_pieces(d, 8)) {
+    if (by16) launch_rotate<4>(*d, sm, s);
+    else launch_rotate<2>(*d, sm, s);
+    return cudaGetLastError() == cudaSuccess ? SPECSTEER_OK : SPECSTEER_ERR_CUDA;
+  }
   const int grid = d->T < sm * 64 ? d->T : sm * 64;
   if (d->dtype == SPECSTEER_F32) rotate_any_kernel<float><<<grid, kRotThreads, 0, s>>>(*d);
   else if (d->dtype == SPECSTEER_BF16) rotate_any_kernel<__nv_bfloat16><<<grid, kRotThreads, 0, s>>>(*d);
