@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 from typing import Dict, Optional
 
 import torch
@@ -679,8 +680,8 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     _launch((_lib or load_library()).specsteer_cache_append, "specsteer_cache_append", d, dev)
 
 
-def _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after):
-    """(descriptor without a workspace, out, lse, device) of an attention call; the outputs are allocated where there are none."""
+def _attention_args(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after):
+    """(an AttentionDesc's fields up to the workspace, out, lse, device) of an attention call; the outputs are allocated where there are none."""
     shape, e, f, dev, code = _caches(k_cache, v_cache)
     n_pages, page_size, Hkv, D = shape
     want, dtype = q.shape, k_cache.dtype
@@ -698,25 +699,30 @@ def _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, win
     o = _heads(out, want, dtype, dev)
     if lse is None:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-    d = AttentionDesc(B, T, Hq, Hkv, D, page_size, n_pages, width, code, window,
+    args = (B, T, Hq, Hkv, D, page_size, n_pages, width, code, window,
                       1.0 / math.sqrt(D) if scale is None else float(scale), (ATTENTION_GENERIC if generic else 0) | (0 if stop_after is None else stop_after + 1 << 16), ld,
                       a[0], a[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
                       q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table, _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev),
-                      out.data_ptr(), _flat(lse, torch.float32, T * Hq, dev), None if status is None else _flat(status, _I32, B, dev), None, 0)
-    return d, out, lse, dev
+                      out.data_ptr(), _flat(lse, torch.float32, T * Hq, dev), 0 if status is None else _flat(status, _I32, B, dev))
+    return args, out, lse, dev
 
 
 def _workspace(size, d, workspace: Optional[torch.Tensor], x: torch.Tensor, dev: int):
     """Put the caller's workspace into the descriptor, or one from torch's pool, which is returned."""
+    workspace, d.workspace, d.workspace_bytes = _workspace_of(size, d, workspace, x, dev)
+    return workspace
+
+
+def _workspace_of(size, d, workspace: Optional[torch.Tensor], x: torch.Tensor, dev: int):
+    """(the caller's workspace or one from torch's pool, its pointer, its bytes) for a call with descriptor d."""
     if workspace is None:
         need = size(d)
-        if need and dev >= 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-            d.workspace, d.workspace_bytes = workspace.data_ptr(), need
-    else:
-        d.workspace_bytes = workspace.numel()
-        d.workspace = _flat(workspace, torch.uint8, d.workspace_bytes, dev)
-    return workspace
+        if need == 0 or dev < 0:
+            return None, 0, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        return workspace, workspace.data_ptr(), need
+    n = workspace.numel()
+    return workspace, _flat(workspace, torch.uint8, n, dev), n
 
 
 def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
@@ -736,14 +742,47 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         with _on(stream, k_cache):
             return chunk_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, scale=scale, window=window, out=out, lse=lse, status=status,
                                    workspace=workspace, generic=generic, stop_after=stop_after)
-    d, out, lse, dev = _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
-    lib = _lib or load_library()
+    args, out, lse, dev = _attention_args(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
+    lib, d = _lib or load_library(), AttentionDesc(*args)
     keep = _workspace(lib.specsteer_chunk_attention_workspace, d, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
     _launch(lib.specsteer_chunk_attention, "specsteer_chunk_attention", d, dev)
     return out, lse
 
 
 # ---- a round over trees of drafts --------------------------------------------------------------------------------------
+# These calls hand their descriptors over as packed bytes of the structures above: half a microsecond a call where filling in a
+# structure takes two.
+_CODES = {C.c_int32: "i", C.c_uint32: "I", C.c_float: "f", C.c_int64: "q", C.c_void_p: "P"}
+
+
+def _codes(desc) -> str:
+    return "".join(_codes(typ) if issubclass(typ, C.Structure) else _CODES[typ] for _, typ in desc._fields_)
+
+
+class _Packed:
+    """An entry point, and its workspace's size, that take a descriptor as bytes: pack(*fields in order)."""
+
+    def __init__(self, name: str, desc, workspace: Optional[str] = None):
+        self.name, self._workspace, self.pack = "specsteer_" + name, workspace, struct.Struct("@" + _codes(desc)).pack
+        self._fn = self._lib = None
+
+    def bind(self):
+        lib = _lib or load_library()
+        if self._lib is not lib:
+            fn = lib[self.name]               # (a handle of its own, with argument types of its own)
+            fn.argtypes, fn.restype = [C.c_char_p, C.c_void_p], C.c_int
+            if self._workspace:
+                self.size = lib["specsteer_" + self._workspace]
+                self.size.argtypes, self.size.restype = [C.c_char_p], C.c_size_t
+            self._fn, self._lib = fn, lib
+        return self._fn
+
+
+_TREE_PLAN, _ROTATE_APPEND, _TREE_KEEP = _Packed("tree_plan", TreePlanDesc), _Packed("rotate_append", RotateAppendDesc), _Packed("tree_keep", TreeKeepDesc)
+_TREE_ATTENTION = _Packed("tree_attention", TreeAttentionDesc, "chunk_attention_workspace")   # (whose descriptor comes first in its own)
+_TOKEN_LOGPROBS = _Packed("token_logprobs", TokenLogprobsDesc, "token_logprobs_workspace")
+
+
 def tree_plan(parent: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, *, words: int, window: int = 0, out: Optional[Dict[str, torch.Tensor]] = None,
               status: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
     """Ancestors and positions of the rows of trees: parent [T] int32 names each row's parent by its number within the
@@ -762,9 +801,10 @@ def tree_plan(parent: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, 
     mask, ld = _mask(out["mask"], T, dev)
     if out["mask"].shape[1] != words:
         raise ValueError("mask must be [T, words]")
-    d = TreePlanDesc(B, T, words, window, ld, _flat(parent, _I32, T, dev), _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev), mask,
-                     _flat(out["positions"], _I32, T, dev), None if status is None else _flat(status, _I32, B, dev))
-    _launch((_lib or load_library()).specsteer_tree_plan, "specsteer_tree_plan", d, dev)
+    fn = _TREE_PLAN.bind()
+    d = _TREE_PLAN.pack(B, T, words, window, ld, _flat(parent, _I32, T, dev), _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev), mask,
+                        _flat(out["positions"], _I32, T, dev), 0 if status is None else _flat(status, _I32, B, dev))
+    _launch(fn, _TREE_PLAN.name, d, dev)
     return out
 
 
@@ -817,13 +857,14 @@ def rotate_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: 
     w_code = _CACHE_DTYPES.get(w_dtype)
     if w_code is None:
         raise ValueError("weights must be float32, bfloat16 or float16")
-    d = RotateAppendDesc(T, Hq, H, D, 2 * half, n_axes, 1 if neighbours else 0, page_size, n_pages, code, w_code, eps, factor,
-                         a[0], a[1], b[0], b[1], c[0], c[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
-                         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(),
-                         None if q_weight is None else _flat(q_weight, w_dtype, D, dev), None if k_weight is None else _flat(k_weight, w_dtype, D, dev),
-                         _flat(positions, _I32, n_axes * T, dev), _flat(inv_freq, torch.float32, half, dev), None if axis_of is None else _flat(axis_of, _I32, half, dev),
-                         _flat(slot_map, _I64, T, dev), k_cache.data_ptr(), v_cache.data_ptr())
-    _launch((_lib or load_library()).specsteer_rotate_append, "specsteer_rotate_append", d, dev)
+    fn = _ROTATE_APPEND.bind()
+    d = _ROTATE_APPEND.pack(T, Hq, H, D, 2 * half, n_axes, 1 if neighbours else 0, page_size, n_pages, code, w_code, eps, factor,
+                            a[0], a[1], b[0], b[1], c[0], c[1], o[0], o[1], e[0], e[1], e[2], f[0], f[1], f[2],
+                            q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(),
+                            0 if q_weight is None else _flat(q_weight, w_dtype, D, dev), 0 if k_weight is None else _flat(k_weight, w_dtype, D, dev),
+                            _flat(positions, _I32, n_axes * T, dev), _flat(inv_freq, torch.float32, half, dev), 0 if axis_of is None else _flat(axis_of, _I32, half, dev),
+                            _flat(slot_map, _I64, T, dev), k_cache.data_ptr(), v_cache.data_ptr())
+    _launch(fn, _ROTATE_APPEND.name, d, dev)
     return q_out
 
 
@@ -838,16 +879,18 @@ def tree_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
         with _on(stream, k_cache):
             return tree_attention(q, k_cache, v_cache, block_table, cu_new, kv_len, mask, positions=positions, scale=scale, window=window, out=out, lse=lse, status=status,
                                   workspace=workspace, generic=generic, stop_after=stop_after)
-    a, out, lse, dev = _attention_desc(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
-    bits, ld = _mask(mask, a.T, dev)
+    args, out, lse, dev = _attention_args(q, k_cache, v_cache, block_table, cu_new, kv_len, scale, window, out, lse, status, generic, stop_after)
+    T = q.shape[0]
+    bits, ld = _mask(mask, T, dev)
     words = mask.shape[1]
-    _fits(words)
-    if a.window and positions is None:
+    if words > TREE_MAX_ROWS:
+        _fits(words)
+    if window and positions is None:
         raise ValueError("a window needs the rows' positions")
-    lib = _lib or load_library()
-    keep = _workspace(lib.specsteer_chunk_attention_workspace, a, workspace, q, dev)   # noqa: F841  (allocated here: alive until the launch)
-    d = TreeAttentionDesc(a, words, ld, bits, None if positions is None else _flat(positions, _I32, a.T, dev))
-    _launch(lib.specsteer_tree_attention, "specsteer_tree_attention", d, dev)
+    tree = (words, ld, bits, 0 if positions is None else _flat(positions, _I32, T, dev))
+    op, fn = _TREE_ATTENTION, _TREE_ATTENTION.bind()
+    workspace, at, size = _workspace_of(op.size, op.pack(*args, 0, 0, *tree) if workspace is None else None, workspace, q, dev)
+    _launch(fn, op.name, op.pack(*args, at, size, *tree), dev)
     return out, lse
 
 
@@ -876,14 +919,14 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
             out["logprob"] = e(*tokens.shape)
         if top:
             out["top_id"], out["top_logprob"] = e(R, top, dt=_I32), e(R, top)
-    d = TokenLogprobsDesc(R, V, M, top, code, logits.stride(0) if R > 1 else V, M, logits.data_ptr(), None if temperature is None else _flat(temperature, torch.float32, R, dev),
-                          None if tokens is None else _flat(tokens, _I32, R * M, dev), None if tokens is None else _flat(out["logprob"], torch.float32, R * M, dev),
-                          _flat(out["lse"], torch.float32, R, dev), _flat(out["entropy"], torch.float32, R, dev),
-                          _flat(out["top_id"], _I32, R * top, dev) if top else None, _flat(out["top_logprob"], torch.float32, R * top, dev) if top else None,
-                          None if status is None else _flat(status, _I32, R, dev))
-    lib = _lib or load_library()
-    keep = _workspace(lib.specsteer_token_logprobs_workspace, d, workspace, logits, dev)   # noqa: F841
-    _launch(lib.specsteer_token_logprobs, "specsteer_token_logprobs", d, dev)
+    op, fn = _TOKEN_LOGPROBS, _TOKEN_LOGPROBS.bind()
+    args = (R, V, M, top, code, logits.stride(0) if R > 1 else V, M, logits.data_ptr(), 0 if temperature is None else _flat(temperature, torch.float32, R, dev),
+            0 if tokens is None else _flat(tokens, _I32, R * M, dev), 0 if tokens is None else _flat(out["logprob"], torch.float32, R * M, dev),
+            _flat(out["lse"], torch.float32, R, dev), _flat(out["entropy"], torch.float32, R, dev),
+            _flat(out["top_id"], _I32, R * top, dev) if top else 0, _flat(out["top_logprob"], torch.float32, R * top, dev) if top else 0,
+            0 if status is None else _flat(status, _I32, R, dev))
+    workspace, at, size = _workspace_of(op.size, op.pack(*args, 0, 0) if workspace is None else None, workspace, logits, dev)
+    _launch(fn, op.name, op.pack(*args, at, size), dev)
     return out
 
 
@@ -906,7 +949,8 @@ def tree_keep(parent: torch.Tensor, token: torch.Tensor, choice: torch.Tensor, c
         out = {"n_out": torch.empty(B, dtype=_I32, device=parent.device)}
         for name in ("path", "out_tokens"):
             out[name] = torch.empty((B, max_out), dtype=_I32, device=parent.device)
-    d = TreeKeepDesc(B, T, max_out)
+    layers = H = D = page_size = n_pages = width = code = ld = table = 0
+    e = f = (0, 0, 0, 0)
     if k_cache is not None:
         if v_cache is None or block_table is None:
             raise ValueError("the caches come together, with the block table")
@@ -919,17 +963,16 @@ def tree_keep(parent: torch.Tensor, token: torch.Tensor, choice: torch.Tensor, c
         table, rows, width, ld = _table(block_table, dev)
         if rows != B:
             raise ValueError("block_table must have a row a request")
-        _fits(max(max(shape), width))
         if len(shape) == 4:
             shape, e, f = (1, *shape), (0, *e), (0, *f)
-        d = TreeKeepDesc(B, T, max_out, shape[0], shape[3], shape[4], shape[2], shape[1], width, code, ld, e[0], e[1], e[2], e[3], f[0], f[1], f[2], f[3],
-                         block_table=table, k_cache=k_cache.data_ptr(), v_cache=v_cache.data_ptr())
+        layers, n_pages, page_size, H, D = shape
+        _fits(max(layers, n_pages, page_size, H, D, width))
     elif v_cache is not None or block_table is not None:
         raise ValueError("the caches come together, with the block table")
-    d.parent, d.token, d.choice = _flat(parent, _I32, T, dev), _flat(token, _I32, T, dev), _flat(choice, _I32, T, dev)
-    d.cu_new, d.kv_len, d.n_out = _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev), _flat(out["n_out"], _I32, B, dev)
-    d.path, d.out_tokens = _flat(out["path"], _I32, B * max_out, dev), _flat(out["out_tokens"], _I32, B * max_out, dev)
-    if status is not None:
-        d.req_status = _flat(status, _I32, B, dev)
-    _launch((_lib or load_library()).specsteer_tree_keep, "specsteer_tree_keep", d, dev)
+    fn = _TREE_KEEP.bind()
+    d = _TREE_KEEP.pack(B, T, max_out, layers, H, D, page_size, n_pages, width, code, ld, e[0], e[1], e[2], e[3], f[0], f[1], f[2], f[3],
+                        _flat(parent, _I32, T, dev), _flat(token, _I32, T, dev), _flat(choice, _I32, T, dev), _flat(cu_new, _I32, B + 1, dev), _flat(kv_len, _I32, B, dev), table,
+                        0 if k_cache is None else k_cache.data_ptr(), 0 if k_cache is None else v_cache.data_ptr(), _flat(out["n_out"], _I32, B, dev),
+                        _flat(out["path"], _I32, B * max_out, dev), _flat(out["out_tokens"], _I32, B * max_out, dev), 0 if status is None else _flat(status, _I32, B, dev))
+    _launch(fn, _TREE_KEEP.name, d, dev)
     return out

@@ -24,7 +24,7 @@ namespace {
 
 typedef long long i64;
 constexpr int kRotMaxD = SPECSTEER_ROTATE_MAX_D;
-constexpr int kRotThreads = 256;
+constexpr int kRotThreads = 128;
 constexpr int kRotWarps = 16;      // on an SM
 
 __device__ __forceinline__ float load_f32(const float* x) { return *x; }
@@ -105,7 +105,7 @@ template <int DT, int WORDS> __device__ __forceinline__ void pack(const float2 (
   }
 }
 
-constexpr int kAhead = 6;   // steps whose copies a warp has on the way
+constexpr int kAhead = 5;   // steps whose copies a warp has on the way
 // A lane has two pieces of WORDS words.  G: lanes of a head, a power of two that covers it.  2^parts_log warps share a row; page_log:
 // log2 of the page size, or -1.
 template <int DT, int WORDS, int G, bool NEIGHBOURS>
@@ -357,10 +357,12 @@ bool takes_pieces(const specsteer_rotate_append_desc* d, int bytes) {
 }
 
 template <int DT, int WORDS, int G> void launch_as(const specsteer_rotate_append_desc& d, int sm, cudaStream_t s) {
-  // Warps a row: while the rows' warps do not fill the SMs (kRotWarps each) and a warp keeps kAhead steps.
+  // Warps a row: as many as the SMs hold at once (kRotWarps each), since a warp waits more than it computes, and another round of
+  // warps costs more than it shares.  bfloat16, 64 and 2 x 8 heads of 128: 5 rows 4.0 us with 8 warps a row (1: 10.2), 400 rows
+  // 5.4 with 4 (8: 8.0, 1: 10.7), 1283 rows 14.4 with 1 (2: 15.3, 8: 19.3).
   const long long steps = ((long long)d.Hq + 2 * d.Hkv) * G / 32;
   int parts_log = 0, page_log = -1;
-  while (parts_log < 3 && ((long long)d.T << parts_log) < (long long)sm * kRotWarps && steps >= (2 * kAhead) << parts_log) ++parts_log;
+  while (parts_log < 3 && ((long long)d.T << (parts_log + 1)) <= (long long)sm * kRotWarps && steps >= 2 << parts_log) ++parts_log;
   for (int i = 0; i < 31; ++i)
     if (d.page_size == 1 << i) page_log = i;
   const unsigned grid = (unsigned)((((long long)d.T << parts_log) + kRotThreads / 32 - 1) / (kRotThreads / 32));
