@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogPara
   float s = 0.f, w = 0.f;
 #pragma unroll
   for (int i = 0; i < kEndWarps; ++i) { s += sh.red[1][i]; w += sh.red[2][i]; }
-  const float l2s = log2f(s), lse = fmaf(l2s, kLn2, M / temp);
+  const float l2s = log2f(s), ln_s = l2s * kLn2, lse = ln_s + M / temp;
   const bool bad_temp = !(temp > 0.f && temp < -kNegInf);
   const bool bad = bad_temp || !(s > 0.f && s < -kNegInf) || !(fabsf(lse) < -kNegInf);
   // vector u of slot j, counted from the row's first; n_vec or more: there is none
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogPara
     const int token = d.token[r * d.ld_tok + i];
     const bool outside = token < 0 || token >= d.V;
     if (outside && token != -1 && d.row_status) atomicOr(d.row_status + r, SPECSTEER_REQ_BAD_TOKEN);
-    d.logprob[r * d.ld_tok + i] = bad ? nan : outside ? kNegInf : ((L::one(x + token) - M) * c - l2s) * kLn2;
+    d.logprob[r * d.ld_tok + i] = bad ? nan : outside ? kNegInf : (L::one(x + token) - M) / temp - ln_s;
   }
   if (d.n_top == 0) return;
   __syncthreads();
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogPara
   if (tid < d.n_top) {
     const u64 key = sh.out[tid];
     d.top_id[r * d.n_top + tid] = bad ? -1 : (int)(0xffffffffu - (uint32_t)key);
-    d.top_logprob[r * d.n_top + tid] = bad ? nan : ((order_val((uint32_t)(key >> 32)) - M) * c - l2s) * kLn2;
+    d.top_logprob[r * d.n_top + tid] = bad ? nan : (order_val((uint32_t)(key >> 32)) - M) / temp - ln_s;
   }
 }
 

@@ -1,7 +1,7 @@
 // Norm by head, rotation by position, and the keys and values into their slots: what stands between a layer's projections
 // and its attention, in one pass.
 //
-// A block takes a row (token).  Its angles are formed once, in float64, where the product of a position of 2^31 and a frequency keeps 22
+// A block takes a row (token).  Its angles are formed once, in float64, where the product of a position of 2^31 and a frequency keeps 24
 // bits behind the point of a turn, and reduced to a turn before the sine; all heads of the row share them.
 //
 //   rotate_kernel      a warp a row, or several that share its heads where rows are few; no warp waits for another.  A lane has a piece

@@ -174,6 +174,7 @@ extern "C" specsteer_status specsteer_tree_keep(const specsteer_tree_keep_desc* 
   if (d->n_layers > 0) {
     if (d->Hkv <= 0 || d->D <= 0 || d->page_size <= 0 || d->n_pages <= 0 || d->table_width <= 0 || d->ld_table < d->table_width) return SPECSTEER_ERR_INVALID_ARG;
     if (d->dtype != SPECSTEER_F32 && d->dtype != SPECSTEER_BF16 && d->dtype != SPECSTEER_F16) return SPECSTEER_ERR_INVALID_ARG;
+    if ((long long)d->Hkv * d->D > 0x7fffffff) return SPECSTEER_ERR_INVALID_ARG;
     if (d->B > 0 && (!d->block_table || !d->k_cache || !d->v_cache)) return SPECSTEER_ERR_INVALID_ARG;
     es = d->dtype == SPECSTEER_F32 ? 4 : 2;
     const int extent[4] = {d->n_layers, d->n_pages, d->page_size, d->Hkv};
