@@ -553,7 +553,10 @@ __global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogPara
       if (!__any_sync(kFullMask, from < row.n_vec && most >= slot_tau && bound > last)) continue;
       uint4 v[kVecs];
 #pragma unroll
-      for (int u = 0; u < kVecs; ++u) v[u] = from + 32 * u < row.n_vec ? __ldg(vec + from + 32 * u) : make_uint4(0u, 0u, 0u, 0u);
+      for (int u = 0; u < kVecs; ++u) v[u] = from + 32 * u < row.n_vec ? __ldg(vec + from + 32 * u) : make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
+      // (of float32 logits the slots' bounds are rounded up: once more, exactly)
+      const float exact = L::largest(v);
+      if (!__any_sync(kFullMask, exact >= tau && entry_key(exact + 0.f, row.head + (int)from * L::N) > last)) continue;
 #pragma unroll
       for (int u = 0; u < kVecs; ++u) {
         const bool there = from + 32 * u < row.n_vec;
