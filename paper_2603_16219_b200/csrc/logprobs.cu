@@ -341,7 +341,7 @@ struct EndShared {
 
 // Executed once a row, so it is its latency that counts, and that of fetching its instructions: what can be is a short loop.
 template <int DT>
-__global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogParams p) {
+__global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const LogParams p) {
   typedef Logit<DT> L;
   typedef Logit<DT == SPECSTEER_F16 ? SPECSTEER_F16 : SPECSTEER_BF16> S;   // of the slots' maxima
   typedef typename L::type T;
@@ -551,20 +551,24 @@ __global__ void __launch_bounds__(kEndThreads) logprobs_end_kernel(const LogPara
       const float most = S::one(slots + tile * 32 + lane);
       const u64 bound = entry_key(slot_bound<DT>(most) + 0.f, row.head + (int)from * L::N);
       if (!__any_sync(kFullMask, from < row.n_vec && most >= slot_tau && bound > last)) continue;
-      uint4 v[kVecs];
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) v[u] = from + 32 * u < row.n_vec ? __ldg(vec + from + 32 * u) : make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
-      // (of float32 logits the slots' bounds are rounded up: once more, exactly)
-      const float exact = L::largest(v);
-      if (!__any_sync(kFullMask, exact >= tau && entry_key(exact + 0.f, row.head + (int)from * L::N) > last)) continue;
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) {
-        const bool there = from + 32 * u < row.n_vec;
+      constexpr int kPart = kVecs / 2;   // (half a tile at a time: the registers are what the ordinary rows' CTAs of an SM share)
 #pragma unroll 1
-        for (int i = 0; i < L::N; ++i) {
-          const int bit = L::N == 8 ? (i >> 1) + 16 * (i & 1) : i;   // entry i
-          const float y = L::value(v[u], bit);
-          offer(y, row.head + (int)(from + 32 * u) * L::N + i, there && y >= tau);
+      for (i64 at = from; at < from + 32 * kVecs; at += 32 * kPart) {
+        uint4 v[kPart];
+#pragma unroll
+        for (int u = 0; u < kPart; ++u) v[u] = at + 32 * u < row.n_vec ? __ldg(vec + at + 32 * u) : make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
+        // (of float32 logits the slots' bounds are rounded up: once more, exactly)
+        const float exact = L::largest(v);
+        if (!__any_sync(kFullMask, exact >= tau && entry_key(exact + 0.f, row.head + (int)at * L::N) > last)) continue;
+#pragma unroll
+        for (int u = 0; u < kPart; ++u) {
+          const bool there = at + 32 * u < row.n_vec;
+#pragma unroll 1
+          for (int i = 0; i < L::N; ++i) {
+            const int bit = L::N == 8 ? (i >> 1) + 16 * (i & 1) : i;   // entry i
+            const float y = L::value(v[u], bit);
+            offer(y, row.head + (int)(at + 32 * u) * L::N + i, there && y >= tau);
+          }
         }
       }
     }
