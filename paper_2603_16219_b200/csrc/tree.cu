@@ -19,6 +19,7 @@ namespace {
 typedef long long i64;
 constexpr int kMaxRows = SPECSTEER_TREE_MAX_ROWS;
 constexpr int kTreeThreads = 256;
+constexpr int kMoves = 4;          // rows of a path moved together
 
 // Rows [row0, row0 + n) of request b and the tokens cached before them; false when the offsets or lengths make no sense.
 struct TreeRequest { int row0, n, past; };
@@ -94,6 +95,7 @@ template <int BYTES, int ES>
 __global__ void __launch_bounds__(kTreeThreads) tree_keep_kernel(const specsteer_tree_keep_desc p) {
   typedef typename Word<BYTES>::type W;
   __shared__ int next_s[kMaxRows], path_s[kMaxRows];
+  __shared__ int4 move_s[kMaxRows];   // page and place a row of the path comes from, page (-1: it stays) and place it goes to
   __shared__ int len_s;
   const int tid = threadIdx.x, b = blockIdx.x;
   const bool first = blockIdx.y == 0;
@@ -126,6 +128,19 @@ __global__ void __launch_bounds__(kTreeThreads) tree_keep_kernel(const specsteer
       if (!ok && p.req_status) atomicOr(p.req_status + b, SPECSTEER_REQ_BAD_LEN);
     }
   }
+  if (p.n_layers == 0 || len < 2) return;
+  for (int i = 1 + tid; i < len; i += kTreeThreads) {
+    int4 m = make_int4(0, 0, -1, 0);
+    if (path_s[i] != i) {
+      const int from = rq.past + path_s[i], to = rq.past + i;
+      const int* table = p.block_table + (i64)b * p.ld_table;
+      const int pf = table[from / p.page_size], pt = table[to / p.page_size];
+      if (pf >= 0 && pf < p.n_pages && pt >= 0 && pt < p.n_pages) m = make_int4(pf, from % p.page_size, pt, to % p.page_size);
+      else if (first && p.req_status) atomicOr(p.req_status + b, SPECSTEER_REQ_BAD_PAGE);
+    }
+    move_s[i] = m;
+  }
+  __syncthreads();
   const int per_head = p.D * ES / BYTES;
   const i64 columns = (i64)p.n_layers * p.Hkv * per_head;
   for (i64 c = (i64)blockIdx.y * kTreeThreads + tid; c < columns; c += (i64)gridDim.y * kTreeThreads) {
@@ -133,18 +148,23 @@ __global__ void __launch_bounds__(kTreeThreads) tree_keep_kernel(const specsteer
     const int h = (int)(c / per_head % p.Hkv), layer = (int)(c / per_head / p.Hkv);
     char* kc = (char*)p.k_cache + (layer * p.kc_layer + h * p.kc_head + e) * ES;
     char* vc = (char*)p.v_cache + (layer * p.vc_layer + h * p.vc_head + e) * ES;
-    for (int i = 1; i < len; ++i) {
-      if (path_s[i] == i) continue;
-      const int from = rq.past + path_s[i], to = rq.past + i;
-      const int* table = p.block_table + (i64)b * p.ld_table;
-      const int pf = table[from / p.page_size], pt = table[to / p.page_size];
-      if (pf < 0 || pf >= p.n_pages || pt < 0 || pt >= p.n_pages) {
-        if (c == 0 && p.req_status) atomicOr(p.req_status + b, SPECSTEER_REQ_BAD_PAGE);
-        continue;
+    // kMoves rows' loads together: what a row's place is read for, if at all, is a row before it
+    for (int i0 = 1; i0 < len; i0 += kMoves) {
+      W k[kMoves], v[kMoves];
+#pragma unroll
+      for (int j = 0; j < kMoves; ++j) {
+        const int4 m = i0 + j < len ? move_s[i0 + j] : make_int4(0, 0, -1, 0);
+        if (m.z < 0) continue;
+        k[j] = *(const W*)(kc + (m.x * p.kc_page + m.y * p.kc_slot) * ES);
+        v[j] = *(const W*)(vc + (m.x * p.vc_page + m.y * p.vc_slot) * ES);
       }
-      const i64 of = from % p.page_size, ot = to % p.page_size;
-      *(W*)(kc + (pt * p.kc_page + ot * p.kc_slot) * ES) = *(const W*)(kc + (pf * p.kc_page + of * p.kc_slot) * ES);
-      *(W*)(vc + (pt * p.vc_page + ot * p.vc_slot) * ES) = *(const W*)(vc + (pf * p.vc_page + of * p.vc_slot) * ES);
+#pragma unroll
+      for (int j = 0; j < kMoves; ++j) {
+        const int4 m = i0 + j < len ? move_s[i0 + j] : make_int4(0, 0, -1, 0);
+        if (m.z < 0) continue;
+        *(W*)(kc + (m.z * p.kc_page + m.w * p.kc_slot) * ES) = k[j];
+        *(W*)(vc + (m.z * p.vc_page + m.w * p.vc_slot) * ES) = v[j];
+      }
     }
   }
 }
