@@ -333,7 +333,9 @@ __device__ __forceinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
 // The cut weighs a unit by its key tiles, twice as much with two query tiles, and a constant for its beginning and end
 // (queries, first scores, result).  Of the constants from 0 to 24 these were the fastest: with 0 / 8 / 14 in place of 4 a
 // batch of 64 single tokens takes 121 / 85 / 93 us instead of 80, four prompt chunks with 4 in place of 6 309 us instead of 287.
-__device__ __forceinline__ int unit_base(bool two) { return two ? 6 : 4; }
+// Trees end in blocks whose rows look their keys up, and their units are short: 64 trees of 15 to 32 rows over up to 4000 keys take 171 us
+// with 6 for both, 177 with 4 / 6, 187 with 2 / 4, 174 with 8 / 12.
+template <bool TREE> __device__ __forceinline__ int unit_base(bool two) { return TREE || two ? 6 : 4; }
 
 // TREE here and below: rows of trees of drafts, which see the cached keys before the chunk and, of the chunk's own, those of their
 // mask.  What depends on it are the spans of a unit, taken as wide as any row's, and the keys that a row keeps in a block at the edge.
@@ -347,6 +349,7 @@ struct Unit {
   bool two;                // two query tiles
   int hi_first, hi_last;   // keys the first / last row sees end here
   int lo_first, lo_last;   // and begin here
+  int base;                // see unit_base
   int t0, nt;              // first key tile, key tiles (at least one, so that a unit that sees nothing is written too)
 };
 template <bool TREE> __device__ __forceinline__ Unit make_unit(const TcParams& p, const AttnRequest& rq, int u) {
@@ -354,6 +357,7 @@ template <bool TREE> __device__ __forceinline__ Unit make_unit(const TcParams& p
   x.tok0 = u * 2 * p.tile_tok;
   x.tok1 = min(rq.n, x.tok0 + 2 * p.tile_tok);
   x.two = x.tok1 - x.tok0 > p.tile_tok;
+  x.base = unit_base<TREE>(x.two);
   if constexpr (TREE) {
     const int past = rq.kv - rq.n;
     x.lo_first = tree_lo(p.d, past);                  // of a row as near as the root
@@ -368,11 +372,10 @@ template <bool TREE> __device__ __forceinline__ Unit make_unit(const TcParams& p
   x.nt = max(1, (max(x.hi_last, 0) + kKeys - 1) / kKeys - x.t0);
   return x;
 }
-__device__ __forceinline__ long long unit_cost(const Unit& x) { return (long long)x.nt * (x.two ? 2 : 1) + unit_base(x.two); }
+__device__ __forceinline__ long long unit_cost(const Unit& x) { return (long long)x.nt * (x.two ? 2 : 1) + x.base; }
 // The key tile at which a cut `pos` into the unit falls.
 __device__ __forceinline__ int cut_tile(const Unit& x, long long pos) {
-  const int base = unit_base(x.two);
-  return pos <= base ? 0 : (int)min((long long)x.nt, (pos - base) >> (x.two ? 1 : 0));
+  return pos <= x.base ? 0 : (int)min((long long)x.nt, (pos - x.base) >> (x.two ? 1 : 0));
 }
 __device__ __forceinline__ int n_units(const TcParams& p, const AttnRequest& rq) { return (rq.n + 2 * p.tile_tok - 1) / (2 * p.tile_tok); }
 template <bool TREE> __device__ __forceinline__ long long head_cost(const TcParams& p, const AttnRequest& rq) {
