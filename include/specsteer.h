@@ -521,7 +521,7 @@ enum { SPECSTEER_REQ_BAD_PARENT = 1024 /* a row's parent is not a row before it 
  * |A(i)| - 1 and past = kv_len - n:
  *   mask[row] bit j (word j/32, bit j mod 32) = j in A(i), and with window > 0 only if depth(i) - depth(j) < window
  *   positions[row] = past + depth(i)
- * Rows behind the last request's (cu_new[B] <= row < T) get no bits and -1.  A request with more rows than 32 * mask_words or
+ * Rows below T behind cu_new[B] and behind every accepted request get no bits and -1.  A request with more rows than 32 * mask_words or
  * SPECSTEER_TREE_MAX_ROWS gets BAD_LEN and the same; one whose offsets or lengths make no sense (cu_new outside [0, T] or decreasing,
  * kv_len < n) BAD_LEN, and nothing of it is written.  positions may be NULL; req_status may be NULL, bits are OR-ed into it.
  * 1 <= mask_words <= SPECSTEER_TREE_MAX_ROWS / 32; ld_mask >= mask_words, in words.  Errors: INVALID_ARG, CUDA. */
@@ -620,7 +620,8 @@ size_t specsteer_token_logprobs_workspace(const specsteer_token_logprobs_desc *d
 /* The end of a round over trees.  token[row] is a row's token, choice[row] the one that the model emits behind it (its likeliest,
  * or one sampled from its probabilities: then the emitted tokens follow the model's law).  Per request:
  *   path[0] = 0;   path[i+1] = the lowest row whose parent is path[i] and whose token is choice[path[i]], while there is one
- *   and i + 1 < max_out;   n_out = the length of the path (0 when the request has no rows)
+ *   and i + 1 < max_out (a negative choice, as specsteer_token_logprobs has it for rows without probabilities, is nobody's token);
+ *   n_out = the length of the path (0 when the request has no rows)
  *   out_tokens[i] = choice[path[i]]: what the round emits; the last of them is the next root
  * and behind them path and out_tokens hold -1.  The keys and values of row path[i] go to the place of row i, in each of n_layers
  * caches: the cache then holds past + n_out tokens of the request, and n_out is the next specsteer_cache_plan's advance.

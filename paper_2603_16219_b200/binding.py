@@ -908,6 +908,8 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     if logits.dim() != 2 or code is None or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [R, V] float32, bfloat16 or float16 with a contiguous last axis")
     R, V = logits.shape
+    if tokens is not None and tokens.dim() not in (1, 2):
+        raise ValueError("tokens must be [R] or [R, M]")
     M = 0 if tokens is None else 1 if tokens.dim() == 1 else tokens.shape[1]
     _fits(max(R, V, M, top), top)
     if not 0 <= top <= min(V, TOP_MAX):

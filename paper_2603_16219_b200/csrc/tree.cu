@@ -36,9 +36,18 @@ __global__ void __launch_bounds__(kTreeThreads) tree_plan_kernel(const specsteer
   __shared__ int parent_s[kMaxRows];
   const int tid = threadIdx.x;
   if ((int)blockIdx.x >= p.B) {   // rows behind the last request's
-    const int end = p.cu_new[p.B];
-    const i64 first = end < 0 ? 0 : end, step = (i64)(gridDim.x - p.B) * kTreeThreads;
-    for (i64 t = first + (i64)(blockIdx.x - p.B) * kTreeThreads + tid; t < p.T; t += step) {
+    __shared__ int end_s[kTreeThreads / 32];
+    int end = max(0, p.cu_new[p.B]);
+    for (int b = tid; b < p.B; b += kTreeThreads) {   // (offsets that go down: behind every request that is accepted)
+      TreeRequest rq;
+      if (tree_request(p.cu_new, p.kv_len, p.T, b, &rq)) end = max(end, rq.row0 + rq.n);
+    }
+    end = __reduce_max_sync(kFullMask, end);
+    if ((tid & 31) == 0) end_s[tid >> 5] = end;
+    __syncthreads();
+    for (int w = 0; w < kTreeThreads / 32; ++w) end = max(end, end_s[w]);
+    const i64 step = (i64)(gridDim.x - p.B) * kTreeThreads;
+    for (i64 t = end + (i64)(blockIdx.x - p.B) * kTreeThreads + tid; t < p.T; t += step) {
       for (int w = 0; w < p.mask_words; ++w) p.mask[t * p.ld_mask + w] = 0u;
       if (p.positions) p.positions[t] = -1;
     }
@@ -107,7 +116,9 @@ __global__ void __launch_bounds__(kTreeThreads) tree_keep_kernel(const specsteer
   __syncthreads();
   for (int i = tid; i < rq.n; i += kTreeThreads) {
     const int j = p.parent[rq.row0 + i];
-    if (j >= 0 && j < i && p.token[rq.row0 + i] == p.choice[rq.row0 + j]) atomicMin(next_s + j, i);   // the lowest, whoever comes first
+    if (j < 0 || j >= i) continue;
+    const int choice = p.choice[rq.row0 + j];
+    if (choice >= 0 && p.token[rq.row0 + i] == choice) atomicMin(next_s + j, i);   // the lowest, whoever comes first
   }
   __syncthreads();
   if (tid == 0) {

@@ -31,7 +31,8 @@ def plan_reference(parent, cu, kv, T, words, window=0):
     """(mask, positions, status): what is not written is None in positions."""
     mask = np.zeros((T, words), np.int64)
     pos, status = [None] * T, [0] * len(kv)
-    for t in range(max(0, cu[-1]), T):
+    accepted = [cu[b + 1] for b in range(len(kv)) if 0 <= cu[b] <= cu[b + 1] <= T and kv[b] >= cu[b + 1] - cu[b]]
+    for t in range(max([0, cu[-1]] + accepted), T):
         pos[t] = -1
     for b in range(len(kv)):
         n = cu[b + 1] - cu[b]
@@ -185,7 +186,7 @@ def keep_reference(parent, token, choice, cu, kv, T, max_out, table=None, page=0
         if not bad and n > 0:
             way = [0]
             while len(way) < max_out:
-                kids = [i for i in range(way[-1] + 1, n) if parent[cu[b] + i] == way[-1] and token[cu[b] + i] == choice[cu[b] + way[-1]]]
+                kids = [i for i in range(way[-1] + 1, n) if parent[cu[b] + i] == way[-1] and token[cu[b] + i] == choice[cu[b] + way[-1]] >= 0]
                 if not kids:
                     break
                 way.append(kids[0])

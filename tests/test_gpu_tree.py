@@ -67,7 +67,7 @@ def test_plan_refusals_are_per_request(binding):
     _check_plan(binding, parent, cu, kv, T, 1)           # the second and fifth do not fit one word
     parent[2], parent[cu[5] + 3], parent[cu[5] + 4], parent[cu[1]] = 2, 2 ** 31 - 1, -2, -2 ** 31
     _check_plan(binding, parent, cu, kv, T, 2)
-    for bad in ([0, 5, 3, 45, 51, 84, 91], [-1, 5, 45, 45, 51, 84, 91], [0, 5, 45, 45, 51, 84, T + 1]):
+    for bad in ([0, 5, 3, 45, 51, 84, 91], [-1, 5, 45, 45, 51, 84, 91], [0, 5, 45, 45, 51, 84, T + 1], [0, 5, 45, 45, 51, 84, -7], [0, 5, 45, 45, 51, 84, 46]):
         _check_plan(binding, parent, bad, kv, T, 2)
     big = _tree.random_parents(rng, 1025)
     _check_plan(binding, big, [0, 1025], [2000], 1025, 32)
@@ -676,6 +676,12 @@ def test_keep_long_paths(binding, seed):
 def test_keep_takes_the_lowest_of_equal_siblings(binding):
     got = binding.tree_keep(i32([-1, 0, 0, 1, 2]), i32([9, 4, 4, 5, 5]), i32([4, 5, 5, 6, 7]), i32([0, 5]), i32([5]), max_out=4)
     assert got["path"].tolist() == [[0, 1, 3, -1]] and got["out_tokens"].tolist() == [[4, 5, 6, -1]] and got["n_out"].tolist() == [3]
+
+
+def test_keep_negative_choices_are_nobodys_token(binding):
+    """Rows without probabilities choose -1, which a padded draft's token of -1 must not confirm."""
+    got = binding.tree_keep(i32([-1, 0, 1, -1, 0]), i32([3, -1, -1, 2, 8]), i32([-1, -1, -1, 8, -5]), i32([0, 3, 5]), i32([3, 2]), max_out=4)
+    assert got["path"].tolist() == [[0, -1, -1, -1], [0, 1, -1, -1]] and got["out_tokens"].tolist() == [[-1, -1, -1, -1], [8, -5, -1, -1]] and got["n_out"].tolist() == [1, 2]
 
 
 def test_keep_refuses_requests(binding):

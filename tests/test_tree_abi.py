@@ -179,7 +179,7 @@ def test_binding_checks_tensors(binding):
         rot(q, k, k, pos, fr, kc, kc, slot)
     lg, tok = torch.zeros(3, 50), torch.zeros(3, dtype=i32)
     lp = binding.token_logprobs
-    for call in (lambda: lp(lg[0]), lambda: lp(lg.double()), lambda: lp(lg.t()), lambda: lp(lg, tok[:2]), lambda: lp(lg, tok.long()), lambda: lp(lg, top=33), lambda: lp(lg, top=-1),
+    for call in (lambda: lp(lg[0]), lambda: lp(lg.double()), lambda: lp(lg.t()), lambda: lp(lg, tok[:2]), lambda: lp(lg, tok.long()), lambda: lp(lg, tok[0]), lambda: lp(lg, tok.view(3, 1, 1)), lambda: lp(lg, top=33), lambda: lp(lg, top=-1),
                  lambda: lp(lg[:, :4], top=5), lambda: lp(lg, temperature=torch.zeros(2)), lambda: lp(lg, status=torch.zeros(3))):
         with pytest.raises(ValueError):
             call()
