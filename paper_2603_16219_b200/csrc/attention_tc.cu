@@ -36,6 +36,11 @@
 //   64 single tokens, up to 4000 keys, 32 heads of 64, float16         81 to 87 us, 3.0 to 3.2 TB/s (78): the few rows of a request
 //     sit in one warp of each stream, whose 2000 clocks a block of 64 keys (1500 of arithmetic and tensor-memory latency,
 //     500 of handshakes) bound it
+// and of trees (specsteer_tree_attention):
+//   64 trees of 15 to 32 rows, up to 4000 keys, 64 heads               171 to 196 us (168 to 187), 0.52 to 0.6 PFLOP/s of useful products: two query
+//     tiles, the second of which is rarely full; bound as the prompt is
+//   2 trees of 49 to 63 rows, 30 to 120 thousand keys, 32 heads        171 to 196 us (166 to 174), 0.75 to 0.9 PFLOP/s
+//   48 trees of up to 25 rows, 32 heads of 64, window 1024, float16    43 to 45 us: ends of pieces
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
