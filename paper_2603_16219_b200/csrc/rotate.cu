@@ -108,7 +108,7 @@ template <int DT, int WORDS> __device__ __forceinline__ void pack(const float2 (
   }
 }
 
-constexpr int kAhead = 5;   // steps whose copies a warp has on the way
+constexpr int kAhead = 4;   // steps whose copies a warp has on the way
 // A lane has two pieces of WORDS words.  G: lanes of a head, a power of two that covers it.  2^parts_log warps share a row; page_log:
 // log2 of the page size, or -1.
 template <int DT, int WORDS, int G, bool NEIGHBOURS>
