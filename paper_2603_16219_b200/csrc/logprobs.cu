@@ -24,6 +24,7 @@
 // issue of 7 instructions an entry come up to it, and pass it at the clocks the power limit leaves.  Eight vectors a lane (two tiles, one
 // ahead, are all the registers of 16 warps an SM) beat four with 24 or 32 warps: 65 us, 72 and 74 without likeliest tokens.
 // A CTA a row that ends it too took 95 us for the sums alone and 140 with 20 tokens: nothing is loaded while a row ends.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -40,6 +41,8 @@ constexpr int kThreads = 256, kCtas = 2;   // of the streaming kernel, on an SM
 constexpr int kVecs = 8;                   // vectors of 16 bytes that a lane has of a tile
 constexpr int kTileVecs = 32 * kVecs;      // of a tile: 4 KB, a warp's step
 constexpr int kEndThreads = 128, kEndWarps = kEndThreads / 32;
+// Few rows: CTAs of a row (a cluster) and their warps; the rows and tiles of a row up to which they are taken.
+constexpr int kFewCtas = 8, kFewWarps = kFewCtas * kEndWarps, kFewRows = 37, kFewTiles = 128;
 constexpr int kPicked = 512;               // slots and entries that the quick selection takes
 constexpr int kMaxSms = 148;                // the workspace is laid out for as many
 constexpr float kSlack = 8.f;        // how far l may be above the reference
@@ -269,16 +272,28 @@ __device__ __forceinline__ uint4 load_once(const uint4* at, uint64_t policy) {
   return v;
 }
 
+// This lane's part of a tile.
+template <int DT> __device__ __forceinline__ void load_tile(const Row<DT>& row, int tile, int lane, uint64_t policy, uint4 (&to)[kVecs]) {
+  typedef Logit<DT> L;
+  const uint4* at = reinterpret_cast<const uint4*>(row.x + row.head) + (i64)tile * kTileVecs + lane;
+  const int left = row.n_vec - tile * kTileVecs - lane;
+  if (left > 32 * (kVecs - 1)) {
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) to[u] = load_once(at + 32 * u, policy);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) to[u] = 32 * u < left ? load_once(at + 32 * u, policy) : make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
+  }
+}
+
 template <int DT>
 __global__ void __launch_bounds__(kThreads, kCtas) logprobs_stream_kernel(const LogParams p) {
-  typedef Logit<DT> L;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
   const i64 w = (i64)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), total = (i64)p.d.R * p.tiles;
   if (w >= p.warps) return;
   const i64 first = divide(total * w, p.warps, p.warp_inv), end = divide(total * (w + 1), p.warps, p.warp_inv);
   if (first >= end) return;
-  const uint4 none = make_uint4(L::kNone, L::kNone, L::kNone, L::kNone);
   const uint64_t policy = l2_policy_evict_first();
   i64 r = divide(first, p.tiles, p.tile_inv);
   int tile = (int)(first - r * p.tiles);
@@ -288,18 +303,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logprobs_stream_kernel(const 
   Row<DT> row(p.d, r);
   float c = 0.f, next_c = kLog2e / (p.d.temperature ? p.d.temperature[r] : 1.f);
   uint4 v[kVecs], next[kVecs];
-  auto load = [&](uint4 (&to)[kVecs]) {
-    const uint4* at = reinterpret_cast<const uint4*>(row.x + row.head) + (i64)next_tile * kTileVecs + lane;
-    const int left = row.n_vec - next_tile * kTileVecs - lane;
-    if (left > 32 * (kVecs - 1)) {
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) to[u] = load_once(at + 32 * u, policy);
-    } else {
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) to[u] = 32 * u < left ? load_once(at + 32 * u, policy) : none;
-    }
-  };
-  load(v);
+  load_tile(row, tile, lane, policy, v);
   Sums a{kNegInf, 0.f, 0.f};
   float top = kNegInf;
   c = next_c;
@@ -312,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logprobs_stream_kernel(const 
         row = Row<DT>(p.d, ++next_r);
         next_c = kLog2e / (p.d.temperature ? p.d.temperature[next_r] : 1.f);
       }
-      load(next);
+      load_tile(row, next_tile, lane, policy, next);
     }
     const float mx = take<DT>(a, v, c);
     top = fmaxf(top, mx);
@@ -349,17 +353,16 @@ struct EndShared {
   u64 out[32];                     // the likeliest, in order
 };
 
+// Row r's end, by kEndThreads threads, from its records (n of them from `record` on) and slots; wait() returns once those are there.
 // Executed once a row, so it is its latency that counts, and that of fetching its instructions: what can be is a short loop.
-template <int DT>
-__global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const LogParams p) {
+template <int DT, typename Wait>
+__device__ __forceinline__ void end_row(const LogParams& p, i64 r, EndShared& sh, const float4* record, int n_record, const uint16_t* slot_max, Wait&& wait) {
   typedef Logit<DT> L;
   typedef Logit<DT == SPECSTEER_F16 ? SPECSTEER_F16 : SPECSTEER_BF16> S;   // of the slots' maxima
   typedef typename L::type T;
-  __shared__ EndShared sh;
   const specsteer_token_logprobs_desc& d = p.d;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float nan = __int_as_float(0x7fc00000);
-  const i64 r = blockIdx.x;
   const Row<DT> row(d, r);
   const T* x = row.x;
   const float temp = d.temperature ? d.temperature[r] : 1.f, c = kLog2e / temp;
@@ -371,12 +374,19 @@ __global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const Log
     single_at = tid < row.head ? tid : d.V - rest + (tid - row.head);
     single = L::one(x + single_at);
   }
-  const i64 w0 = p.tiles > 0 ? warp_of(p, r * p.tiles) : 0, w1 = p.tiles > 0 ? warp_of(p, (r + 1) * p.tiles - 1) : -1;
+  // the first of the given tokens
+  auto logit_of = [&](int i, int* token) {
+    *token = d.token[r * d.ld_tok + i];
+    return *token >= 0 && *token < d.V ? L::one(x + *token) : 0.f;
+  };
+  int token = -1;
+  float given = 0.f;
+  if (tid < d.n_tokens) given = logit_of(tid, &token);
   if (tid == 0) sh.n_slots = sh.n_keys = 0;
-  pdl_wait();
+  wait();
   // ---- the slots' maxima: vectors, kHeld a thread at a time; the last ones stay in registers
   const int n_slot = p.tiles * 32, n_max = d.n_top > 0 ? n_slot / S::N : 0;
-  const typename S::type* slots = (const typename S::type*)p.slot_max + r * n_slot;
+  const typename S::type* slots = (const typename S::type*)slot_max;
   const uint4* maxima = reinterpret_cast<const uint4*>(slots);
   constexpr int kHeld = 4;
   const uint4 none = make_uint4(S::kNone, S::kNone, S::kNone, S::kNone);
@@ -386,15 +396,15 @@ __global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const Log
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       const int j = base + mine + k * kEndThreads;
-      held[k] = j < n_max ? __ldcg(maxima + j) : none;
+      held[k] = j < n_max ? maxima[j] : none;
     }
   };
   hold(0);
   // ---- the row's records
   Sums a{kNegInf, 0.f, 0.f};
 #pragma unroll 1
-  for (i64 w = w0 + tid; w <= w1; w += kEndThreads) {
-    const float4 q = __ldcg(p.record + r + w);
+  for (int w = tid; w < n_record; w += kEndThreads) {
+    const float4 q = record[w];
     const float M = fmaxf(a.ref, q.x);
     rescale(a, M, c);
     Sums b{q.x, q.y, q.z};
@@ -522,10 +532,10 @@ __global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const Log
   }
 #pragma unroll 1
   for (int i = tid; i < d.n_tokens; i += kEndThreads) {
-    const int token = d.token[r * d.ld_tok + i];
+    if (i != tid) given = logit_of(i, &token);
     const bool outside = token < 0 || token >= d.V;
     if (outside && token != -1 && d.row_status) atomicOr(d.row_status + r, SPECSTEER_REQ_BAD_TOKEN);
-    d.logprob[r * d.ld_tok + i] = bad ? nan : outside ? kNegInf : (L::one(x + token) - M) / temp - ln_s;
+    d.logprob[r * d.ld_tok + i] = bad ? nan : outside ? kNegInf : (given - M) / temp - ln_s;
   }
   if (d.n_top == 0) return;
   __syncthreads();
@@ -599,11 +609,60 @@ __global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const Log
   }
 }
 
-struct LogPlan { int tiles, grid; long long warps; size_t record_bytes, max_bytes; };
+template <int DT>
+__global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const LogParams p) {
+  __shared__ EndShared sh;
+  const i64 r = blockIdx.x;
+  const i64 w0 = p.tiles > 0 ? warp_of(p, r * p.tiles) : 0, w1 = p.tiles > 0 ? warp_of(p, (r + 1) * p.tiles - 1) : -1;
+  end_row<DT>(p, r, sh, p.record + r + w0, (int)(w1 - w0 + 1), p.slot_max + r * p.tiles * 32, [] { pdl_wait(); });
+}
+
+// Few rows of few tiles: a cluster reads a row, leaves records and slots in its first CTA's shared memory, and that one ends it.
+template <int DT>
+__global__ void __launch_bounds__(kEndThreads) logprobs_few_kernel(const LogParams p) {
+  __shared__ EndShared sh;
+  __shared__ __align__(16) uint16_t slot_s[kFewTiles * 32];
+  __shared__ float4 record_s[kFewWarps];
+  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int rank = (int)cluster.block_rank(), lane = threadIdx.x & 31, w = rank * kEndWarps + (threadIdx.x >> 5);
+  const i64 r = blockIdx.x / kFewCtas;
+  const Row<DT> row(p.d, r);
+  const float c = kLog2e / (p.d.temperature ? p.d.temperature[r] : 1.f);
+  const int first = p.tiles * w / kFewWarps, end = p.tiles * (w + 1) / kFewWarps;
+  const uint64_t policy = l2_policy_evict_first();
+  uint4 v[kVecs];
+  if (first < end) load_tile(row, first, lane, policy, v);
+  uint16_t* slots = cluster.map_shared_rank(slot_s, 0);
+  float4* records = cluster.map_shared_rank(record_s, 0);
+  cluster.sync();   // the first CTA is there
+  Sums a{kNegInf, 0.f, 0.f};
+  float top = kNegInf;
+#pragma unroll 1
+  for (int tile = first; tile < end; ++tile) {
+    uint4 next[kVecs];
+    if (tile + 1 < end) load_tile(row, tile + 1, lane, policy, next);
+    const float mx = take<DT>(a, v, c);
+    top = fmaxf(top, mx);
+    slots[tile * 32 + lane] = slot_bits<DT>(mx);
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) v[u] = next[u];
+  }
+  const float M = warp_max(top);
+  rescale(a, M == kNegInf ? 0.f : M, c);
+  const float s = warp_sum(a.s), ww = warp_sum(a.w);
+  if (lane == 0) records[w] = make_float4(M, s, ww, 0.f);
+  auto all_written = [&] { cluster.sync(); };   // (nobody reads another's memory from there on)
+  if (rank == 0) end_row<DT>(p, r, sh, record_s, kFewWarps, slot_s, all_written);
+  else all_written();
+}
+
+struct LogPlan { int tiles, grid; bool few; long long warps; size_t record_bytes, max_bytes; };
 LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
   LogPlan q;
   const int es = d->dtype == SPECSTEER_F32 ? 4 : 2;
   q.tiles = (int)(((long long)d->V * es / 16 + kTileVecs - 1) / kTileVecs);
+  // One launch, and no workspace, for up to two CTAs an SM and four tiles a warp (kFewRows, kFewTiles): see kFewCtas.
+  q.few = d->R <= kFewRows && q.tiles <= kFewTiles;
   const long long total = (long long)d->R * q.tiles, most = (long long)sm * kCtas * (kThreads / 32);
   q.warps = total < most ? total : most;
   q.grid = (int)((q.warps + kThreads / 32 - 1) / (kThreads / 32));
@@ -613,6 +672,19 @@ LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
 }
 
 template <int DT> cudaError_t launch(const LogParams& p, const LogPlan& q, cudaStream_t s) {
+  if (q.few) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.d.R * kFewCtas);
+    cfg.blockDim = dim3(kEndThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kFewCtas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, logprobs_few_kernel<DT>, p);
+  }
   if (q.grid > 0) {
     logprobs_stream_kernel<DT><<<q.grid, kThreads, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
@@ -646,13 +718,14 @@ using namespace specsteer;
 extern "C" size_t specsteer_token_logprobs_workspace(const specsteer_token_logprobs_desc* d) {
   if (check_logprobs(d) != SPECSTEER_OK || d->R == 0) return 0;
   const LogPlan q = plan_of(d, kMaxSms);
-  return q.record_bytes + q.max_bytes;
+  return q.few ? 0 : q.record_bytes + q.max_bytes;
 }
 
 extern "C" specsteer_status specsteer_token_logprobs(const specsteer_token_logprobs_desc* d, void* cuda_stream) {
   const specsteer_status st = check_logprobs(d);
   if (st != SPECSTEER_OK || d->R == 0) return st;
-  if (!d->workspace || ((uintptr_t)d->workspace & 31u) || d->workspace_bytes < (long long)specsteer_token_logprobs_workspace(d)) return SPECSTEER_ERR_WORKSPACE;
+  const size_t need = specsteer_token_logprobs_workspace(d);
+  if (need > 0 && (!d->workspace || ((uintptr_t)d->workspace & 31u) || d->workspace_bytes < (long long)need)) return SPECSTEER_ERR_WORKSPACE;
   const int sm = current_sm_count();
   if (sm <= 0) return SPECSTEER_ERR_CUDA;
   const LogPlan q = plan_of(d, sm < kMaxSms ? sm : kMaxSms);
