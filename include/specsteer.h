@@ -594,7 +594,8 @@ specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc *d
  * A token outside [0, V) has logprob -inf, and BAD_TOKEN is set unless it is -1 (no token).  A row that holds NaN or +inf, or nothing
  * but -inf, or whose lse is no finite float32, gets NaN everywhere, ids of -1, and NONFINITE; so does one whose temperature is not
  * positive and finite, with BAD_PARAM.  lse and entropy may be NULL; so may row_status,
- * into which bits are OR-ed.  Sums in float32, one read of the logits.  Equal inputs give equal bits.
+ * into which bits are OR-ed.  Sums in float32, one read of the logits.  The same call gives the same bits
+ * (equal rows of a call need not: their sums may be cut at different places).
  * R, n_tokens >= 0; 1 <= V; 0 <= n_top <= min(V, SPECSTEER_TOP_MAX); ld_row >= V.  dtype F32, BF16 or F16.  Any alignment is taken,
  * and rows of any length.  workspace: 32-byte aligned device memory of at least specsteer_token_logprobs_workspace(desc) bytes, whose content
  * before and after the call means nothing; calls that may overlap need one each.  Errors: INVALID_ARG, WORKSPACE, CUDA. */

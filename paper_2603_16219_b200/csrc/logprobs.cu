@@ -19,7 +19,7 @@
 //   1280 rows of 151 936, bfloat16, tempered, top 20    76 us (60), 82 to 88 in a loop of a second; without likeliest tokens 64 us
 //   640 rows of 151 936, float32, top 20                69 us (60); without 61 us, 6.3 TB/s
 //   3584 rows of 256 000, bfloat16, top 20              315 us (285)
-//   5 rows of 32 000, float32, top 8                    6.4 us: two launches and a chain of trips to L2
+//   5 rows of 32 000, float32, top 8                    5.5 us (in one launch: logprobs_few_kernel): a chain of trips to L2 and barriers
 // The stream is bound by HBM with float32; with 16 bits the special-function unit (one ex2 an entry, busy for 69 % of the cycles) and the
 // issue of 7 instructions an entry come up to it, and pass it at the clocks the power limit leaves.  Eight vectors a lane (two tiles, one
 // ahead, are all the registers of 16 warps an SM) beat four with 24 or 32 warps: 65 us, 72 and 74 without likeliest tokens.
@@ -42,7 +42,7 @@ constexpr int kVecs = 8;                   // vectors of 16 bytes that a lane ha
 constexpr int kTileVecs = 32 * kVecs;      // of a tile: 4 KB, a warp's step
 constexpr int kEndThreads = 128, kEndWarps = kEndThreads / 32;
 // Few rows: CTAs of a row (a cluster) and their warps; the rows and tiles of a row up to which they are taken.
-constexpr int kFewCtas = 8, kFewWarps = kFewCtas * kEndWarps, kFewRows = 37, kFewTiles = 128;
+constexpr int kFewCtas = 8, kFewWarps = kFewCtas * kEndWarps, kFewRows = 148, kFewTiles = 128;
 constexpr int kPicked = 512;               // slots and entries that the quick selection takes
 constexpr int kMaxSms = 148;                // the workspace is laid out for as many
 constexpr float kSlack = 8.f;        // how far l may be above the reference
@@ -661,7 +661,8 @@ LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
   LogPlan q;
   const int es = d->dtype == SPECSTEER_F32 ? 4 : 2;
   q.tiles = (int)(((long long)d->V * es / 16 + kTileVecs - 1) / kTileVecs);
-  // One launch, and no workspace, for up to two CTAs an SM and four tiles a warp (kFewRows, kFewTiles): see kFewCtas.
+  // One launch, and no workspace, up to kFewRows rows of kFewTiles tiles (four a warp).  bfloat16, top 20: 64 rows of 151 936 take 11.0 us, with
+  // two launches 13.7; 148 rows of 32 000 11.3 and 11.6; 296 rows 19.6 and 13.7.  One row of 151 936 7.3 and 6.8, but the call 9.8 and 12.8.
   q.few = d->R <= kFewRows && q.tiles <= kFewTiles;
   const long long total = (long long)d->R * q.tiles, most = (long long)sm * kCtas * (kThreads / 32);
   q.warps = total < most ? total : most;

@@ -475,21 +475,21 @@ def test_logprobs_match_definition(binding, R, V, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("off,ld", [(0, 1001), (1, 1003), (3, 1008), (7, 1040)])
-def test_logprobs_of_rows_of_any_alignment(binding, off, ld, dtype):
+@pytest.mark.parametrize("R", [12, 170])
+def test_logprobs_of_rows_of_any_alignment(binding, R, off, ld, dtype):
     g = torch.Generator().manual_seed(off + ld)
-    buf = torch.full((12 * ld + 16,), NAN).to(dtype)
-    x = buf.cuda()[off:off + 12 * ld].view(12, ld)[:, :1000]
-    x.copy_((torch.randn(12, 1000, generator=g) * 3).to(dtype))
-    _check_logprobs(binding, x, torch.randint(0, 1000, (12,), generator=g, dtype=torch.int32).cuda(), None, 9)
+    buf = torch.full((R * ld + 16,), NAN).to(dtype)
+    x = buf.cuda()[off:off + R * ld].view(R, ld)[:, :1000]
+    x.copy_((torch.randn(R, 1000, generator=g) * 3).to(dtype))
+    _check_logprobs(binding, x, torch.randint(0, 1000, (R,), generator=g, dtype=torch.int32).cuda(), None, 9)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("kind", ["flat", "masked", "lowest", "half_masked", "ascending", "descending", "one_spike", "ties", "two_values", "huge", "all_lowest"])
-@pytest.mark.parametrize("V", [700, 40003])
-def test_logprobs_of_odd_rows(binding, V, kind, dtype):
+@pytest.mark.parametrize("R,V", [(4, 700), (4, 40003), (170, 700), (170, 5003)])
+def test_logprobs_of_odd_rows(binding, R, V, kind, dtype):
     """Rows with many equal entries, masked vocabularies, sorted rows, a spike, values next to the type's end."""
     g = torch.Generator().manual_seed(V)
-    R = 4
     x = torch.randn(R, V, generator=g).to(dtype)
     low = torch.finfo(dtype).min
     if kind == "flat":
@@ -532,7 +532,8 @@ def test_logprobs_of_odd_rows(binding, V, kind, dtype):
 
 
 @pytest.mark.parametrize("V", [50, 9001])
-def test_logprobs_of_rows_that_have_none(binding, V):
+@pytest.mark.parametrize("times", [1, 20])
+def test_logprobs_of_rows_that_have_none(binding, times, V):
     """NaN, +inf, nothing but -inf, temperatures that make no sense, tokens outside: said in the status, the others as alone."""
     g = torch.Generator().manual_seed(V)
     x = torch.randn(10, V, generator=g).cuda()
@@ -543,8 +544,13 @@ def test_logprobs_of_rows_that_have_none(binding, V):
     tokens = torch.zeros(10, 3, dtype=torch.int32, device="cuda")
     tokens[0] = i32([V, -1, 3])
     tokens[1, 0], tokens[9] = -2, i32([2 ** 31 - 1, -2 ** 31, V - 1])
-    status = i32([0] * 10)
-    got = binding.token_logprobs(x, tokens, temperature=temp, top=4, status=status)
+    status = i32([0] * 10 * times)
+    got = binding.token_logprobs(x.repeat(times, 1), tokens.repeat(times, 1), temperature=temp.repeat(times), top=4, status=status)
+    for k in got:   # (the sums of equal rows may be cut at different places)
+        a, b = got[k], got[k][:10].repeat([times] + [1] * (got[k].dim() - 1))
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.isinf(), b.isinf()) and (a.nan_to_num(7, 8, 9) - b.nan_to_num(7, 8, 9)).abs().max() < 1e-4
+    assert torch.equal(status, status[:10].repeat(times))
+    got, status = {k: v[:10] for k, v in got.items()}, status[:10]
     NONFINITE, BAD_TOKEN, BAD_PARAM = binding.REQ_NONFINITE, binding.REQ_BAD_TOKEN, binding.REQ_BAD_PARAM
     assert status.tolist() == [BAD_TOKEN, NONFINITE | BAD_TOKEN, NONFINITE, NONFINITE] + [BAD_PARAM] * 4 + [NONFINITE, BAD_TOKEN]
     for r in range(1, 9):
