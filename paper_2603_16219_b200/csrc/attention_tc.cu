@@ -131,7 +131,8 @@ struct TcParams {
   float* part;                         // [2*gridDim][256][DP] unnormalised sums
   float2* part_ml;                     // [2*gridDim][256] reference (raw score) and sum
   int* head;                           // [gridDim][8] 0: slot of the part of a unit that goes on in the next CTA (-1: none), 2..4: that
-                                       // unit; 1: this CTA's part of a unit that began before it (0: none, 1: its end, 2: more)
+                                       // unit's first row, kv head and tokens; 1: this CTA's part of a unit that began before it (0: none,
+                                       // 1: its end, 2: more)
   int* failed;                         // [gridDim] whether a bounded wait of the CTA has run out
   int stop_at;                         // blocks of keys after which a CTA loads no more (see SPECSTEER_ATTENTION_STOP)
 };
@@ -1059,7 +1060,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       if (tid == 0 && !whole) {
         int* h = p.head + blockIdx.x * 8;
-        if (x.starts) { h[0] = slot; h[2] = x.b; h[3] = x.hk; h[4] = x.u; }
+        if (x.starts) { h[0] = slot; h[2] = x.row0 + x.tok0; h[3] = x.hk; h[4] = x.tok1 - x.tok0; }
         else h[1] = x.ends ? 1 : 2;
       }
       if (!two) meet(true);   // both halves of the sums are read before either stream goes on
@@ -1104,7 +1105,7 @@ __global__ void __launch_bounds__(256, 4) attention_join_kernel(const __grid_con
   const int cta = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // what every row begins with, on its way before anything is known to be needed (the addresses are the workspace's own)
   const int4 h = *reinterpret_cast<const int4*>(p.head + cta * 8);
-  const int u = p.head[cta * 8 + 4], first_kind = lane == 0 ? 2 : cta + lane < n_cta ? p.head[(cta + lane) * 8 + 1] : 1;
+  const int tokens = p.head[cta * 8 + 4], first_kind = lane == 0 ? 2 : cta + lane < n_cta ? p.head[(cta + lane) * 8 + 1] : 1;
   const int failed = threadIdx.x < n_cta ? p.failed[threadIdx.x] : 0;   // (at most kMaxCtas of them, fewer than the threads)
   const int slot0 = h.x;
   const bool first_block = blockIdx.x == 0 && blockIdx.y == 0;
@@ -1114,9 +1115,7 @@ __global__ void __launch_bounds__(256, 4) attention_join_kernel(const __grid_con
     return;
   }
   if (slot0 < 0) return;
-  const AttnRequest rq = request_of<TREE>(p, h.z);
-  const Unit x = make_unit<TREE>(p, rq, u);
-  const int rows = (x.tok1 - x.tok0) * p.G, tile_rows = p.tile_tok * p.G;
+  const int rows = tokens * p.G, tile_rows = p.tile_tok * p.G;
   for (int q = blockIdx.y * 8 + warp; q < rows; q += gridDim.y * 8) {
     const int part_row = q < tile_rows ? q : 128 + q - tile_rows;
     float m = kNegInf, l = 0.f, o[DP / 32];
@@ -1169,8 +1168,8 @@ __global__ void __launch_bounds__(256, 4) attention_join_kernel(const __grid_con
         }
       }
     }
-    const int tok = x.tok0 + q / p.G, head = h.w * p.G + q % p.G;
-    const long long row = (long long)rq.row0 + tok;
+    const int head = h.w * p.G + q % p.G;
+    const long long row = (long long)h.z + q / p.G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     unsigned short* dst = reinterpret_cast<unsigned short*>(p.d.out) + row * p.d.o_tok + head * p.d.o_head;
 #pragma unroll
