@@ -598,7 +598,8 @@ specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc *d
  * (equal rows of a call need not: their sums may be cut at different places).
  * R, n_tokens >= 0; 1 <= V; 0 <= n_top <= min(V, SPECSTEER_TOP_MAX); ld_row >= V.  dtype F32, BF16 or F16.  Any alignment is taken,
  * and rows of any length.  workspace: 32-byte aligned device memory of at least specsteer_token_logprobs_workspace(desc) bytes, whose content
- * before and after the call means nothing; calls that may overlap need one each.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
+ * before and after the call means nothing; calls that may overlap need one each.  Up to 740 rows (fewer of a large vocabulary) need none (0 bytes).
+ * Errors: INVALID_ARG, WORKSPACE, CUDA. */
 #define SPECSTEER_TOP_MAX 32
 typedef struct {
   int32_t R, V, n_tokens, n_top, dtype;

@@ -44,8 +44,9 @@ constexpr int kThreads = 256, kCtas = 2;   // of the streaming kernel, on an SM
 constexpr int kVecs = 8;                   // vectors of 16 bytes that a lane has of a tile
 constexpr int kTileVecs = 32 * kVecs;      // of a tile: 4 KB, a warp's step
 constexpr int kEndThreads = 128, kEndWarps = kEndThreads / 32;
-// Few rows: CTAs of a row (a cluster) and their warps; the rows and tiles of a row up to which they are taken.
-constexpr int kFewCtas = 8, kFewWarps = kFewCtas * kEndWarps, kFewRows = 148, kFewTiles = 128;
+// Few rows: the most CTAs of a row (a cluster), and the tiles that a CTA takes (four a warp).
+constexpr int kFewCtas = 8, kFewTiles = 16;
+constexpr int kFewSm = 5, kFewMax = kFewSm * 148;   // CTAs that an SM holds, and all of them
 constexpr int kPicked = 512;               // slots and entries that the quick selection takes
 constexpr int kMaxSms = 148;                // the workspace is laid out for as many
 constexpr float kSlack = 8.f;        // how far l may be above the reference
@@ -622,16 +623,17 @@ __global__ void __launch_bounds__(kEndThreads, 10) logprobs_end_kernel(const Log
 
 // Few rows of few tiles: a cluster reads a row, leaves records and slots in its first CTA's shared memory, and that one ends it.
 template <int DT>
-__global__ void __launch_bounds__(kEndThreads) logprobs_few_kernel(const LogParams p) {
+__global__ void __launch_bounds__(kEndThreads, kFewSm) logprobs_few_kernel(const LogParams p) {
   __shared__ EndShared sh;
-  __shared__ __align__(16) uint16_t slot_s[kFewTiles * 32];
-  __shared__ float4 record_s[kFewWarps];
+  __shared__ __align__(16) uint16_t slot_s[kFewCtas * kFewTiles * 32];
+  __shared__ float4 record_s[kFewCtas * kEndWarps];
   cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int ctas = (int)cluster.num_blocks(), warps = ctas * kEndWarps;
   const int rank = (int)cluster.block_rank(), lane = threadIdx.x & 31, w = rank * kEndWarps + (threadIdx.x >> 5);
-  const i64 r = blockIdx.x / kFewCtas;
+  const i64 r = blockIdx.x / ctas;
   const Row<DT> row(p.d, r);
   const float c = kLog2e / (p.d.temperature ? p.d.temperature[r] : 1.f);
-  const int first = p.tiles * w / kFewWarps, end = p.tiles * (w + 1) / kFewWarps;
+  const int first = p.tiles * w / warps, end = p.tiles * (w + 1) / warps;
   const uint64_t policy = l2_policy_evict_first();
   uint4 v[kVecs];
   if (first < end) load_tile(row, first, lane, policy, v);
@@ -655,18 +657,22 @@ __global__ void __launch_bounds__(kEndThreads) logprobs_few_kernel(const LogPara
   const float s = warp_sum(a.s), ww = warp_sum(a.w);
   if (lane == 0) records[w] = make_float4(M, s, ww, 0.f);
   auto all_written = [&] { cluster.sync(); };   // (nobody reads another's memory from there on)
-  if (rank == 0) end_row<DT>(p, r, sh, record_s, kFewWarps, slot_s, all_written);
+  if (rank == 0) end_row<DT>(p, r, sh, record_s, warps, slot_s, all_written);
   else all_written();
 }
 
-struct LogPlan { int tiles, grid; bool few; long long warps; size_t record_bytes, max_bytes; };
+struct LogPlan { int tiles, grid, few; long long warps; size_t record_bytes, max_bytes; };
 LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
   LogPlan q;
   const int es = d->dtype == SPECSTEER_F32 ? 4 : 2;
   q.tiles = (int)(((long long)d->V * es / 16 + kTileVecs - 1) / kTileVecs);
-  // One launch, and no workspace, up to kFewRows rows of kFewTiles tiles (four a warp).  bfloat16, top 20: 64 rows of 151 936 take 11.0 us, with
-  // two launches 13.7; 148 rows of 32 000 11.3 and 11.6; 296 rows 19.6 and 13.7.  One row of 151 936 7.3 and 6.8, but the call 9.8 and 12.8.
-  q.few = d->R <= kFewRows && q.tiles <= kFewTiles;
+  // One launch, and no workspace, while all of its CTAs are on the SMs at once: clusters of as many CTAs as that leaves a row.  bfloat16, top
+  // 20, device / call: 64 rows of 151 936 take 11.0 / 12.6 us, with two launches 13.7 / 16.2; 300 rows of 8000 8.4 / 10.3, 11.0 / 12.9; 740
+  // rows of 16 000 12.0 / 14.4, 14.8 / 16.5; but 900 of them, in another round of CTAs, 16.9, 15.9.  With twice as many CTAs 160 rows of 32 000
+  // take 13.5 instead of 9.5.
+  q.few = 0;
+  for (int ctas = kFewCtas; ctas > 0 && !q.few; ctas /= 2)
+    if ((long long)d->R * ctas <= kFewMax && q.tiles <= ctas * kFewTiles) q.few = ctas;
   const long long total = (long long)d->R * q.tiles, most = (long long)sm * kCtas * (kThreads / 32);
   q.warps = total < most ? total : most;
   q.grid = (int)((q.warps + kThreads / 32 - 1) / (kThreads / 32));
@@ -678,12 +684,12 @@ LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
 template <int DT> cudaError_t launch(const LogParams& p, const LogPlan& q, cudaStream_t s) {
   if (q.few) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.d.R * kFewCtas);
+    cfg.gridDim = dim3(p.d.R * q.few);
     cfg.blockDim = dim3(kEndThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kFewCtas;
+    attr[0].val.clusterDim.x = q.few;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;

@@ -460,7 +460,7 @@ def _check_logprobs(binding, x, tokens=None, temperature=None, top=0):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
-@pytest.mark.parametrize("R,V", [(1, 1), (3, 2), (5, 7), (4, 33), (9, 255), (6, 1000), (1, 4099), (300, 1111), (40, 32000), (3, 151936), (1, 256000)])
+@pytest.mark.parametrize("R,V", [(1, 1), (3, 2), (5, 7), (4, 33), (9, 255), (6, 1000), (1, 4099), (300, 1111), (900, 1111), (40, 32000), (150, 31000), (3, 151936), (1, 256000), (1, 300001)])
 def test_logprobs_match_definition(binding, R, V, dtype):
     g = torch.Generator().manual_seed(R + V)
     x = (torch.randn(R, V, generator=g) * 3).to(dtype).cuda()
@@ -475,7 +475,7 @@ def test_logprobs_match_definition(binding, R, V, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("off,ld", [(0, 1001), (1, 1003), (3, 1008), (7, 1040)])
-@pytest.mark.parametrize("R", [12, 170])
+@pytest.mark.parametrize("R", [12, 170, 760])
 def test_logprobs_of_rows_of_any_alignment(binding, R, off, ld, dtype):
     g = torch.Generator().manual_seed(off + ld)
     buf = torch.full((R * ld + 16,), NAN).to(dtype)
@@ -486,7 +486,7 @@ def test_logprobs_of_rows_of_any_alignment(binding, R, off, ld, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("kind", ["flat", "masked", "lowest", "half_masked", "ascending", "descending", "one_spike", "ties", "two_values", "huge", "all_lowest"])
-@pytest.mark.parametrize("R,V", [(4, 700), (4, 40003), (170, 700), (170, 5003)])
+@pytest.mark.parametrize("R,V", [(4, 700), (4, 40003), (170, 5003), (760, 700), (760, 5003)])
 def test_logprobs_of_odd_rows(binding, R, V, kind, dtype):
     """Rows with many equal entries, masked vocabularies, sorted rows, a spike, values next to the type's end."""
     g = torch.Generator().manual_seed(V)
@@ -532,7 +532,7 @@ def test_logprobs_of_odd_rows(binding, R, V, kind, dtype):
 
 
 @pytest.mark.parametrize("V", [50, 9001])
-@pytest.mark.parametrize("times", [1, 20])
+@pytest.mark.parametrize("times", [1, 20, 80])
 def test_logprobs_of_rows_that_have_none(binding, times, V):
     """NaN, +inf, nothing but -inf, temperatures that make no sense, tokens outside: said in the status, the others as alone."""
     g = torch.Generator().manual_seed(V)

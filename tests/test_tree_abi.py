@@ -108,7 +108,7 @@ def test_attention_refuses(binding):
     assert fn(_tree(binding, a=dict(T=0), mask=None), None) == binding.OK
 
 
-LOG = dict(R=300, V=100, n_tokens=1, n_top=5, dtype=1, ld_row=100, ld_tok=1, workspace_bytes=1 << 30)
+LOG = dict(R=3000, V=100, n_tokens=1, n_top=5, dtype=1, ld_row=100, ld_tok=1, workspace_bytes=1 << 30)
 
 
 @pytest.mark.parametrize("bad", [dict(R=-1), dict(V=0), dict(n_tokens=-1), dict(n_top=-1), dict(n_top=33), dict(V=4, ld_row=4), dict(ld_row=99), dict(dtype=3), dict(ld_tok=0),
