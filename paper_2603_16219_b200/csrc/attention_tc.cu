@@ -39,7 +39,7 @@
 // and of trees (specsteer_tree_attention):
 //   64 trees of 15 to 32 rows, up to 4000 keys, 64 heads               170 to 203 us (168 to 194), 0.5 to 0.6 PFLOP/s of useful products: bound by the
 //     ends of its pieces (one every 17 tiles) and the join; without softmax and most of the products it takes 150 us
-//   2 trees of 49 to 63 rows, 30 to 120 thousand keys, 32 heads        171 to 204 us (164 to 197), 0.75 to 0.9 PFLOP/s: bound by the chain of scores, weights
+//   2 trees of 49 to 63 rows, 30 to 120 thousand keys, 32 heads        171 to 207 us (164 to 197), 0.75 to 0.9 PFLOP/s: bound by the chain of scores, weights
 //     and sums (152 us without the arithmetic of the softmax, 119 without most of the products too)
 //   48 trees of up to 25 rows, 32 heads of 64, window 1024, float16    43 to 45 us: ends of pieces
 #include <cuda.h>
