@@ -178,7 +178,7 @@ rotate_kernel(const specsteer_rotate_append_desc p, const int parts_log, const i
   auto weights = [&](const void* weight) {
 #pragma unroll
     for (int i = 0; i < H; ++i) w0[i] = w1[i] = 1.f;
-    if (weight && mine) {
+    if (weight && mine && p.eps >= 0.f) {   // (weights belong to the norm)
       if (p.weight_dtype == SPECSTEER_F32) {
 #pragma unroll
         for (int i = 0; i < H; ++i) { w0[i] = ((const float*)weight)[e0 + i]; w1[i] = ((const float*)weight)[e1 + i]; }
