@@ -18,7 +18,7 @@
 namespace specsteer {
 namespace {
 
-constexpr int kGenRows = 16, kGenKeys = 32, kGenThreads = 128, kGenWarps = kGenThreads / 32, kGenSplit = 8;
+constexpr int kGenRows = 16, kGenKeys = 32, kGenThreads = 128, kGenWarps = kGenThreads / 32, kGenSplit = 8, kGenCtas = 4;
 constexpr int kGenMaxD = SPECSTEER_ATTENTION_MAX_D;
 
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -27,8 +27,10 @@ __device__ __forceinline__ void from_f32(float x, __nv_bfloat16* y) { *y = __flo
 __device__ __forceinline__ void from_f32(float x, __half* y) { *y = __float2half_rn(x); }
 
 // Blocks of kGenRows rows are numbered request by request; a block finds its request from the lengths (device data).
+// Four CTAs an SM, which the host's rule for splitting blocks counts on: without the bound the trees' form takes 139 registers, three
+// CTAs, and 64 trees of 15 to 32 rows over 130 to 4000 keys, 16/4 heads of 256, 6.05 ms instead of 4.62 (chains of the same lengths 4.63, 4.56).
 template <typename T, bool TREE>
-__global__ void __launch_bounds__(kGenThreads) attention_generic_kernel(const specsteer_attention_desc p, const TreeMask tree) {
+__global__ void __launch_bounds__(kGenThreads, kGenCtas) attention_generic_kernel(const specsteer_attention_desc p, const TreeMask tree) {
   __shared__ float qs[kGenRows][kGenMaxD];   // the queries; at the end of a split block its sums
   __shared__ T ks[kGenKeys][kGenMaxD + 2];   // an odd number of words a row: 8 keys in 8 banks
   __shared__ float ps[kGenRows][kGenKeys];
@@ -291,9 +293,9 @@ specsteer_status run_attention(const specsteer_attention_desc* d, const TreeMask
   const long long blocks = ((long long)d->T * (d->Hq / d->Hkv) + kGenRows - 1) / kGenRows + d->B;
   const int sm = current_sm_count();
   if (sm <= 0) return SPECSTEER_ERR_CUDA;
-  // A cluster of 8 a block while the blocks do not fill the SMs (four CTAs each) four times over: 5 rows over 720 keys of
+  // A cluster of 8 a block while the blocks do not fill the SMs (kGenCtas each) four times over: 5 rows over 720 keys of
   // width 256 take 51 us (one CTA a block: 250 us), a batch of 64 single tokens of width 256 1.6 ms (2.4 ms).
-  const int split = blocks * d->Hkv <= (long long)sm * 16 ? kGenSplit : 1;
+  const int split = blocks * d->Hkv <= (long long)sm * kGenCtas * 4 ? kGenSplit : 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)) * split, d->Hkv);
   cfg.blockDim = dim3(kGenThreads);
