@@ -80,7 +80,7 @@ template <int DP> struct TcLayout {
 
 // A piece of work: key tiles [first, first + take) of one unit (see Unit).
 struct Piece {
-  int b, hk, u;
+  int b, hk;
   int row0, n, kv;             // of the request
   int tok0, tok1;              // the unit's tokens
   int two;                     // two query tiles
@@ -425,7 +425,7 @@ template <bool TREE> struct Walk {
     }
   }
   __device__ __forceinline__ void publish(Piece* q) const {
-    q->b = b; q->hk = hk; q->u = u;
+    q->b = b; q->hk = hk;
     q->row0 = rq.row0; q->n = rq.n; q->kv = rq.kv;
     q->tok0 = x.tok0; q->tok1 = x.tok1; q->two = x.two;
     q->lo_first = x.lo_first; q->hi_first = x.hi_first; q->lo_last = x.lo_last;
