@@ -539,7 +539,7 @@ specsteer_status specsteer_tree_plan(const specsteer_tree_plan_desc *desc, void 
 
 /* What stands between a layer's projections and its attention, in one pass over T rows of Hq query heads and Hkv key and
  * value heads of width D.  For every head x of q and of k:
- *   norm     with eps >= 0:  x <- x / sqrt(mean(x^2) + eps) * weight     (weight NULL: 1; eps < 0: no norm)
+ *   norm     with eps >= 0:  x <- x / sqrt(mean(x^2) + eps) * weight     (weight NULL: 1; eps < 0: no norm and no weights)
  *   turn     for i < rot/2, with p = positions[axis_of[i]][t] and the angle a = p * inv_freq[i]:
  *            (x_i, x_j) <- factor * (x_i cos a - x_j sin a, x_j cos a + x_i sin a), where (i, j) = (i, i + rot/2), or
  *            (2i, 2i+1) with neighbours != 0.  Elements from rot on are not turned (nor multiplied by factor).
@@ -550,7 +550,8 @@ specsteer_status specsteer_tree_plan(const specsteer_tree_plan_desc *desc, void 
  * outside [0, n_axes) leaves its pair unturned (angle 0).
  * T, Hq, Hkv >= 0 (any may be 0: nothing to do for those), 1 <= D <= SPECSTEER_ROTATE_MAX_D, 0 <= rot <= D, even.  Strides in
  * elements, the innermost axis dense; any strides (q_out's and the caches' not zero on axes longer than one) and alignment
- * are taken, 16-byte multiples with rot a multiple of 16 (with neighbours: of 8) are faster.  dtype (of q, k, v, q_out and the caches) and weight_dtype:
+ * are taken; 16-byte multiples with D and rot multiples of 16 (float32: of 8) are fastest, 8-byte multiples with multiples of 8
+ * (float32: of 4, D up to 128) next.  Squares are float32 too, and pass its range with elements above 2^60.  dtype (of q, k, v, q_out and the caches) and weight_dtype:
  * F32, BF16 or F16.  Errors: INVALID_ARG, UNSUPPORTED (D), CUDA. */
 #define SPECSTEER_ROTATE_MAX_D 256
 typedef struct {
@@ -594,7 +595,8 @@ specsteer_status specsteer_tree_attention(const specsteer_tree_attention_desc *d
  * A token outside [0, V) has logprob -inf, and BAD_TOKEN is set unless it is -1 (no token).  A row that holds NaN or +inf, or nothing
  * but -inf, or whose lse is no finite float32, gets NaN everywhere, ids of -1, and NONFINITE; so does one whose temperature is not
  * positive and finite, with BAD_PARAM.  lse and entropy may be NULL; so may row_status,
- * into which bits are OR-ed.  Sums in float32, one read of the logits.  The same call gives the same bits
+ * into which bits are OR-ed.  Logits and temperatures may lie anywhere in float32's range; a log probability below it is -inf.
+ * Sums in float32, one read of the logits.  The same call gives the same bits
  * (equal rows of a call need not: their sums may be cut at different places).
  * R, n_tokens >= 0; 1 <= V; 0 <= n_top <= min(V, SPECSTEER_TOP_MAX); ld_row >= V.  dtype F32, BF16 or F16.  Any alignment is taken,
  * and rows of any length.  workspace: 32-byte aligned device memory of at least specsteer_token_logprobs_workspace(desc) bytes, whose content
@@ -620,7 +622,9 @@ specsteer_status specsteer_token_logprobs(const specsteer_token_logprobs_desc *d
 size_t specsteer_token_logprobs_workspace(const specsteer_token_logprobs_desc *desc);
 
 /* The end of a round over trees.  token[row] is a row's token, choice[row] the one that the model emits behind it (its likeliest,
- * or one sampled from its probabilities: then the emitted tokens follow the model's law).  Per request:
+ * or one sampled from its probabilities: then the emitted tokens follow the model's law).  A round without drafts over the rows
+ * (specsteer_verify_round and specsteer_recover_sample with B = T, K = 0 and SPECSTEER_FLAG_BONUS) samples and steers such choices: its
+ * rec_token.  What earlier calls refused (req_status) is not looked at here.  Per request:
  *   path[0] = 0;   path[i+1] = the lowest row whose parent is path[i] and whose token is choice[path[i]], while there is one
  *   and i + 1 < max_out (a negative choice, as specsteer_token_logprobs has it for rows without probabilities, is nobody's token);
  *   n_out = the length of the path (0 when the request has no rows)

@@ -37,11 +37,13 @@
 //     sit in one warp of each stream, whose 2000 clocks a block of 64 keys (1500 of arithmetic and tensor-memory latency,
 //     500 of handshakes) bound it
 // and of trees (specsteer_tree_attention):
-//   64 trees of 15 to 32 rows, up to 4000 keys, 64 heads               170 to 203 us (168 to 194), 0.5 to 0.6 PFLOP/s of useful products: bound by the
+//   64 trees of 15 to 32 rows, up to 4000 keys, 64 heads               196 to 207 us (168 to 203), 0.5 to 0.6 PFLOP/s of useful products: bound by the
 //     ends of its pieces (one every 17 tiles) and the join; without softmax and most of the products it takes 150 us
-//   2 trees of 49 to 63 rows, 30 to 120 thousand keys, 32 heads        171 to 207 us (164 to 197), 0.75 to 0.9 PFLOP/s: bound by the chain of scores, weights
+//   2 trees of 49 to 63 rows, 30 to 120 thousand keys, 32 heads        196 to 207 us (164 to 203), 0.71 to 0.75 PFLOP/s (to 0.9): bound by the chain of scores, weights
 //     and sums (152 us without the arithmetic of the softmax, 119 without most of the products too)
-//   48 trees of up to 25 rows, 32 heads of 64, window 1024, float16    43 to 45 us: ends of pieces
+//   48 trees of up to 25 rows, 32 heads of 64, window 1024, float16    42 to 45 us: ends of pieces
+//   a tree of 1024 rows, 1100 keys, 32 heads                           73 us where a chain takes 44: masks need not be trees, so every unit of it
+//     reads all of the chunk's keys, at the edge
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

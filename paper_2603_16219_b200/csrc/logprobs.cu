@@ -19,10 +19,10 @@
 // CTA's shared memory, and that CTA ends the row.  It needs no workspace, so that a call is 5 us shorter on the host.
 //
 // Measured (a pass among others of a captured graph on changing rows; in brackets what its bytes would take at the copy bandwidth):
-//   1280 rows of 151 936, bfloat16, tempered, top 20    76 us (60), 82 to 88 in a loop of a second; without likeliest tokens 64 us
-//   640 rows of 151 936, float32, top 20                69 us (60); without 61 us, 6.3 TB/s
-//   3584 rows of 256 000, bfloat16, top 20              315 us (285)
-//   5 rows of 32 000, float32, top 8                    5.5 us (in one launch: logprobs_few_kernel): a chain of trips to L2 and barriers
+//   1280 rows of 151 936, bfloat16, tempered, top 20    74 to 75 us (60), 82 to 88 in a loop of a second; without likeliest tokens 64.5 us
+//   640 rows of 151 936, float32, top 20                69 us (60); without 61 us, 6.4 TB/s
+//   3584 rows of 256 000, bfloat16, top 20              306 us (285)
+//   5 rows of 32 000, float32, top 8                    6 us (in one launch: logprobs_few_kernel): a chain of trips to L2 and barriers
 // The stream is bound by HBM with float32; with 16 bits the special-function unit (one ex2 an entry, busy for 69 % of the cycles) and the
 // issue of 7 instructions an entry come up to it, and pass it at the clocks the power limit leaves.  Eight vectors a lane (two tiles, one
 // ahead, are all the registers of 16 warps an SM) beat four with 24 or 32 warps: 65 us, 72 and 74 without likeliest tokens.
@@ -44,7 +44,8 @@ constexpr int kThreads = 256, kCtas = 2;   // of the streaming kernel, on an SM
 constexpr int kVecs = 8;                   // vectors of 16 bytes that a lane has of a tile
 constexpr int kTileVecs = 32 * kVecs;      // of a tile: 4 KB, a warp's step
 constexpr int kEndThreads = 128, kEndWarps = kEndThreads / 32;
-// Few rows: the most CTAs of a row (a cluster), and the tiles that a CTA takes (four a warp).
+// Few rows: the most CTAs of a row (a cluster), and the tiles that a CTA takes (four a warp).  No CTA waits for one of another row, so that
+// all of them being on a B200's 148 SMs at once is a matter of time only; the bound is the same on a device with fewer.
 constexpr int kFewCtas = 8, kFewTiles = 16;
 constexpr int kFewSm = 5, kFewMax = kFewSm * 148;   // CTAs that an SM holds, and all of them
 constexpr int kPicked = 512;               // slots and entries that the quick selection takes
@@ -686,7 +687,7 @@ LogPlan plan_of(const specsteer_token_logprobs_desc* d, int sm) {
   LogPlan q;
   const int es = d->dtype == SPECSTEER_F32 ? 4 : 2;
   q.tiles = (int)(((long long)d->V * es / 16 + kTileVecs - 1) / kTileVecs);
-  // One launch, and no workspace, while all of its CTAs are on the SMs at once: clusters of as many CTAs as that leaves a row.  bfloat16, top
+  // One launch, and no workspace, up to the CTAs that 148 SMs hold at once: clusters of as many as that leaves a row.  bfloat16, top
   // 20, device / call: 64 rows of 151 936 take 11.0 / 12.6 us, with two launches 13.7 / 16.2; 300 rows of 8000 8.4 / 10.3, 11.0 / 12.9; 740
   // rows of 16 000 12.0 / 14.4, 14.8 / 16.5; but 900 of them, in another round of CTAs, 16.9, 15.9.  With twice as many CTAs 160 rows of 32 000
   // take 13.5 instead of 9.5.

@@ -1,19 +1,24 @@
 // Norm by head, rotation by position, and the keys and values into their slots: what stands between a layer's projections
 // and its attention, in one pass.
 //
-// A block takes a row (token).  Its angles are formed once, in float64, where the product of a position of 2^31 and a frequency keeps 24
-// bits behind the point of a turn, and reduced to a turn before the sine; all heads of the row share them.
+// Angles are formed in float64, where the product of a position of 2^31 and a frequency keeps 24 bits behind the point of a turn, and
+// reduced to a turn before the sine; all heads that a warp (rotate_kernel) or a block (rotate_any_kernel) takes of a row (token) share them.
 //
-//   rotate_kernel      a warp a row, or several that share its heads where rows are few; no warp waits for another.  A lane has a piece
+//   rotate_kernel      a warp a row, or up to eight that share its heads where rows are few; each forms the row's angles for itself, and
+//                      none waits for another.  A lane has a piece
 //                      (16 bytes; 8 where the widths or alignments want it) of each half of a head, or two neighbouring pieces, so
 //                      that the elements of a pair meet in it, and with weights w, the norm r and an element's partner x' an
-//                      element becomes r (x A + x' B), A = w cos and B = -+w' sin, formed once a row for the queries and once
-//                      for the keys.  The words come through shared
+//                      element becomes r (x A + x' B), A = w cos and B = -+w' sin, formed once a row and warp for the queries and
+//                      once for the keys.  The words come through shared
 //                      memory, by asynchronous copies several steps ahead, which takes no registers.
-//                      Measured, bfloat16 heads of 128 with norm: 7671 rows of 32 + 2 x 8 heads, three axes, 37 us (5.1 TB/s; 29 at the copy
-//                      bandwidth), bound by the copies in flight and, at 45 % of its slots, by issue; 1280 rows of 64 + 2 x 8 heads 13.4 us
-//                      (8.2): a warp's walk along its row; 5 rows 3.6 us.  With the words in registers 42 us, with pieces of 8 bytes 48.
-//   rotate_any_kernel  every shape, alignment and width: a warp a head, an element a lane (the two cases above: 72 and 205 us, bound by issue).
+//                      Measured (a pass of a captured graph on changing inputs), heads of 128 with norm, bfloat16 unless said: 7671 rows of
+//                      32 + 2 x 8 heads, three axes, 36.4 us (5.2 TB/s; 29.3 at the copy bandwidth), bound by the copies in flight and, at 45 % of
+//                      its slots, by issue; with one axis 34.7, without norm 32.6, neighbours 46, half of each head turned 40.5; float32 (58.6
+//                      at the copy bandwidth) 61, neighbours 90, half turned 70.  1280 rows of 64 + 2 x 8 heads 13.1 us (8.1): a warp's walk
+//                      along its row.  5 rows of 64 + 2 x 8 heads 4.0 us, of 32 + 2 x 8 3.6.  The case with three axes took 42 us with
+//                      the words in registers, 48 with pieces of 8 bytes.
+//   rotate_any_kernel  every shape, alignment and width: a block a row, a warp a head, an element a lane, bound by issue (1280 and 7671 rows
+//                      above: 72 and 205 us; 3000 rows of 32 + 2 x 8 heads of 33 69 us).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -361,8 +366,8 @@ bool takes_pieces(const specsteer_rotate_append_desc* d, int bytes) {
 
 template <int DT, int WORDS, int G> void launch_as(const specsteer_rotate_append_desc& d, int sm, cudaStream_t s) {
   // Warps a row: as many as the SMs hold at once (kRotWarps each), since a warp waits more than it computes, and another round of
-  // warps costs more than it shares.  bfloat16, 64 and 2 x 8 heads of 128: 5 rows 4.0 us with 8 warps a row (1: 10.2), 400 rows
-  // 5.4 with 4 (8: 8.0, 1: 10.7), 1283 rows 14.4 with 1 (2: 15.3, 8: 19.3).
+  // warps costs more than it shares.  bfloat16, 64 + 2 x 8 heads of 128, inputs that change: 5 rows 3.8 us with 8 warps a
+  // row (4: 4.5, 1: 9.5), 400 rows 6.9 with 4 (8: 8.8, 2: 7.9, 1: 10.5), 1280 rows 13.2 with 1 (2: 15.4, 8: 18.5).
   const long long steps = ((long long)d.Hq + 2 * d.Hkv) * G / 32;
   int parts_log = 0, page_log = -1;
   while (parts_log < 3 && ((long long)d.T << (parts_log + 1)) <= (long long)sm * kRotWarps && steps >= 2 << parts_log) ++parts_log;

@@ -2,14 +2,15 @@
 //
 //   tree_plan_kernel   a block a request: parents into shared memory, then a thread a row climbs to its root.  Ancestors come
 //                      in falling order, so the words of a row's mask are written one after the other as the climb leaves
-//                      them, and no mask is held in registers.  Bound by latency: launch, parents' trip, the climb.  A tree of 9 rows 1.9 us,
-//                      256 trees of 3 to 200 rows 3.4 us.
+//                      them, and no mask is held in registers.  Bound by latency: launch, parents' trip, the climb.  A tree of 9 rows 1.8 us,
+//                      256 trees of 3 to 200 rows 3.3 us.  The climb is a chain of reads of shared memory, one a step: a bushy tree of 1024 rows
+//                      23 us, a star of as many 18 us, a chain of 1024, where every row climbs to the front, 441 us.
 //   tree_keep_kernel   every block of a request finds the path for itself (a pass over the rows gives each row its confirmed
 //                      child, then as many steps as the path is long), and moves its share of the keys and values.  A
 //                      thread owns a column, 16 bytes of one head in one layer's keys or values, and moves it along the path:
 //                      rows only move towards the front, so what a column's later steps read its earlier ones have not written.
 //                      Bound by latency: rows, their parents' choices, table, keys.  A tree of 9 rows in 36 layers 3.9 us, 64 trees
-//                      of 15 to 32 rows in 16 layers 5.7 us (11 MB moved).
+//                      of 15 to 32 rows in 16 layers 5.9 us (11 MB moved).
 #include <cuda_runtime.h>
 
 #include "common.cuh"
